@@ -58,6 +58,7 @@ extern "C" {
 #define KF_PAGE_SIZE 16
 #define KF_HEAD_DIM 128
 #define KF_MAX_GROUP 16 /* num_q_heads / num_kv_heads may not exceed this */
+#define KF_MAX_DRAFT 64 /* drafted tokens per sequence of kf_tree_attn */
 
 /* One entry of the routing table (Section 4.1), single-GPU form: a token
  * range of one request and the pages that hold it.  `part` names the
@@ -339,6 +340,109 @@ int kf_decode_step_no_alloc(const kf_shape* shape, const void* q, void* k_pool, 
                             const int32_t* page_ids, const int32_t* seq_route_begin,
                             float* o_part, float* lse_part, float* out, float* lse_out,
                             int32_t* err_flags, void* stream);
+
+/*
+ * Operators on whole rows of tokens: a prompt's (or an accepted draft's) K/V
+ * written into the cache, the prompt's attention over it, and the attention of
+ * a tree of drafted tokens.  Rows of all sequences are packed one after
+ * another; `*_stride` is the distance between two rows in elements, so that
+ * q, K and V may be parts of one projection's output (a multiple of 8, at
+ * least the row's own length; the elements of a row are contiguous).
+ */
+
+/*
+ * kf_kv_append_rows -- append of several tokens per route (Section 3.2: the K/V
+ * of a prompt, stored at its range's node; after a tree of drafted tokens, the
+ * rows of the accepted path).  Route r takes the entries
+ * e = route_entry_begin[r] .. route_entry_begin[r+1] - 1 in order: entry e is
+ * row row_list[e] (row e if row_list is NULL) of k_rows and v_rows, bfloat16
+ * [num_rows][num_kv_heads][128] with row_stride elements between rows.  The
+ * pools, scales and route rows are left bit for bit as one kf_kv_append per
+ * token, in this order, would leave them (fp8 pools: its E4M3 rule), and
+ * routes[r].tok_end grows by the route's entries.  route_entry_begin has
+ * num_routes + 1 values; num_entries bounds them (the length of row_list; at
+ * most num_rows without one).
+ * A route takes all of its rows or none.  Device checks (flag, that route
+ * unchanged): its row of the table (0 <= seq < num_seqs, tok_end >= tok_begin,
+ * page_base >= 0, pages in page_ids), its reserved pages (KF_EFLAG_TAIL_FULL),
+ * the page ids that it writes to (KF_EFLAG_BAD_PAGE), its row indices in
+ * [0, num_rows) (KF_EFLAG_BAD_ROUTE).  A route_entry_begin that decreases or
+ * leaves [0, num_entries] sets KF_EFLAG_BAD_ROUTE and appends nothing at all.
+ * workspace: kf_kv_append_rows_workspace_bytes(num_routes), 16-byte aligned.
+ * Alignment: k_rows, v_rows and pools 16 bytes, the rest 4.
+ */
+size_t kf_kv_append_rows_workspace_bytes(int32_t num_routes);
+int kf_kv_append_rows(const kf_shape* shape, void* k_pool, void* v_pool, float* k_scale,
+                      float* v_scale, const void* k_rows, const void* v_rows, int32_t num_rows,
+                      int64_t row_stride, const int32_t* row_list, int32_t num_entries,
+                      const int32_t* route_entry_begin, kf_route* routes, int32_t num_routes,
+                      const int32_t* page_ids, void* workspace, size_t workspace_bytes,
+                      int32_t* err_flags, void* stream);
+
+/*
+ * kf_rows_attn_workspace_bytes -- device scratch that kf_prompt_attn and
+ * kf_tree_attn need for num_rows query rows of shape->num_seqs sequences on
+ * the current device: the launch's list of work items, and the partials of
+ * rows whose keys are split over several workgroups.  It does not depend on
+ * the routes, the pages or the lengths.  No initialisation is needed; contents
+ * are dead between calls; calls that may overlap (graphs among them) need
+ * workspaces of their own.  Returns 0 for invalid arguments and for sizes that
+ * the launches do not take.  Host only.
+ */
+size_t kf_rows_attn_workspace_bytes(const kf_shape* shape, int32_t num_rows);
+
+/*
+ * kf_prompt_attn -- causal attention of packed prompts, whole or in chunks, over
+ * their cached K/V (their own tokens appended before, kf_kv_append_rows).  Row
+ * i in [seq_row_begin[b], seq_row_begin[b+1]) belongs to sequence b and sits at
+ * its logical position p = first_pos[b] + i - seq_row_begin[b]; over the
+ * resident tokens t <= p of the routes
+ * seq_route_begin[b] .. seq_route_begin[b+1] - 1, for query head h,
+ *   s_t = scale * (q[i][h] . k_t),
+ *   out[i][h][:] = sum_t softmax(s)_t v_t   (bfloat16)
+ *   lse[i][h]    = ln sum_t exp(s_t)        (float32)
+ * A row that sees no token gives out = 0, lse = -inf.  A token that a row does
+ * not see never changes the row, whatever it holds.  The weights enter their
+ * product with V as bfloat16 (their sum as float32): the output's own precision.
+ * q and out are [num_rows][num_q_heads][128] bfloat16 (q with q_stride elements
+ * between rows), lse [num_rows][num_q_heads]; rows outside
+ * [seq_row_begin[0], seq_row_begin[num_seqs]) are left as they were.
+ * Device checks: a seq_row_begin that decreases or leaves [0, num_rows] sets
+ * KF_EFLAG_BAD_ROUTE and makes every row of out and lse NaN; a sequence whose
+ * seq_route_begin is inconsistent or that lists a route of another sequence or
+ * one that fails kf_partial_attn's checks sets KF_EFLAG_BAD_ROUTE and makes its
+ * rows NaN; a page id outside the pool sets KF_EFLAG_BAD_PAGE and makes the
+ * rows NaN that see a token of that page.  Sequences without rows are not
+ * looked at.
+ * Alignment: q, pools and out 16 bytes, workspace 256, the rest 4.
+ */
+int kf_prompt_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64_t q_stride,
+                   const int32_t* seq_row_begin, const int32_t* first_pos, const void* k_pool,
+                   const void* v_pool, const float* k_scale, const float* v_scale,
+                   const kf_route* routes, int32_t num_routes, int32_t max_pages_per_route,
+                   const int32_t* page_ids, const int32_t* seq_route_begin, void* out, float* lse,
+                   void* workspace, size_t workspace_bytes, int32_t* err_flags, void* stream);
+
+/*
+ * kf_tree_attn -- attention of drafted tokens over the cache and over their own
+ * tree.  Rows as for kf_prompt_attn, at most KF_MAX_DRAFT per sequence; row i
+ * of sequence b sees every resident token of the sequence's routes and the
+ * drafted rows seq_row_begin[b] + j for the bits j set in tree_mask[i] (its
+ * ancestors, and itself if its own bit is set; bits past the sequence's last
+ * row are ignored).  k_draft and v_draft hold the drafted tokens' K/V, bfloat16
+ * [num_rows][num_kv_heads][128] with kv_stride elements between rows; they are
+ * not in the cache: append the rows that are accepted with kf_kv_append_rows.
+ * Outputs, checks and alignment as for kf_prompt_attn (k_draft and v_draft 16
+ * bytes, tree_mask 8); a sequence of more than KF_MAX_DRAFT rows sets
+ * KF_EFLAG_BAD_ROUTE and makes its rows NaN.
+ */
+int kf_tree_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64_t q_stride,
+                 const void* k_draft, const void* v_draft, int64_t kv_stride,
+                 const uint64_t* tree_mask, const int32_t* seq_row_begin, const void* k_pool,
+                 const void* v_pool, const float* k_scale, const float* v_scale,
+                 const kf_route* routes, int32_t num_routes, int32_t max_pages_per_route,
+                 const int32_t* page_ids, const int32_t* seq_route_begin, void* out, float* lse,
+                 void* workspace, size_t workspace_bytes, int32_t* err_flags, void* stream);
 
 /*
  * kf_debug_gather -- test export: the resident tokens of route `route`

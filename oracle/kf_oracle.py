@@ -325,6 +325,128 @@ def _append_e4m3(page, scales, pid, g, slot, x_bits, kmajor):
         page[:, slot] = codes
 
 
+# --------------------------------------------------- operators on whole rows
+def kv_append_rows(k_pool, v_pool, routes, page_ids, k_rows, v_rows, route_entry_begin,
+                   row_list=None, *, num_seqs, k_scale=None, v_scale=None):
+    """Several tokens per route: route r takes the entries
+    route_entry_begin[r] .. route_entry_begin[r+1] - 1 in order (entry e is row
+    row_list[e], or row e), each as kv_append stores one token; all of a route's
+    entries or none.  Works on copies; returns as kv_append."""
+    fp8 = k_pool.dtype == np.uint8
+    k_pool, v_pool = k_pool.copy(), v_pool.copy()
+    if fp8:
+        k_scale, v_scale = (np.array(x, np.float32, copy=True) for x in (k_scale, v_scale))
+    routes = np.array(routes, np.int32, copy=True)
+    begin = np.asarray(route_entry_begin, np.int64)
+    entries = len(k_rows) if row_list is None else len(row_list)
+    flags = 0
+    if begin[0] < 0 or np.any(np.diff(begin) < 0) or begin[-1] > entries:
+        flags = EFLAG_BAD_ROUTE
+        begin = np.zeros_like(begin)
+    for r in range(len(routes)):
+        mine = np.arange(begin[r], begin[r + 1])
+        n = len(mine)
+        if n == 0:
+            continue
+        rows = mine if row_list is None else np.asarray(row_list, np.int64)[mine]
+        seq, _, tb, te, base, cap = (int(x) for x in routes[r])
+        j = te - tb + np.arange(n)
+        if not 0 <= seq < num_seqs or te < tb or te + n >= 2 ** 31:
+            flags |= EFLAG_BAD_ROUTE
+            continue
+        if j[-1] // PAGE >= cap:
+            flags |= EFLAG_TAIL_FULL
+            continue
+        if base < 0 or base + j[-1] // PAGE >= len(page_ids):
+            flags |= EFLAG_BAD_ROUTE
+            continue
+        pids = np.asarray(page_ids)[base + j // PAGE]
+        if np.any((pids < 0) | (pids >= k_pool.shape[0])):
+            flags |= EFLAG_BAD_PAGE
+            continue
+        if np.any((rows < 0) | (rows >= len(k_rows))):
+            flags |= EFLAG_BAD_ROUTE
+            continue
+        for pid, slot, row in zip(pids, j % PAGE, rows):
+            if fp8:
+                for g in range(k_pool.shape[1]):
+                    _append_e4m3(k_pool[pid, g], k_scale, pid, g, slot, k_rows[row, g], kmajor=True)
+                    _append_e4m3(v_pool[pid, g], v_scale, pid, g, slot, v_rows[row, g], kmajor=False)
+            else:
+                k_pool[pid, :, slot, :] = k_rows[row]
+                v_pool[pid, :, :, slot] = v_rows[row]
+        routes[r, 3] = te + n
+    if fp8:
+        return k_pool, v_pool, k_scale, v_scale, routes, flags
+    return k_pool, v_pool, routes, flags
+
+
+def rows_attn(q, row_begin, k_pool, v_pool, routes, page_ids, seq_route_begin, *, num_kv_heads,
+              scale, max_pages_per_route, first_pos=None, tree_mask=None, k_draft=None,
+              v_draft=None, k_scale=None, v_scale=None, max_draft=64):
+    """Attention of packed query rows (bf16 bits [N, Hq, d]) over the cache of
+    their sequences.  Prompts (first_pos): row i of sequence b sits at position
+    first_pos[b] + i - row_begin[b] and sees the resident tokens up to it.  Trees
+    (tree_mask): it sees every resident token, and the drafted rows
+    row_begin[b] + j (bf16 bits [N, Hkv, d]) of its mask's bits j.
+
+    Returns out [N, Hq, d], lse [N, Hq], flags, and spread [N, Hq, d]: the
+    weighted mean of |v|, by which roundings of the weights are bounded.  Rows
+    of no sequence stay NaN with lse NaN; a row that sees nothing is (0, -inf)."""
+    N, Hq, d = q.shape
+    G = Hq // num_kv_heads
+    out, lse = np.full((N, Hq, d), np.nan), np.full((N, Hq), np.nan)
+    spread = np.zeros((N, Hq, d))
+    begin = np.asarray(row_begin, np.int64)
+    if begin[0] < 0 or np.any(np.diff(begin) < 0) or begin[-1] > N:
+        return out, lse, EFLAG_BAD_ROUTE, spread
+    flags = 0
+    for b in range(len(begin) - 1):
+        i0, i1 = int(begin[b]), int(begin[b + 1])
+        if i1 == i0:
+            continue
+        r0, r1 = int(seq_route_begin[b]), int(seq_route_begin[b + 1])
+        if (not 0 <= r0 <= r1 <= len(routes)
+                or any(not _route_ok(routes[r], len(begin) - 1, len(page_ids), max_pages_per_route)
+                       or int(routes[r][0]) != b for r in range(r0, r1))
+                or (tree_mask is not None and i1 - i0 > max_draft)):
+            flags |= EFLAG_BAD_ROUTE
+            continue
+        tok = np.concatenate([np.arange(routes[r][2], routes[r][3], dtype=np.int64)
+                              for r in range(r0, r1)] + [np.zeros(0, np.int64)])
+        pids = np.concatenate([np.asarray(page_ids)[routes[r][4] + np.arange(routes[r][3] - routes[r][2]) // PAGE]
+                               for r in range(r0, r1)] + [np.zeros(0, np.int64)])
+        bad = (pids < 0) | (pids >= k_pool.shape[0])
+        safe = np.where((np.asarray(page_ids) < 0) | (np.asarray(page_ids) >= k_pool.shape[0]), 0,
+                        np.asarray(page_ids))
+        n = i1 - i0
+        if tree_mask is None:
+            sees = tok[None, :] <= (int(first_pos[b]) + np.arange(n))[:, None]
+        else:
+            bits = np.asarray(tree_mask[i0:i1]).astype(np.int64).view(np.uint64)
+            drafted = (bits[:, None] >> np.arange(n, dtype=np.uint64)[None, :]) & np.uint64(1)
+            sees = np.concatenate([np.ones((n, len(tok)), bool), drafted.astype(bool)], 1)
+            bad = np.concatenate([bad, np.zeros(n, bool)])
+        for g in range(num_kv_heads):
+            parts = [gather_kv(routes[r], safe, k_pool, v_pool, g, k_scale, v_scale)
+                     for r in range(r0, r1)]
+            K = np.concatenate([k for k, _ in parts] + [np.zeros((0, d))])
+            V = np.concatenate([v for _, v in parts] + [np.zeros((0, d))])
+            if tree_mask is not None:
+                K = np.concatenate([K, bf16_to_f64(k_draft[i0:i1, g])])
+                V = np.concatenate([V, bf16_to_f64(v_draft[i0:i1, g])])
+            for i in range(n):
+                at = sees[i]
+                if np.any(bad & at):
+                    flags |= EFLAG_BAD_PAGE
+                    continue
+                rows = bf16_to_f64(q[i0 + i, g * G:(g + 1) * G])
+                out[i0 + i, g * G:(g + 1) * G], lse[i0 + i, g * G:(g + 1) * G] = attend(
+                    rows, K[at], V[at], scale)
+                spread[i0 + i, g * G:(g + 1) * G] = attend(rows, K[at], np.abs(V[at]), scale)[0]
+    return out, lse, flags, spread
+
+
 # --------------------------------------------------------------------- bytes
 def kv_footprint_bytes(seq_lens, num_kv_heads, head_dim, num_layers=1, elem_bytes=2):
     """KV footprint of a batch (Section 4.2, post-prefill initialisation):

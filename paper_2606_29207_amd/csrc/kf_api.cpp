@@ -16,7 +16,13 @@ bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p
 
 size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-// Checks shared by append and partial attention.
+hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
+
+}  // namespace
+
+namespace kf {
+
+// Checks shared by append and attention.
 int check_shape(const kf_shape* s) {
   if (!s) return KF_ERR_INVALID_ARG;
   if (s->num_seqs < 0 || s->num_q_heads <= 0 || s->num_kv_heads <= 0 || s->num_pages < 1 ||
@@ -33,15 +39,10 @@ int check_shape(const kf_shape* s) {
   return KF_OK;
 }
 
-hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
-
-}  // namespace
-
-namespace kf {
-
 namespace {
 constexpr int kMaxDevices = 64;
 std::atomic<int> g_cu_count[kMaxDevices];
+}  // namespace
 
 // Compute units of the current device (queried once per device; 256 when no
 // device is visible, so that sizes can be computed on a host without a GPU).
@@ -60,7 +61,6 @@ int cu_count() {
   g_cu_count[dev].store(n, std::memory_order_relaxed);
   return n;
 }
-}  // namespace
 
 bool ragged_table(int64_t num_page_ids, int32_t num_routes, int32_t max_pages_per_route) {
   // The page table is under 90% of routes x max pages: the routes reserve
@@ -355,7 +355,7 @@ const char* kf_version(void) { return "kf 0.1 gfx950"; }
 
 size_t kf_partial_attn_workspace_bytes(const kf_shape* shape, int32_t num_routes,
                                        int32_t max_pages_per_route) {
-  if (check_shape(shape) != KF_OK || num_routes < 0 || max_pages_per_route < 0) return 0;
+  if (kf::check_shape(shape) != KF_OK || num_routes < 0 || max_pages_per_route < 0) return 0;
   if (num_routes > kf::kMaxLaunchRoutes || shape->num_kv_heads > kf::kMaxLaunchRoutes) return 0;
   const int32_t group = shape->num_q_heads / shape->num_kv_heads;
   const bool fp8 = shape->kv_dtype == KF_KV_FP8_E4M3;
@@ -388,7 +388,7 @@ size_t kf_partial_attn_workspace_bytes(const kf_shape* shape, int32_t num_routes
 int kf_partial_attn_plan(const kf_shape* shape, int32_t num_launch, int32_t max_pages_per_route,
                          int32_t route_list_launch, int32_t* chunk_pages, int32_t* max_chunks,
                          int32_t* units_per_wg) {
-  const int st = check_shape(shape);
+  const int st = kf::check_shape(shape);
   if (st != KF_OK) return st;
   if (num_launch < 0 || max_pages_per_route < 0 || (route_list_launch != 0 && route_list_launch != 1))
     return KF_ERR_INVALID_ARG;
@@ -431,7 +431,7 @@ int prepare_append(const kf_shape* shape, void* k_pool, void* v_pool, float* k_s
                    float* v_scale, const void* k_new, const void* v_new, kf_route* routes,
                    int32_t num_routes, const int32_t* tail_route, const int32_t* page_ids,
                    int32_t* err_flags, kf::AppendArgs& a) {
-  int st = check_shape(shape);
+  int st = kf::check_shape(shape);
   if (st != KF_OK) return st;
   if (num_routes < 0) return KF_ERR_INVALID_ARG;
   if (shape->num_seqs == 0) return KF_OK;
@@ -471,7 +471,7 @@ int prepare_partial(const kf_shape* shape, const void* q, const void* k_pool, co
                     int32_t max_pages_per_route, const int32_t* page_ids, float* o_part,
                     float* lse_part, void* workspace, size_t workspace_bytes, int32_t* err_flags,
                     kf::PartialArgs& a) {
-  int st = check_shape(shape);
+  int st = kf::check_shape(shape);
   if (st != KF_OK) return st;
   if (num_routes < 0 || num_launch < 0 || max_pages_per_route < 0) return KF_ERR_INVALID_ARG;
   if (num_launch == 0) return KF_OK;
@@ -712,7 +712,7 @@ int kf_debug_gather(const kf_shape* shape, const void* k_pool, const void* v_poo
                     const kf_route* routes, int32_t num_routes, int32_t route,
                     int32_t max_pages_per_route, const int32_t* page_ids, int32_t max_tokens,
                     void* out_k, void* out_v, int32_t* err_flags, void* stream) {
-  const int st = check_shape(shape);
+  const int st = kf::check_shape(shape);
   if (st != KF_OK) return st;
   if (num_routes < 0 || route < 0 || route >= num_routes || max_pages_per_route < 0 ||
       max_tokens < 0)

@@ -33,6 +33,9 @@ constexpr int kMergeRowsFourWaves = 8;   // mean rows per sequence from which fo
 constexpr int kOrderBuckets = 64;        // range-size classes of the dispatch order
 constexpr int64_t kMaxOrderItems = int64_t(1) << 20;  // largest split launch given a dispatch order
 
+// Checks of a kf_shape that the entry points share.
+int check_shape(const kf_shape* s);
+
 struct AppendArgs {
   void* k_pool;
   void* v_pool;
@@ -195,6 +198,9 @@ bool ordered_dispatch(const ChunkPlan& plan, int32_t num_launch, int32_t num_kv_
                       int64_t slots);
 WorkspaceLayout workspace_layout(int32_t num_routes, int32_t num_kv_heads, int32_t group,
                                  int32_t max_chunks, bool ordered);
+
+// Compute units of the current device (256 when none is visible).
+int cu_count();
 
 // Address of the current device's scratch array (KF_SCRATCH_BYTES, for
 // kf_decode_step_no_alloc), looked up once per device.

@@ -1,0 +1,1093 @@
+// gfx950 kernels of the operators on whole rows of tokens:
+//   append_plan_kernel, append_tile_kernel -- rows of K/V into the paged cache
+//   rows_plan_kernel     -- work items of an attention launch
+//   rows_kernel          -- attention of prompt rows or drafted trees over it
+//   rows_combine_kernel  -- reduction of the row tiles whose keys were split
+#include "kf_rows.h"
+
+namespace kf {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLn2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+__device__ __forceinline__ float qnan() { return __builtin_nanf(""); }
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  bf16x2 v = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// Slice index of (page, KV head) in a pool of either layout.
+__device__ __forceinline__ size_t slice_of(int page, int g, int H, int P, int32_t head_major) {
+  return head_major ? (size_t)g * P + page : (size_t)page * H + g;
+}
+
+template <class T>
+__device__ __forceinline__ u32x4 ld16(const T* p) {
+  return *reinterpret_cast<const u32x4*>(p);
+}
+
+// ------------------------------------------------------------------- append
+// E4M3FN codes of two floats, round to nearest even, clamped to +-448, the
+// sign bit the input's (a NaN becomes 448), in the low half.
+__device__ __forceinline__ uint32_t e4m3_pair(float x, float y) {
+  x = __builtin_copysignf(fminf(fabsf(x), 448.0f), x);
+  y = __builtin_copysignf(fminf(fabsf(y), 448.0f), y);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false) & 0xFFFFu;
+}
+
+// Values of the two codes in the low half (exact).
+__device__ __forceinline__ f32x2 e4m3_values(uint32_t codes) {
+  const uint32_t b = __builtin_bit_cast(
+      uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, false));
+  return f32x2{__builtin_bit_cast(float, b << 16), __builtin_bit_cast(float, b & 0xFFFF0000u)};
+}
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) x = fmaxf(x, __shfl_xor(x, m));
+  return x;
+}
+
+// One route's check, by a whole workgroup: its tokens before the append, or -1
+// if it takes no rows (flag says why).
+__device__ int append_check(const AppendRowsArgs& a, int r, int& flag) {
+  const int tid = threadIdx.x, nt = blockDim.x;
+  // the whole table of entries: nondecreasing within [0, num_entries]
+  int bad = 0;
+  for (int i = tid; i <= a.num_routes; i += nt) {
+    const int v = a.entry_begin[i];
+    bad |= v < 0 || v > a.num_entries || (i > 0 && a.entry_begin[i - 1] > v);
+  }
+  if (__syncthreads_or(bad)) {
+    flag = KF_EFLAG_BAD_ROUTE;
+    return -1;
+  }
+  const int e0 = a.entry_begin[r], n = a.entry_begin[r + 1] - e0;
+  if (n == 0) return -1;
+  const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + r);
+  const int seq = rp[0], tb = rp[2], te = rp[3], base = rp[4], cap = rp[5];
+  const int64_t j0 = (int64_t)te - tb, last = (j0 + n - 1) / kPage;
+  if (seq < 0 || seq >= a.num_seqs || j0 < 0 || (int64_t)te + n > INT32_MAX || j0 + n > INT32_MAX) {
+    flag = KF_EFLAG_BAD_ROUTE;
+    return -1;
+  }
+  if (last >= cap) {
+    flag = KF_EFLAG_TAIL_FULL;
+    return -1;
+  }
+  if (base < 0 || base + last >= a.num_page_ids) {
+    flag = KF_EFLAG_BAD_ROUTE;
+    return -1;
+  }
+  bad = 0;
+  for (int64_t p = j0 / kPage + tid; p <= last; p += nt) {
+    const int id = a.page_ids[base + p];
+    if (id < 0 || id >= a.num_pages) bad |= KF_EFLAG_BAD_PAGE;
+  }
+  if (a.row_list) {
+    for (int i = tid; i < n; i += nt) {
+      const int row = a.row_list[e0 + i];
+      if (row < 0 || row >= a.num_rows) bad |= KF_EFLAG_BAD_ROUTE;
+    }
+  }
+  const int page = __syncthreads_or(bad & KF_EFLAG_BAD_PAGE);
+  const int row = __syncthreads_or(bad & KF_EFLAG_BAD_ROUTE);
+  flag = page ? KF_EFLAG_BAD_PAGE : row ? KF_EFLAG_BAD_ROUTE : 0;
+  return flag ? -1 : (int)j0;
+}
+
+// The slots [s0, s1) of one page of one KV head, K or V, filled from the rows of
+// entries e0 .. by one wave.
+template <bool FP8>
+__device__ void append_page(const AppendRowsArgs& a, int page, int g, bool is_v, int s0, int s1,
+                            int e0, uint16_t* lds) {
+  const int lane = threadIdx.x & 63, H = a.num_kv_heads;
+  const size_t head = slice_of(page, g, H, a.num_pages, a.head_major);
+  const uint16_t* rows = (is_v ? a.v_rows : a.k_rows) + (size_t)g * kDim;
+  auto row_of = [&](int s) -> int64_t {
+    const int e = e0 + s - s0;
+    return (a.row_list ? a.row_list[e] : e) * a.row_stride;
+  };
+  if (!FP8 && !is_v) {  // sixteen lanes a row
+    uint16_t* k = static_cast<uint16_t*>(a.k_pool) + head * (kPage * kDim);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int s = 4 * i + (lane >> 4);
+      if (s >= s0 && s < s1)
+        *reinterpret_cast<u32x4*>(k + s * kDim + 8 * (lane & 15)) =
+            ld16(rows + row_of(s) + 8 * (lane & 15));
+    }
+    return;
+  }
+  uint32_t x[kPage];  // dims 2 lane, 2 lane + 1 of each token
+#pragma unroll
+  for (int s = 0; s < kPage; ++s)
+    x[s] = s >= s0 && s < s1 ? reinterpret_cast<const uint32_t*>(rows + row_of(s))[lane] : 0;
+  if constexpr (!FP8) {  // two rows of sixteen slots a lane
+    u32x4* v = reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.v_pool) + head * (kPage * kDim)) +
+               4 * lane;
+    u32x4 r[4] = {};
+    if (s1 - s0 < kPage) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = v[i];
+    }
+#pragma unroll
+    for (int d = 0; d < 2; ++d)
+#pragma unroll
+      for (int s = 0; s < kPage; ++s) {
+        const uint32_t bits = (d ? x[s] >> 16 : x[s] & 0xFFFFu) << (16 * (s & 1));
+        const uint32_t keep = s & 1 ? 0xFFFFu : 0xFFFF0000u;
+        const int at = 2 * d + (s >> 3), wd = (s & 7) >> 1;
+        if (s >= s0 && s < s1) r[at][wd] = (r[at][wd] & keep) | bits;
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = r[i];
+  } else {
+    // The E4M3 append rule, token after token, in float32: the token at slot 0
+    // sets scale = amax / 28; a later one beyond 448 scale re-encodes the slots
+    // before it to amax / 28; each is stored as RNE(x / scale).
+    uint8_t* pool = static_cast<uint8_t*>(is_v ? a.v_pool : a.k_pool) + head * (kPage * kDim);
+    float* scale_at = (is_v ? a.v_scale : a.k_scale) + (size_t)page * H + g;
+    uint16_t* codes = lds + lane;  // [slot][lane]: the code pairs of this lane's dims
+    if (is_v) {
+      uint32_t w[8];
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const u32x4 r = ld16(pool + (2 * lane + d) * kPage);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[4 * d + i] = r[i];
+      }
+#pragma unroll
+      for (int s = 0; s < kPage; ++s)
+        codes[64 * s] = (uint16_t)((w[s >> 2] >> (8 * (s & 3)) & 0xFFu) |
+                                   (w[4 + (s >> 2)] >> (8 * (s & 3)) & 0xFFu) << 8);
+    } else {
+      for (int s = 0; s < s0; ++s) codes[64 * s] = reinterpret_cast<uint16_t*>(pool)[64 * s + lane];
+    }
+    float scale = s0 > 0 ? *scale_at : 0.0f;
+#pragma unroll
+    for (int s = 0; s < kPage; ++s) {
+      if (s < s0 || s >= s1) continue;
+      const float x0 = __builtin_bit_cast(float, x[s] << 16);
+      const float x1 = __builtin_bit_cast(float, x[s] & 0xFFFF0000u);
+      const float amax = wave_max(fmaxf(fabsf(x0), fabsf(x1)));
+      if (s == 0) {
+        scale = amax > 0.0f ? amax / 28.0f : 1.0f;
+      } else if (amax > 448.0f * scale) {
+        const float fresh = amax / 28.0f;
+#pragma unroll 1
+        for (int t = 0; t < s; ++t) {
+          const f32x2 old = e4m3_values(codes[64 * t]);
+          codes[64 * t] = (uint16_t)e4m3_pair(old.x * scale / fresh, old.y * scale / fresh);
+        }
+        scale = fresh;
+      }
+      codes[64 * s] = (uint16_t)e4m3_pair(x0 / scale, x1 / scale);
+    }
+    if (is_v) {
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        u32x4 r = {0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < kPage; ++s)
+          r[s >> 2] |= (uint32_t)((codes[64 * s] >> (8 * d)) & 0xFFu) << (8 * (s & 3));
+        *reinterpret_cast<u32x4*>(pool + (2 * lane + d) * kPage) = r;
+      }
+    } else {
+      for (int s = 0; s < s1; ++s) reinterpret_cast<uint16_t*>(pool)[64 * s + lane] = codes[64 * s];
+    }
+    if (lane == 0) *scale_at = scale;
+  }
+}
+
+// One workgroup per route: the check; the plan of its pages, or with DIRECT the
+// pages themselves; the route's new end.
+template <bool FP8, bool DIRECT>
+__global__ __launch_bounds__(512) void append_plan_kernel(AppendRowsArgs a) {
+  __shared__ uint16_t lds[FP8 && DIRECT ? 8 * kPage * 64 : 1];
+  const int r = blockIdx.x;
+  int flag = 0;
+  const int j0 = append_check(a, r, flag);
+  if (threadIdx.x == 0 && flag) atomicOr(a.err_flags, flag);
+  if (!DIRECT && threadIdx.x == 0) a.plan[4 * r] = j0;
+  if (j0 < 0) return;
+  const int e0 = a.entry_begin[r], n = a.entry_begin[r + 1] - e0;
+  const int base = a.routes[r].page_base;
+  if constexpr (DIRECT) {
+    const int p0 = j0 / kPage, pages = (j0 + n - 1) / kPage - p0 + 1, w = threadIdx.x >> 6;
+    const int units = 2 * a.num_kv_heads;
+    for (int64_t u = w; u < (int64_t)pages * units; u += 8) {
+      const int p = p0 + (int)(u / units), k = (int)(u % units);
+      const int s0 = p == p0 ? j0 % kPage : 0;
+      const int s1 = min(kPage, j0 + n - p * kPage);
+      append_page<FP8>(a, uniform(a.page_ids[base + p]), k >> 1, k & 1, s0, s1,
+                       e0 + p * kPage + s0 - j0, lds + (FP8 ? w * kPage * 64 : 0));
+    }
+  } else if (threadIdx.x == 0) {
+    a.plan[4 * r + 1] = e0;
+    a.plan[4 * r + 2] = n;
+    a.plan[4 * r + 3] = base;
+  }
+  __syncthreads();  // every thread has read tok_end before it moves
+  if (threadIdx.x == 0) a.routes[r].tok_end += n;
+}
+
+// One wave per (page tile, KV head, K or V).  Route r has the tiles
+// floor(entry_begin[r] / 16) + 2 r and on: at least its n / 16 + 2 pages fit
+// before the next route's.
+template <bool FP8>
+__global__ __launch_bounds__(256) void append_tile_kernel(AppendRowsArgs a) {
+  __shared__ uint16_t lds[FP8 ? 4 * kPage * 64 : 1];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + w;
+  const int units = 2 * a.num_kv_heads;
+  const int64_t tile = unit / units;
+  const int k = (int)(unit % units);
+  // the last route whose first tile is at most `tile`: 64 probes a step
+  int lo = 0, hi = a.num_routes;  // first(lo) <= tile < first(hi)
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+    const bool in = at < hi && (int64_t)(a.entry_begin[at] / kPage) + 2 * (int64_t)at <= tile;
+    const uint64_t v = __ballot(in);
+    // a table that decreases can answer anything; a plan is then never made
+    const int last = v ? 63 - __builtin_clzll(v) : 0;
+    lo += last * step;
+    hi = min(hi, lo + step);
+  }
+  const int j0 = a.plan[4 * lo];
+  if (j0 < 0) return;
+  const int e0 = a.plan[4 * lo + 1], n = a.plan[4 * lo + 2], base = a.plan[4 * lo + 3];
+  const int p0 = j0 / kPage;
+  const int64_t p = p0 + tile - (e0 / kPage + 2 * (int64_t)lo);
+  if (p < p0 || p > (j0 + n - 1) / kPage) return;
+  const int s0 = p == p0 ? j0 % kPage : 0;
+  const int s1 = (int)min((int64_t)kPage, j0 + n - p * kPage);
+  append_page<FP8>(a, uniform(a.page_ids[base + p]), k >> 1, k & 1, s0, s1,
+                   (int)(e0 + p * kPage + s0 - j0), lds + (FP8 ? w * kPage * 64 : 0));
+}
+
+// --------------------------------------------------------------------- plan
+__device__ __forceinline__ bool route_ok(const RowsArgs& a, int b, const int32_t* rp) {
+  const int64_t n = (int64_t)rp[3] - rp[2], pages = n > 0 ? (n + kPage - 1) / kPage : 0;
+  return rp[0] == b && n >= 0 && n <= INT32_MAX && rp[4] >= 0 && pages <= rp[5] &&
+         pages <= a.max_pages_per_route && rp[4] + pages <= a.num_page_ids;
+}
+
+__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor((long long)x, m);
+  return x;
+}
+
+// Key tiles of row tile t of sequence b (an estimate where ranges do not follow
+// one another from the first token on).
+template <bool TREE>
+__device__ __forceinline__ int key_tiles(const RowsArgs& a, int b, int t, int n, int tokens,
+                                         int first) {
+  if (TREE) return (tokens + kKeyTile - 1) / kKeyTile + 1;
+  const int64_t rows = ((int64_t)(t + 1) * kRowTile - 1) / a.group;
+  const int64_t end = a.first_pos[b] + (rows < n ? rows : n - 1) + 1 - first;
+  const int64_t see = end < 0 ? 0 : end < tokens ? end : tokens;
+  return (int)((see + kKeyTile - 1) / kKeyTile);
+}
+
+// One workgroup: the row tiles of every sequence, cut into parts of at most
+// `cap` key tiles, largest first.
+template <bool TREE>
+__global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
+  __shared__ unsigned long long s_work;
+  __shared__ int s_most, s_recs, s_splits;
+  __shared__ int s_count[64], s_scan[16];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, B = a.num_seqs;
+  int bad = 0;
+  for (int b = tid; b <= B; b += 1024) {
+    const int v = a.seq_row_begin[b];
+    bad |= v < 0 || v > a.num_rows || (b > 0 && a.seq_row_begin[b - 1] > v);
+  }
+  if (tid == 0) s_work = 0, s_most = 0;
+  if (tid < 64) s_count[tid] = 0;
+  if (__syncthreads_or(bad)) {
+    if (tid == 0) {
+      a.head[0] = -1;
+      a.head[1] = 0;
+      atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
+    }
+    return;
+  }
+  // the sequences' resident tokens, a wave each
+  for (int b = w; b < B; b += 16) {
+    const int n = a.seq_row_begin[b + 1] - a.seq_row_begin[b];
+    if (n == 0) continue;
+    const int r0 = a.seq_route_begin[b], r1 = a.seq_route_begin[b + 1];
+    bool wrong = r0 < 0 || r1 < r0 || r1 > a.num_routes || (TREE && n > KF_MAX_DRAFT);
+    int64_t tokens = 0;
+    int first = INT32_MAX;
+    if (!wrong) {
+      bool mine = true;
+      for (int r = r0 + lane; r < r1; r += 64) {
+        const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + r);
+        mine &= route_ok(a, b, rp);
+        tokens += (int64_t)rp[3] - rp[2];
+        first = min(first, rp[2]);
+      }
+      wrong = __ballot(!mine) != 0;
+    }
+    tokens = wave_sum(tokens);
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) first = min(first, __shfl_xor(first, m));
+    if (lane == 0) {
+      a.seq_info[4 * b] = (int)min(tokens, (int64_t)INT32_MAX - 2 * kKeyTile);
+      a.seq_info[4 * b + 1] = first;
+      a.seq_info[4 * b + 2] = wrong;
+      if (wrong) atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
+    }
+  }
+  // their first row tiles
+  int sum = 0;
+  for (int b0 = 0; b0 < B; b0 += 1024) {
+    const int b = b0 + tid;
+    const int64_t n = b < B ? a.seq_row_begin[b + 1] - a.seq_row_begin[b] : 0;
+    const int mine = (int)((n * a.group + kRowTile - 1) / kRowTile);
+    int x = mine;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const int y = __shfl_up(x, m);
+      if (lane >= m) x += y;
+    }
+    if (lane == 63) s_scan[w] = x;
+    __syncthreads();
+    int before = sum;
+    for (int i = 0; i < 16; ++i) {
+      if (i < w) before += s_scan[i];
+      sum += s_scan[i];
+    }
+    if (b < B) a.seq_tiles[b] = before + x - mine;
+    __syncthreads();
+  }
+  if (tid == 0) a.seq_tiles[B] = sum;
+  __syncthreads();
+  const int T = min(sum, a.max_tiles);
+  // a tile's sequence and key tiles; a bad sequence's tile has one
+  auto look = [&](int t, int& b, bool& wrong) -> int {
+    int lo = 0, hi = B;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      (a.seq_tiles[mid] <= t ? lo : hi) = mid;
+    }
+    b = lo;
+    wrong = a.seq_info[4 * b + 2] != 0;
+    if (wrong) return 1;
+    const int k = key_tiles<TREE>(a, b, t - a.seq_tiles[b],
+                                  a.seq_row_begin[b + 1] - a.seq_row_begin[b], a.seq_info[4 * b],
+                                  a.seq_info[4 * b + 1]);
+    return k > 0 ? k : 1;
+  };
+  unsigned long long work = 0;
+  int most = 0;
+  for (int t = tid; t < T; t += 1024) {
+    int b;
+    bool wrong;
+    const int k = look(t, b, wrong);
+    work += k;
+    most = max(most, k);
+  }
+  work = (unsigned long long)wave_sum((int64_t)work);
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) most = max(most, __shfl_xor(most, m));
+  if (lane == 0) {
+    atomicAdd(&s_work, work);
+    atomicMax(&s_most, most);
+  }
+  __syncthreads();
+  most = s_most;
+  int cap = most;
+  if (a.max_recs > 1 && (int64_t)T * a.num_kv_heads < 4 * (int64_t)a.slots) {
+    const unsigned long long share = (s_work * a.num_kv_heads + a.slots - 1) / a.slots;
+    cap = (int)min((unsigned long long)most, max(share, 8ull));
+    for (;;) {  // parts of split tiles, until their records fit
+      __syncthreads();
+      if (tid == 0) s_recs = 0;
+      __syncthreads();
+      int64_t recs = 0;
+      for (int t = tid; t < T; t += 1024) {
+        int b;
+        bool wrong;
+        const int k = look(t, b, wrong);
+        if (k > cap) recs += (k + cap - 1) / cap;
+      }
+      recs = min(wave_sum(recs), (int64_t)1 << 24);
+      if (lane == 0) atomicAdd(&s_recs, (int)recs);
+      __syncthreads();
+      if (s_recs <= a.max_recs) break;
+      cap += cap / 4 + 1;
+    }
+  }
+  __syncthreads();
+  if (tid == 0) s_recs = 0, s_splits = 0;
+  const int per = max(1, min(cap, most));
+  // by size of their parts, largest first
+  auto place = [&](int part) { return 63 - (int)((int64_t)part * 63 / per); };
+  for (int t = tid; t < T; t += 1024) {
+    int b;
+    bool wrong;
+    const int k = look(t, b, wrong), parts = (k + per - 1) / per;
+    atomicAdd(&s_count[place((k + parts - 1) / parts)], parts);
+  }
+  __syncthreads();
+  if (w == 0) {
+    const int mine = s_count[lane];
+    int x = mine;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const int y = __shfl_up(x, m);
+      if (lane >= m) x += y;
+    }
+    s_count[lane] = x - mine;
+    if (lane == 63) a.head[0] = x;
+  }
+  __syncthreads();
+  for (int t = tid; t < T; t += 1024) {
+    int b;
+    bool wrong;
+    const int k = look(t, b, wrong), parts = (k + per - 1) / per;
+    const int at = atomicAdd(&s_count[place((k + parts - 1) / parts)], parts);
+    RowsItem it;
+    it.seq = wrong ? -1 - b : b;
+    it.tile = t - a.seq_tiles[b];
+    it.rec = -1;
+    if (parts > 1) {
+      it.rec = atomicAdd(&s_recs, parts);
+      a.splits[atomicAdd(&s_splits, 1)] = RowsSplit{b, it.tile, it.rec, parts};
+    }
+    for (int p = 0; p < parts; ++p) {
+      it.key0 = (int)((int64_t)k * p / parts);
+      it.key1 = p + 1 < parts ? (int)((int64_t)k * (p + 1) / parts) : INT32_MAX;
+      a.items[at + p] = it;
+      if (parts > 1) it.rec += 1;
+    }
+  }
+  __syncthreads();
+  if (tid == 0) a.head[1] = s_splits;
+}
+
+// ---------------------------------------------------------------- attention
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// x of the lane 32 away.
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// The visible tokens of a sequence as tiles of 64, route after route.
+struct Walk {
+  int r, r_end;   // current route, the sequence's last + 1
+  int base, n;    // its first page id's index, its tokens that the row tile sees
+  int tb;         // its first token
+  int j, tiles;   // next tile of the route, its tiles
+};
+
+// One tile: tokens tok0 .. of a route of which the row tile sees n, and its pages.
+struct Tile {
+  int tok0, n, tb;
+  int pid[4];
+  bool draft;
+};
+
+__device__ __forceinline__ int visible(const int32_t* rp, int64_t last_pos) {
+  const int64_t n = (int64_t)rp[3] - rp[2], see = last_pos + 1 - rp[2];
+  return (int)(see < 0 ? 0 : see < n ? see : n);
+}
+
+// Positions the walk at key tile k of the sequence; tiles of a route: its
+// visible tokens / 64, rounded up.  Sixty-four routes at a time.
+__device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int r1, int64_t last_pos,
+                                        int64_t k, int lane) {
+  w.r = w.r_end = r1;
+  w.j = w.tiles = 0;
+  w.base = w.n = w.tb = 0;
+  for (int r = r0; r < r1; r += 64) {
+    int tiles = 0;
+    if (r + lane < r1)
+      tiles = (visible(reinterpret_cast<const int32_t*>(a.routes + r + lane), last_pos) +
+               kKeyTile - 1) / kKeyTile;
+    int64_t x = tiles;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const int64_t y = __shfl_up((long long)x, m);
+      if (lane >= m) x += y;
+    }
+    const uint64_t found = __ballot(x > k);
+    if (found) {
+      const int at = __builtin_ctzll(found);
+      const int64_t before = __shfl((long long)(x - tiles), at);
+      w.r = uniform(r + at);
+      const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + w.r);
+      w.n = uniform(visible(rp, last_pos));
+      w.tb = uniform(rp[2]);
+      w.base = uniform(rp[4]);
+      w.tiles = (w.n + kKeyTile - 1) / kKeyTile;
+      w.j = uniform((int)(k - before));
+      return;
+    }
+    k -= __shfl((long long)x, 63);
+  }
+}
+
+// The next tile; false at the end of the routes.
+__device__ __forceinline__ bool walk_next(const RowsArgs& a, Walk& w, int64_t last_pos, Tile& t) {
+  while (w.j >= w.tiles) {
+    if (w.r >= w.r_end || ++w.r >= w.r_end) return false;
+    const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + w.r);
+    w.n = uniform(visible(rp, last_pos));
+    w.tb = uniform(rp[2]);
+    w.base = uniform(rp[4]);
+    w.tiles = (w.n + kKeyTile - 1) / kKeyTile;
+    w.j = 0;
+  }
+  t.tok0 = w.j * kKeyTile;
+  t.n = w.n;
+  t.tb = w.tb;
+  t.draft = false;
+  const int last = (w.n - 1) / kPage;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t.pid[i] = uniform(a.page_ids[w.base + min(4 * w.j + i, last)]);
+  w.j += 1;
+  return true;
+}
+
+// Byte offset of 16-byte chunk c of token row `row` in a K tile in LDS, and of
+// half hh (slots 8 hh ..) of row d of page `page` in a V tile.  The exclusive
+// ors spread the rows that a matrix operand reads at once over all banks.
+__device__ __forceinline__ int k_at(int row, int c) { return row * 256 + ((c ^ (row & 15)) << 4); }
+__device__ __forceinline__ int v_at(int page, int d, int hh) {
+  return page * 4096 + d * 32 + ((hh ^ ((d >> 3) & 1)) << 4);
+}
+
+// A tile's K and V as a thread loads them.
+template <bool FP8>
+struct Staged {
+  u32x4 k[FP8 ? 2 : 4], v[FP8 ? 2 : 4];
+  float scale;  // fp8: thread i < 8 the K (i < 4) or V scale of page i % 4
+};
+
+template <bool FP8>
+__device__ __forceinline__ int page_or_0(const RowsArgs& a, int pid) {
+  return pid >= 0 && pid < a.num_pages ? pid : 0;
+}
+
+template <bool FP8>
+__device__ __forceinline__ void load_tile(const RowsArgs& a, const Tile& t, int g, int tid,
+                                          Staged<FP8>& s) {
+  const int H = a.num_kv_heads, wave = tid >> 6;
+  if constexpr (!FP8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const size_t at =
+          slice_of(page_or_0<FP8>(a, t.pid[i]), g, H, a.num_pages, a.head_major) * (kPage * kDim);
+      s.k[i] = ld16(static_cast<const uint16_t*>(a.k_pool) + at + tid * 8);
+      s.v[i] = ld16(static_cast<const uint16_t*>(a.v_pool) + at + tid * 8);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int pid = uniform(wave >> 1 ? t.pid[2 * i + 1] : t.pid[2 * i]);
+      const size_t at =
+          slice_of(page_or_0<FP8>(a, pid), g, H, a.num_pages, a.head_major) * (kPage * kDim);
+      s.k[i] = ld16(static_cast<const uint8_t*>(a.k_pool) + at + (tid & 127) * 16);
+      s.v[i] = ld16(static_cast<const uint8_t*>(a.v_pool) + at + (tid & 127) * 16);
+    }
+    if (tid < 8) {
+      const int i = tid & 3;
+      const int pid = i & 2 ? (i & 1 ? t.pid[3] : t.pid[2]) : (i & 1 ? t.pid[1] : t.pid[0]);
+      s.scale = (tid < 4 ? a.k_scale : a.v_scale)[(size_t)page_or_0<FP8>(a, pid) * H + g];
+    }
+  }
+}
+
+// 16 E4M3 codes -> two times 8 bf16, exactly.
+__device__ __forceinline__ void widen(u32x4 codes, u32x4& lo, u32x4& hi) {
+  uint32_t o[8];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    o[2 * w] = __builtin_bit_cast(
+        uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[w], 1.0f, false));
+    o[2 * w + 1] = __builtin_bit_cast(
+        uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[w], 1.0f, true));
+  }
+  lo = u32x4{o[0], o[1], o[2], o[3]};
+  hi = u32x4{o[4], o[5], o[6], o[7]};
+}
+
+// Zeroes the bf16 slots first, first + 1 .. of a chunk at and past token `lim`.
+__device__ __forceinline__ u32x4 cut(u32x4 x, int first, int lim) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    x[i] &= (first + 2 * i < lim ? 0x0000FFFFu : 0u) | (first + 2 * i + 1 < lim ? 0xFFFF0000u : 0u);
+  return x;
+}
+
+// Into LDS as bf16; V of slots past the visible tokens is zeroed (they may hold
+// anything, and a weight of 0 does not undo an infinity).
+template <bool FP8>
+__device__ __forceinline__ void store_tile(const Staged<FP8>& s, const Tile& t, int tid, char* lk,
+                                           char* lv, float* scales) {
+  const bool ends = t.tok0 + kKeyTile > t.n;
+  if constexpr (!FP8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      *reinterpret_cast<u32x4*>(lk + k_at(16 * i + (tid >> 4), tid & 15)) = s.k[i];
+      u32x4 v = s.v[i];
+      if (ends) v = cut(v, t.tok0 + 16 * i + 8 * (tid & 1), t.n);
+      *reinterpret_cast<u32x4*>(lv + v_at(i, tid >> 1, tid & 1)) = v;
+    }
+  } else {
+    const int t7 = tid & 127;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int page = 2 * i + (tid >> 7);
+      u32x4 lo, hi;
+      widen(s.k[i], lo, hi);
+      const int row = 16 * page + (t7 >> 3);
+      *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7))) = lo;
+      *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7) + 1)) = hi;
+      widen(s.v[i], lo, hi);
+      if (ends) {
+        lo = cut(lo, t.tok0 + 16 * page, t.n);
+        hi = cut(hi, t.tok0 + 16 * page + 8, t.n);
+      }
+      *reinterpret_cast<u32x4*>(lv + v_at(page, t7, 0)) = lo;
+      *reinterpret_cast<u32x4*>(lv + v_at(page, t7, 1)) = hi;
+    }
+    if (tid < 8) scales[tid] = s.scale;
+  }
+}
+
+// The drafted tokens of a sequence as a tile: V is turned around on its way.
+__device__ __forceinline__ void stage_draft(const RowsArgs& a, int row0, int n, int g, int tid,
+                                            char* lk, char* lv, float* scales) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = 16 * i + (tid >> 4), c = tid & 15;
+    u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
+    if (row < n) {
+      const size_t at = (size_t)(row0 + row) * a.kv_stride + (size_t)g * kDim + 8 * c;
+      k = ld16(a.k_draft + at);
+      v = ld16(a.v_draft + at);
+    }
+    *reinterpret_cast<u32x4*>(lk + k_at(row, c)) = k;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      *reinterpret_cast<uint16_t*>(lv + v_at(i, 8 * c + e, (row & 15) >> 3) + 2 * (row & 7)) =
+          (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+  }
+  if (tid < 8) scales[tid] = 1.0f;
+}
+
+// Whether any of 8 bf16 is infinite or NaN.
+__device__ __forceinline__ bool not_finite(u32x4 x) {
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    any |= (x[i] & 0x7F80u) == 0x7F80u || (x[i] & 0x7F800000u) == 0x7F800000u;
+  return any;
+}
+
+// Softmax state of one (row, head) per lane column q = lane % 32, shared by the
+// two half waves: lane (half, q) holds dims 32 dt + 8 i + 4 half + j at
+// o[dt][4 i + j], m is the running reference (base 2), l the lane's own sum.
+struct State {
+  f32x16 o[4];
+  float m, l;
+};
+
+// One tile.  S^T = K Q^T: matrix row 8 i + 4 half + j of 32 is token
+// 16 (i / 2) + 8 half + 4 (i % 2) + j, so that a lane's 16 results are the 8
+// slots 8 half .. of two pages: just the p that the lane feeds to O^T += V^T P^T,
+// whose depth of 16 is one page.  No value crosses lanes between the products.
+// sees: the tokens of this lane's row (MASK); bad: pages outside the pool.
+template <bool FP8, bool MASK>
+__device__ __forceinline__ void attend(const char* lk, const char* lv, const float* scales,
+                                       const u32x4 (&q)[8], float c, uint64_t sees, int bad,
+                                       int lane, State& st) {
+  const int half = lane >> 5, l32 = lane & 31;
+  const int krow = 16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
+  f32x16 s[2];
+#pragma unroll
+  for (int tg = 0; tg < 2; ++tg) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[tg][i] = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks)
+      s[tg] = mfma32(*reinterpret_cast<const u32x4*>(lk + k_at(32 * tg + krow, 2 * ks + half)),
+                     q[ks], s[tg]);
+  }
+  // scores in base 2: s c (fp8: the page's scale in it)
+  float cs[4];
+#pragma unroll
+  for (int p = 0; p < 4; ++p) cs[p] = FP8 ? c * scales[p] : c;
+  if constexpr (FP8 || MASK) {
+    const uint64_t mine = sees >> (8 * half);
+#pragma unroll
+    for (int tg = 0; tg < 2; ++tg)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int page = 2 * tg + (i >> 3);
+        if constexpr (FP8) s[tg][i] *= cs[page];
+        if constexpr (MASK) {
+          if (bad >> page & 1) s[tg][i] = qnan();
+          if (!(mine >> (32 * tg + 16 * (i >> 3) + (i & 7)) & 1)) s[tg][i] = neg_inf();
+        }
+      }
+  }
+  float top = neg_inf();
+#pragma unroll
+  for (int tg = 0; tg < 2; ++tg)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[tg][i]);
+  top = fmaxf(top, other_half(top));
+  if constexpr (!FP8) top *= c;
+  // The reference moves only when a score exceeds it by 2^8: exp2 and the sums
+  // stay in range, and most tiles leave the outputs unscaled.
+  if (__ballot(top > st.m + 8.0f)) {
+    const float m = fmaxf(st.m, top);
+    const float f = m == neg_inf() ? 1.0f : exp2_fast(st.m - m);
+    st.m = m;
+    st.l *= f;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) st.o[dt][i] *= f;
+  }
+  const float m = st.m == neg_inf() ? 0.0f : st.m;
+  u32x4 p[4];
+#pragma unroll
+  for (int page = 0; page < 4; ++page)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = 8 * (page & 1) + 2 * i;
+      const float x0 = s[page >> 1][at], x1 = s[page >> 1][at + 1];
+      const float e0 = FP8 ? exp2_fast(x0 - m) : exp2_fast(__builtin_fmaf(x0, c, -m));
+      const float e1 = FP8 ? exp2_fast(x1 - m) : exp2_fast(__builtin_fmaf(x1, c, -m));
+      st.l += e0 + e1;
+      if constexpr (FP8) {
+        float y0 = e0 * scales[4 + page], y1 = e1 * scales[4 + page];
+        if constexpr (MASK) {  // nothing, whatever the page's scale
+          const uint64_t mine = sees >> (8 * half + 16 * page + 2 * i);
+          if (!(mine & 1)) y0 = 0.0f;
+          if (!(mine & 2)) y1 = 0.0f;
+        }
+        p[page][i] = pack_bf16(y0, y1);
+      } else {
+        p[page][i] = pack_bf16(e0, e1);
+      }
+    }
+  if constexpr (MASK) {
+    // A row that does not see a token must not meet its infinities: where the
+    // tile holds any, its tokens enter one by one, by a select.
+    bool any = false;
+#pragma unroll
+    for (int page = 0; page < 4; ++page)
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+        any |= not_finite(*reinterpret_cast<const u32x4*>(lv + v_at(page, 32 * dt + l32, half)));
+    if (__ballot(any)) {
+#pragma unroll 1
+      for (int t = 0; t < kKeyTile; ++t) {
+        const int page = t >> 4, k = t & 15;
+        const u32x4 pp = page & 2 ? (page & 1 ? p[3] : p[2]) : (page & 1 ? p[1] : p[0]);
+        u32x4 keep = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (half == k >> 3 && i == (k & 7) >> 1) keep[i] = k & 1 ? 0xFFFF0000u : 0x0000FFFFu;
+        const bool see = sees >> t & 1;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) {
+          f32x16 x;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+          x = mfma32(*reinterpret_cast<const u32x4*>(lv + v_at(page, 32 * dt + l32, half)) & keep,
+                     pp & keep, x);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) st.o[dt][i] += see ? x[i] : 0.0f;
+        }
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int page = 0; page < 4; ++page)
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+      st.o[dt] = mfma32(*reinterpret_cast<const u32x4*>(lv + v_at(page, 32 * dt + l32, half)),
+                        p[page], st.o[dt]);
+}
+
+// NaN into the outputs of the (row, head) pairs [m0, m1) of KV head g of rows
+// row0 ...
+__device__ void fill_nan(const RowsArgs& a, int row0, int64_t m0, int64_t m1, int g, int tid,
+                         int nt) {
+  const int G = a.group;
+  for (int64_t x = m0 * 16 + tid; x < m1 * 16; x += nt) {
+    const int64_t m = x >> 4, at = (row0 + m / G) * a.num_q_heads + g * G + m % G;
+    *reinterpret_cast<u32x4*>(a.out + at * kDim + 8 * (x & 15)) =
+        u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
+    if ((x & 15) == 0) a.lse[at] = qnan();
+  }
+}
+
+// One work item of one KV head: four waves of 32 (row, head) pairs each, over
+// K/V tiles of 64 tokens that they share through LDS.
+template <bool FP8, bool TREE>
+__global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
+  __shared__ __align__(16) char lk[2][kKeyTile * 256];
+  __shared__ __align__(16) char lv[2][kKeyTile * 256];
+  __shared__ __align__(16) float scales[2][8];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int half = lane >> 5, l32 = lane & 31;
+  const int H = a.num_kv_heads, G = a.group;
+  const int g = blockIdx.x % H, item = blockIdx.x / H;
+  const int items = a.head[0];
+  if (items < 0) {  // no row's sequence is known
+    for (int r = item; r < a.num_rows; r += gridDim.x / H) fill_nan(a, r, 0, G, g, tid, 256);
+    return;
+  }
+  if (item >= items) return;
+  const RowsItem it = a.items[item];
+  const int b = uniform(it.seq < 0 ? -1 - it.seq : it.seq);
+  const int row0 = a.seq_row_begin[b], n_rows = a.seq_row_begin[b + 1] - row0;
+  const int64_t m_all = (int64_t)n_rows * G, m0 = (int64_t)it.tile * kRowTile;
+  const int64_t m1 = min(m_all, m0 + kRowTile);
+  if (it.seq < 0) {
+    fill_nan(a, row0, m0, m1, g, tid, 256);
+    return;
+  }
+  // this lane's row and head
+  const int64_t m = m0 + 32 * wave + l32;
+  const bool mine = m < m1, any = m0 + 32 * wave < m1;
+  const int64_t mc = mine ? m : m1 - 1;
+  const int row = (int)(mc / G), h = g * G + (int)(mc % G);
+  const float c0 = a.scale_log2;
+  const float c = c0 == 0.0f ? 1.0f : fabsf(c0);
+  u32x4 q[8];
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks) {
+    q[ks] = ld16(a.q + (row0 + row) * a.q_stride + (size_t)h * kDim + 16 * ks + 8 * half);
+    if (c0 < 0.0f) q[ks] ^= 0x80008000u;                 // a negative scale turns the row around
+    if (c0 == 0.0f || !mine) q[ks] = u32x4{0, 0, 0, 0};  // a zero one makes all scores equal
+  }
+  int64_t pos = INT32_MAX, pos_min = INT32_MAX, last_pos = INT32_MAX;
+  uint64_t draft = 0;
+  if constexpr (TREE) {
+    draft = mine ? a.tree_mask[row0 + row] : 0;
+    if (n_rows < 64) draft &= ((uint64_t)1 << n_rows) - 1;
+  } else {
+    const int64_t p0 = a.first_pos[b];
+    pos = p0 + row;
+    pos_min = p0 + (m0 + 32 * wave < m1 ? m0 + 32 * wave : m1 - 1) / G;
+    last_pos = p0 + (m1 - 1) / G;
+  }
+  const int64_t pos_max = TREE ? INT32_MAX : a.first_pos[b] + (min(m1, m0 + 32 * wave + 32) - 1) / G;
+
+  State st;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) st.o[dt][i] = 0.0f;
+  st.m = neg_inf();
+  st.l = 0.0f;
+
+  Walk walk;
+  walk_to(a, walk, a.seq_route_begin[b], a.seq_route_begin[b + 1], last_pos, it.key0, lane);
+  // the tiles of this part, the drafted tokens behind the last one
+  int left = it.key1 == INT32_MAX ? INT32_MAX : it.key1 - it.key0;
+  bool drafted = !TREE || it.key1 != INT32_MAX;
+  auto next = [&](Tile& t) -> bool {
+    if (left > 0 && walk_next(a, walk, last_pos, t)) {
+      if (left != INT32_MAX) --left;
+      return true;
+    }
+    left = 0;
+    if (drafted) return false;
+    drafted = true;
+    t.draft = true;
+    t.tok0 = 0;
+    t.n = n_rows;
+    t.tb = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t.pid[i] = 0;
+    return true;
+  };
+  Tile cur{}, nxt{};
+  Staged<FP8> sg;
+  bool has = next(cur);
+  if (has) {
+    if (cur.draft) {
+      stage_draft(a, row0, n_rows, g, tid, lk[0], lv[0], scales[0]);
+    } else {
+      load_tile<FP8>(a, cur, g, tid, sg);
+      store_tile<FP8>(sg, cur, tid, lk[0], lv[0], scales[0]);
+    }
+  }
+  int buf = 0, flag = 0;
+  while (has) {
+    __syncthreads();
+    const bool more = next(nxt);
+    if (more && !nxt.draft) load_tile<FP8>(a, nxt, g, tid, sg);
+    // which of the tile's tokens this lane's row sees
+    const int64_t n_see = min(pos - cur.tb + 1, (int64_t)cur.n) - cur.tok0;
+    int bad = 0;
+    if (!cur.draft) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (cur.tok0 + 16 * i < cur.n && (cur.pid[i] < 0 || cur.pid[i] >= a.num_pages))
+          bad |= 1 << i;
+      if (bad) flag = KF_EFLAG_BAD_PAGE;
+    }
+    if (any && pos_max - cur.tb >= cur.tok0) {
+      const bool mask = bad || cur.draft || cur.tok0 + kKeyTile > cur.n ||
+                        pos_min - cur.tb < cur.tok0 + kKeyTile - 1;
+      if (mask) {
+        const uint64_t sees = cur.draft ? draft
+                              : n_see <= 0 ? 0
+                              : n_see >= 64 ? ~(uint64_t)0
+                                            : ((uint64_t)1 << n_see) - 1;
+        attend<FP8, true>(lk[buf], lv[buf], scales[buf], q, c, sees, bad, lane, st);
+      } else {
+        attend<FP8, false>(lk[buf], lv[buf], scales[buf], q, c, 0, 0, lane, st);
+      }
+    }
+    buf ^= 1;
+    if (more) {
+      if (nxt.draft)
+        stage_draft(a, row0, n_rows, g, tid, lk[buf], lv[buf], scales[buf]);
+      else
+        store_tile<FP8>(sg, nxt, tid, lk[buf], lv[buf], scales[buf]);
+    }
+    cur = nxt;
+    has = more;
+  }
+  if (flag && tid == 0) atomicOr(a.err_flags, flag);
+  if (!any) return;
+  const float l = st.l + other_half(st.l);
+  if (it.rec >= 0) {
+    const int rm = (int)(m - m0);
+    if (!mine) return;
+    const size_t rec = ((size_t)it.rec * H + g) * a.rec_rows + rm;
+    if (half == 0) *reinterpret_cast<f32x2*>(a.rec_ml + 2 * rec) = f32x2{st.m, l};
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(a.rec_o + rec * kDim + 32 * dt + 8 * i + 4 * half) =
+            f32x4{st.o[dt][4 * i], st.o[dt][4 * i + 1], st.o[dt][4 * i + 2], st.o[dt][4 * i + 3]};
+    return;
+  }
+  if (!mine) return;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const size_t at = (size_t)(row0 + row) * a.num_q_heads + h;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<u32x2*>(a.out + at * kDim + 32 * dt + 8 * i + 4 * half) =
+          u32x2{pack_bf16(st.o[dt][4 * i] * inv, st.o[dt][4 * i + 1] * inv),
+                pack_bf16(st.o[dt][4 * i + 2] * inv, st.o[dt][4 * i + 3] * inv)};
+  if (half == 0) a.lse[at] = l == 0.0f ? neg_inf() : (st.m + __log2f(l)) * kLn2;
+}
+
+// The parts of a split row tile into its outputs: a wave per (row, head).
+__global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
+  const int H = a.num_kv_heads, G = a.group, g = blockIdx.y;
+  const int split = blockIdx.x / 8;
+  if (split >= a.head[1]) return;
+  const RowsSplit sp = a.splits[split];
+  const int row0 = a.seq_row_begin[sp.seq];
+  const int64_t m_all = (int64_t)(a.seq_row_begin[sp.seq + 1] - row0) * G;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int k = wave; k < kRowTile / 8; k += 4) {
+    const int rm = (blockIdx.x & 7) * (kRowTile / 8) + k;
+    const int64_t m = (int64_t)sp.tile * kRowTile + rm;
+    if (m >= m_all) return;
+    const size_t stride = (size_t)H * a.rec_rows;
+    const size_t rec = ((size_t)sp.rec * H + g) * a.rec_rows + rm;
+    float top = neg_inf();
+    for (int p = lane; p < sp.parts; p += 64) top = fmaxf(top, a.rec_ml[2 * (rec + p * stride)]);
+    top = wave_max(top);
+    const float ref = top == neg_inf() ? 0.0f : top;
+    float l = 0.0f;
+    f32x2 o = {0.0f, 0.0f};
+    for (int p = 0; p < sp.parts; ++p) {
+      const f32x2 ml = *reinterpret_cast<const f32x2*>(a.rec_ml + 2 * (rec + p * stride));
+      const f32x2 x =
+          reinterpret_cast<const f32x2*>(a.rec_o + (rec + p * stride) * kDim)[lane];
+      const float f = exp2_fast(ml.x - ref);
+      l = __builtin_fmaf(f, ml.y, l);
+      o.x = __builtin_fmaf(f, x.x, o.x);
+      o.y = __builtin_fmaf(f, x.y, o.y);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const size_t at = (row0 + m / G) * a.num_q_heads + g * G + m % G;
+    reinterpret_cast<uint32_t*>(a.out + at * kDim)[lane] = pack_bf16(o.x * inv, o.y * inv);
+    if (lane == 0) a.lse[at] = l == 0.0f ? neg_inf() : (top + __log2f(l)) * kLn2;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_append_rows(const AppendRowsArgs& a, bool fp8, hipStream_t stream) {
+  if (a.num_entries <= 256) {
+    if (fp8)
+      append_plan_kernel<true, true><<<a.num_routes, 512, 0, stream>>>(a);
+    else
+      append_plan_kernel<false, true><<<a.num_routes, 512, 0, stream>>>(a);
+    return hipGetLastError();
+  }
+  append_plan_kernel<false, false><<<a.num_routes, 512, 0, stream>>>(a);
+  const hipError_t st = hipGetLastError();
+  if (st != hipSuccess) return st;
+  const int64_t tiles = (int64_t)a.num_entries / kPage + 2 * (int64_t)a.num_routes;
+  const int64_t grid = (tiles * 2 * a.num_kv_heads + 3) / 4;
+  if (fp8)
+    append_tile_kernel<true><<<(uint32_t)grid, 256, 0, stream>>>(a);
+  else
+    append_tile_kernel<false><<<(uint32_t)grid, 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_rows_attn(const RowsArgs& a, bool fp8, bool tree, hipStream_t stream) {
+  if (tree)
+    rows_plan_kernel<true><<<1, 1024, 0, stream>>>(a);
+  else
+    rows_plan_kernel<false><<<1, 1024, 0, stream>>>(a);
+  hipError_t st = hipGetLastError();
+  if (st != hipSuccess) return st;
+  const uint32_t grid = (uint32_t)(a.max_tiles + a.max_recs) * a.num_kv_heads;
+  if (fp8 && tree)
+    rows_kernel<true, true><<<grid, 256, 0, stream>>>(a);
+  else if (fp8)
+    rows_kernel<true, false><<<grid, 256, 0, stream>>>(a);
+  else if (tree)
+    rows_kernel<false, true><<<grid, 256, 0, stream>>>(a);
+  else
+    rows_kernel<false, false><<<grid, 256, 0, stream>>>(a);
+  st = hipGetLastError();
+  if (st != hipSuccess || a.max_recs < 2) return st;
+  const uint32_t splits = (uint32_t)min(a.max_tiles, a.max_recs / 2);
+  rows_combine_kernel<<<dim3(splits * 8, a.num_kv_heads), 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace kf

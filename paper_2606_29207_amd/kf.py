@@ -16,6 +16,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libkf.so")
 PAGE_SIZE = 16
 HEAD_DIM = 128
 MAX_GROUP = 16
+MAX_DRAFT = 64   # drafted tokens per sequence of tree_attn
 
 KV_BF16 = 0
 KV_FP8_E4M3 = 1
@@ -39,7 +40,9 @@ KV_HEAD_MAJOR = 1
 # every symbol include/kf.h declares
 EXPORTS = ("kf_kv_append", "kf_partial_attn_workspace_bytes", "kf_partial_attn_plan",
            "kf_partial_attn_spans", "kf_partial_attn", "kf_partial_attn_subset",
-           "kf_merge_partials", "kf_decode_step", "kf_decode_step_no_alloc", "kf_debug_gather",
+           "kf_merge_partials", "kf_decode_step", "kf_decode_step_no_alloc",
+           "kf_kv_append_rows_workspace_bytes", "kf_kv_append_rows",
+           "kf_rows_attn_workspace_bytes", "kf_prompt_attn", "kf_tree_attn", "kf_debug_gather",
            "kf_status_str", "kf_version")
 
 
@@ -95,6 +98,20 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.kf_decode_step_no_alloc.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp,
                                             vp, vp, vp, vp, vp, vp, vp]
     lib.kf_decode_step_no_alloc.restype = ctypes.c_int
+    i64 = ctypes.c_int64
+    lib.kf_kv_append_rows_workspace_bytes.argtypes = [i32]
+    lib.kf_kv_append_rows_workspace_bytes.restype = sz
+    lib.kf_kv_append_rows.argtypes = [sp, vp, vp, vp, vp, vp, vp, i32, i64, vp, i32, vp, vp, i32, vp,
+                                      vp, sz, vp, vp]
+    lib.kf_kv_append_rows.restype = ctypes.c_int
+    lib.kf_rows_attn_workspace_bytes.argtypes = [sp, i32]
+    lib.kf_rows_attn_workspace_bytes.restype = sz
+    lib.kf_prompt_attn.argtypes = [sp, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp,
+                                   vp, vp, sz, vp, vp]
+    lib.kf_prompt_attn.restype = ctypes.c_int
+    lib.kf_tree_attn.argtypes = [sp, vp, i32, i64, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, i32, i32,
+                                 vp, vp, vp, vp, vp, sz, vp, vp]
+    lib.kf_tree_attn.restype = ctypes.c_int
     lib.kf_debug_gather.argtypes = [sp, vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, vp, vp]
     lib.kf_debug_gather.restype = ctypes.c_int
     lib.kf_status_str.argtypes = [ctypes.c_int]
@@ -457,6 +474,192 @@ def decode_step(shape: Shape, q, k_pool, v_pool, k_new, v_new, routes, tail_rout
     bind_decode_step(shape, q, k_pool, v_pool, routes, tail_route, max_pages_per_route, page_ids,
                      seq_route_begin, o_part, lse_part, out, lse_out, workspace, err_flags,
                      k_scale, v_scale)(k_new, v_new, stream)
+
+
+# ------------------------------------------------------- operators on rows
+def _rows(t: torch.Tensor, name: str, heads: int) -> int:
+    """Checks packed rows bf16 [N, heads, 128], contiguous within a row (parts of
+    a wider projection's output included); returns the elements between rows."""
+    _need(isinstance(t, torch.Tensor) and t.is_cuda, f"{name} must be a device tensor")
+    _need(t.dtype == torch.bfloat16 and t.dim() == 3 and tuple(t.shape[1:]) == (heads, HEAD_DIM),
+          f"{name} must be bf16 [num_rows, {heads}, 128]")
+    _need(t.stride(2) == 1 and (heads == 1 or t.stride(1) == HEAD_DIM),
+          f"{name}: the {heads} x 128 elements of a row must be contiguous")
+    if t.shape[0] <= 1:
+        return heads * HEAD_DIM
+    _need(t.stride(0) >= heads * HEAD_DIM and t.stride(0) % 8 == 0,
+          f"{name}: rows must be a multiple of 8 elements apart and not overlap")
+    return t.stride(0)
+
+
+def _same_device(first: torch.Tensor, tensors):
+    for t, n in tensors:
+        _need(t is None or t.device == first.device, f"{n} must be on {first.device}")
+
+
+def _csr(t, name: str, n: int):
+    _dev(t, name, torch.int32)
+    _need(t.dim() == 1 and t.numel() >= n + 1, f"{name} must be int32 [{n} + 1]")
+
+
+def kv_append_rows_workspace_bytes(num_routes: int) -> int:
+    return int(load().kf_kv_append_rows_workspace_bytes(int(num_routes)))
+
+
+def bind_kv_append_rows(shape: Shape, k_pool, v_pool, k_rows, v_rows, routes, route_entry_begin,
+                        page_ids, err_flags, row_list=None, k_scale=None, v_scale=None,
+                        workspace=None) -> BoundCall:
+    """kf_kv_append_rows bound to its buffers; call it as (stream).  k_rows and
+    v_rows bf16 [N, Hkv, 128], rows of one stride; route_entry_begin int32
+    [R + 1]: route r takes its entries in order, entry e being row row_list[e]
+    (int32) or, without a list, row e.  workspace=None allocates the few bytes
+    per route that the call needs."""
+    lib = load()
+    H, R = shape.num_kv_heads, routes.shape[0]
+    for t, n in ((k_pool, "k_pool"), (v_pool, "v_pool"), (routes, "routes"),
+                 (page_ids, "page_ids"), (err_flags, "err_flags")):
+        _dev(t, n)
+    stride = _rows(k_rows, "k_rows", H)
+    _need(_rows(v_rows, "v_rows", H) == stride and v_rows.shape == k_rows.shape,
+          "k_rows and v_rows must have the same shape and stride")
+    _need(err_flags.dtype == torch.int32 and err_flags.numel() >= 1, "err_flags must be int32 [1]")
+    _csr(route_entry_begin, "route_entry_begin", R)
+    if row_list is not None:
+        _dev(row_list, "row_list", torch.int32)
+        _need(row_list.dim() == 1, "row_list must be int32 [n]")
+    _check_tables(shape, k_pool, v_pool, routes, page_ids)
+    _check_scales(shape, k_scale, v_scale)
+    if workspace is None:
+        workspace = torch.empty(kv_append_rows_workspace_bytes(R), dtype=torch.uint8,
+                                device=k_pool.device)
+    _dev(workspace, "workspace")
+    _same_device(k_pool, ((v_pool, "v_pool"), (k_rows, "k_rows"), (v_rows, "v_rows"),
+                          (routes, "routes"), (route_entry_begin, "route_entry_begin"),
+                          (page_ids, "page_ids"), (err_flags, "err_flags"),
+                          (row_list, "row_list"), (k_scale, "k_scale"), (v_scale, "v_scale"),
+                          (workspace, "workspace")))
+    sh = _copy_shape(shape)
+    N = k_rows.shape[0]
+    args = (ctypes.byref(sh), _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale),
+            _ptr(k_rows), _ptr(v_rows), N, stride, _ptr(row_list),
+            N if row_list is None else row_list.numel(), _ptr(route_entry_begin), _ptr(routes), R,
+            _ptr(page_ids), _ptr(workspace), workspace.numel() * workspace.element_size(),
+            _ptr(err_flags))
+    keep = (sh, k_pool, v_pool, k_scale, v_scale, k_rows, v_rows, row_list, route_entry_begin,
+            routes, page_ids, workspace, err_flags)
+    return BoundCall(lib.kf_kv_append_rows, "kf_kv_append_rows", args, keep, k_pool.device.index)
+
+
+def kv_append_rows(shape: Shape, k_pool, v_pool, k_rows, v_rows, routes, route_entry_begin,
+                   page_ids, err_flags, row_list=None, k_scale=None, v_scale=None, workspace=None,
+                   stream=None):
+    """kf_kv_append_rows.  routes: int32 [R, 6] (updated in place); fp8 pools also
+    take (and update) k_scale/v_scale float32 [P, Hkv].  On another stream than
+    the current one give a workspace of your own."""
+    _need(workspace is not None or stream is None, "a workspace is needed with a stream")
+    bind_kv_append_rows(shape, k_pool, v_pool, k_rows, v_rows, routes, route_entry_begin, page_ids,
+                        err_flags, row_list, k_scale, v_scale, workspace)(stream)
+
+
+def rows_attn_workspace_bytes(shape: Shape, num_rows: int) -> int:
+    return int(load().kf_rows_attn_workspace_bytes(ctypes.byref(shape), int(num_rows)))
+
+
+def alloc_rows_workspace(shape: Shape, num_rows: int, device="cuda"):
+    """Workspace of prompt_attn and tree_attn for num_rows rows."""
+    n = rows_attn_workspace_bytes(shape, num_rows)
+    if n == 0:
+        raise KFError("invalid workspace request")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _bind_rows(fn, what: str, shape: Shape, q, mid, mid_keep, k_pool, v_pool, routes,
+               max_pages_per_route, page_ids, seq_route_begin, seq_row_begin, out, lse, workspace,
+               err_flags, k_scale, v_scale) -> BoundCall:
+    """prompt_attn and tree_attn: the arguments that they share.  mid: the C
+    arguments around seq_row_begin, which is given as a marker."""
+    B, Hq = shape.num_seqs, shape.num_q_heads
+    stride = _rows(q, "q", Hq)
+    N = q.shape[0]
+    for t, n in ((k_pool, "k_pool"), (v_pool, "v_pool"), (routes, "routes"),
+                 (page_ids, "page_ids"), (out, "out"), (lse, "lse"), (workspace, "workspace"),
+                 (err_flags, "err_flags")):
+        _dev(t, n)
+    _csr(seq_route_begin, "seq_route_begin", B)
+    _csr(seq_row_begin, "seq_row_begin", B)
+    _need(tuple(out.shape) == (N, Hq, HEAD_DIM) and out.dtype == torch.bfloat16,
+          "out must be bf16 [num_rows, Hq, 128]")
+    _need(tuple(lse.shape) == (N, Hq) and lse.dtype == torch.float32,
+          "lse must be float32 [num_rows, Hq]")
+    _need(err_flags.dtype == torch.int32 and err_flags.numel() >= 1, "err_flags must be int32 [1]")
+    _check_tables(shape, k_pool, v_pool, routes, page_ids)
+    _check_scales(shape, k_scale, v_scale)
+    _same_device(k_pool, ((v_pool, "v_pool"), (q, "q"), (routes, "routes"),
+                          (page_ids, "page_ids"), (seq_route_begin, "seq_route_begin"),
+                          (seq_row_begin, "seq_row_begin"), (out, "out"), (lse, "lse"),
+                          (workspace, "workspace"), (err_flags, "err_flags"),
+                          (k_scale, "k_scale"), (v_scale, "v_scale")) + tuple(mid_keep))
+    sh = _copy_shape(shape)
+    args = (ctypes.byref(sh), _ptr(q), N, stride, *mid(_ptr(seq_row_begin)), _ptr(k_pool),
+            _ptr(v_pool), _ptr(k_scale), _ptr(v_scale), _ptr(routes), routes.shape[0],
+            int(max_pages_per_route), _ptr(page_ids), _ptr(seq_route_begin), _ptr(out), _ptr(lse),
+            _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(err_flags))
+    keep = (sh, q, k_pool, v_pool, k_scale, v_scale, routes, page_ids, seq_route_begin,
+            seq_row_begin, out, lse, workspace, err_flags) + tuple(t for t, _ in mid_keep)
+    return BoundCall(fn, what, args, keep, k_pool.device.index)
+
+
+def bind_prompt_attn(shape: Shape, q, first_pos, k_pool, v_pool, routes, max_pages_per_route,
+                     page_ids, seq_route_begin, seq_row_begin, out, lse, workspace, err_flags,
+                     k_scale=None, v_scale=None) -> BoundCall:
+    """kf_prompt_attn bound to its buffers; call it as (stream).  q bf16
+    [N, Hq, 128], the packed rows of all sequences; seq_row_begin int32 [B + 1];
+    first_pos int32 [B]: the position of each sequence's first row; out bf16
+    [N, Hq, 128], lse float32 [N, Hq]; workspace: alloc_rows_workspace(shape, N)."""
+    _dev(first_pos, "first_pos", torch.int32)
+    _need(first_pos.numel() >= shape.num_seqs, "first_pos must be int32 [num_seqs]")
+    return _bind_rows(load().kf_prompt_attn, "kf_prompt_attn", shape, q,
+                      lambda begin: (begin, _ptr(first_pos)), ((first_pos, "first_pos"),), k_pool,
+                      v_pool, routes, max_pages_per_route, page_ids, seq_route_begin,
+                      seq_row_begin, out, lse, workspace, err_flags, k_scale, v_scale)
+
+
+def prompt_attn(shape: Shape, q, first_pos, k_pool, v_pool, routes, max_pages_per_route, page_ids,
+                seq_route_begin, seq_row_begin, out, lse, workspace, err_flags, k_scale=None,
+                v_scale=None, stream=None):
+    """kf_prompt_attn: causal attention of packed prompt rows over their cache."""
+    bind_prompt_attn(shape, q, first_pos, k_pool, v_pool, routes, max_pages_per_route, page_ids,
+                     seq_route_begin, seq_row_begin, out, lse, workspace, err_flags, k_scale,
+                     v_scale)(stream)
+
+
+def bind_tree_attn(shape: Shape, q, k_draft, v_draft, tree_mask, k_pool, v_pool, routes,
+                   max_pages_per_route, page_ids, seq_route_begin, seq_row_begin, out, lse,
+                   workspace, err_flags, k_scale=None, v_scale=None) -> BoundCall:
+    """kf_tree_attn bound to its buffers; call it as (stream).  q bf16 [N, Hq, 128]
+    and k_draft, v_draft bf16 [N, Hkv, 128]: the drafted rows of all sequences,
+    at most 64 each; tree_mask int64 [N]: bit j set if the row sees its
+    sequence's drafted row j; the rest as for bind_prompt_attn."""
+    H, N = shape.num_kv_heads, q.shape[0]
+    stride = _rows(k_draft, "k_draft", H)
+    _need(_rows(v_draft, "v_draft", H) == stride and k_draft.shape[0] == v_draft.shape[0] == N,
+          "k_draft and v_draft must have q's rows and one stride")
+    _dev(tree_mask, "tree_mask", torch.int64)
+    _need(tree_mask.numel() == N, "tree_mask must be int64 [num_rows]")
+    return _bind_rows(load().kf_tree_attn, "kf_tree_attn", shape, q,
+                      lambda begin: (_ptr(k_draft), _ptr(v_draft), stride, _ptr(tree_mask), begin),
+                      ((k_draft, "k_draft"), (v_draft, "v_draft"), (tree_mask, "tree_mask")),
+                      k_pool, v_pool, routes, max_pages_per_route, page_ids, seq_route_begin,
+                      seq_row_begin, out, lse, workspace, err_flags, k_scale, v_scale)
+
+
+def tree_attn(shape: Shape, q, k_draft, v_draft, tree_mask, k_pool, v_pool, routes,
+              max_pages_per_route, page_ids, seq_route_begin, seq_row_begin, out, lse, workspace,
+              err_flags, k_scale=None, v_scale=None, stream=None):
+    """kf_tree_attn: attention of drafted trees over their cache."""
+    bind_tree_attn(shape, q, k_draft, v_draft, tree_mask, k_pool, v_pool, routes,
+                   max_pages_per_route, page_ids, seq_route_begin, seq_row_begin, out, lse,
+                   workspace, err_flags, k_scale, v_scale)(stream)
 
 
 def debug_gather(shape: Shape, k_pool, v_pool, routes, route, max_pages_per_route, page_ids,

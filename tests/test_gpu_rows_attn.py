@@ -1,0 +1,281 @@
+"""kf_prompt_attn and kf_tree_attn against the fp64 oracle, elementwise within
+bounds derived from their roundings (rows_testlib.assert_rows)."""
+import numpy as np
+import pytest
+
+from rows_testlib import DIM, Cache, Rows, assert_rows, bits
+
+pytestmark = pytest.mark.gpu
+
+
+# ----------------------------------------------------------------- prompts
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 8, 16])
+def test_prompts_of_every_group_size(gpu, G, fp8):
+    lens = [70, 1, 33, 200]
+    c = Cache(lens, H=2, fp8=fp8, part=64, seed=G)
+    r = Rows(c, lens, G, seed=G)
+    assert_rows(r.gpu(), r.oracle(), f"G {G}")
+
+
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 300])
+def test_whole_prompts_of_every_length(gpu, n):
+    c = Cache([n], H=1, seed=n)
+    r = Rows(c, [n], 4, seed=n)
+    assert_rows(r.gpu(), r.oracle(), f"n {n}")
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("head_major", [False, True])
+def test_chunks_behind_a_cached_prefix(gpu, fp8, head_major):
+    lens, counts = [700, 129, 64, 1025, 5], [3, 129, 1, 40, 5]
+    c = Cache(lens, H=3, fp8=fp8, part=192, seed=5)
+    r = Rows(c, counts, 4, seed=6)
+    assert_rows(r.gpu(head_major=head_major, pad=24), r.oracle())
+
+
+def test_sequences_without_rows_and_rows_without_tokens(gpu):
+    # positions before the first token (a node that holds a later range), between
+    # routes and behind the last one; sequences of no rows and of no tokens
+    c = Cache([100, 0, 50, 80, 0], H=2, part=48, first=[40, 0, 0, 1000, 7], seed=3)
+    r = Rows(c, [60, 4, 0, 33, 0], 3, first_pos=[10, 0, 0, 990, 0], seed=4)
+    got, ref = r.gpu(), r.oracle()
+    assert np.isneginf(ref[1]).sum() > 0
+    assert_rows(got, ref)
+
+
+def test_positions_at_the_ends_of_32_bits(gpu):
+    top = 2 ** 31 - 1
+    c = Cache([70, 40, 40], H=1, first=[top - 70, top - 40, -20], seed=8)
+    r = Rows(c, [70, 8, 9], 2, first_pos=[top - 70, top - 3, -25], seed=8)
+    assert_rows(r.gpu(), r.oracle())
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1.5])
+def test_scales(gpu, scale):
+    c = Cache([150], H=2, seed=1)
+    r = Rows(c, [150], 4, seed=2)
+    got, ref = r.gpu(scale), r.oracle(scale)
+    # scores of scale 1.5 reach 60: their products' sums are off by 17 times more
+    wide = max(1.0, abs(scale) / 0.0884)
+    d = np.abs(got[1] - ref[1])
+    assert d.max() <= 1e-4 * wide
+    bound = 2.0 ** -8 * np.abs(ref[0]) + (2.0 ** -8 + 2.0 ** -16 + 4e-4 * (wide > 1)) * ref[3]
+    assert np.all(np.abs(got[0] - ref[0]) <= bound + 1e-30)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_few_rows_over_a_long_cache_are_split(gpu, fp8):
+    c = Cache([9000, 20, 4096], H=2, fp8=fp8, part=4096, seed=9)
+    r = Rows(c, [4, 20, 1], 4, seed=9)
+    assert_rows(r.gpu(), r.oracle())
+
+
+def test_rows_of_no_sequence_are_left_alone(gpu):
+    c = Cache([40, 30], H=1, seed=2)
+    r = Rows(c, [40, 30], 2, seed=2)
+    whole = r.gpu()
+    extra = bits(np.random.default_rng(0).standard_normal((5, 2, DIM)))
+    r.q = np.concatenate([extra[:2], r.q, extra[2:]])
+    r.row_begin = r.row_begin + 2
+    out, lse, flags = r.gpu()
+    assert flags == 0
+    assert np.array_equal(out[2:72], whole[0]) and np.array_equal(lse[2:72], whole[1])
+    for x in (out, lse):
+        assert np.isnan(x[:2]).all() and np.isnan(x[72:]).all()
+
+
+def test_hidden_tokens_never_reach_a_row(gpu):
+    """Infinities and NaN in tokens that a row does not see: same bits."""
+    n = 150
+    c = Cache([n], H=2, part=96, seed=11)
+    r = Rows(c, [n], 4, seed=11)
+    clean = r.gpu()
+    for t, v in ((100, 0x7F80), (101, 0x7FC0), (103, 0xFF80), (149, 0x7FC0)):
+        pid, slot = c.at(0, t)
+        c.k_pool[pid, :, slot] = 0x7FC0
+        c.v_pool[pid, :, ::3, slot] = v
+    out, lse, flags = r.gpu()
+    assert flags == 0
+    # rows up to 95 share no tile with them but the pages' own: bit for bit
+    assert np.array_equal(out[:64], clean[0][:64]) and np.array_equal(lse[:64], clean[1][:64])
+    # in their tile the products are added token by token: within the roundings
+    ref = r.oracle()
+    assert_rows((out[:100], lse[:100], 0), (ref[0][:100], ref[1][:100], 0, ref[3][:100]))
+    assert np.isnan(out[100:]).all() and np.isnan(lse[100:]).all()
+
+
+def test_an_infinite_value_reaches_exactly_the_rows_that_see_it(gpu):
+    n = 90
+    c = Cache([n], H=1, seed=12)
+    r = Rows(c, [n], 2, seed=12)
+    pid, slot = c.at(0, 70)
+    c.v_pool[pid, 0, 5, slot] = 0x7F80
+    out, lse, flags = r.gpu()
+    ref = r.oracle()
+    assert flags == 0 and np.isinf(ref[0][70:, :, 5]).all()
+    assert np.array_equal(np.isinf(out), np.isinf(ref[0]))
+    fine = np.isfinite(ref[0])
+    assert (np.abs(out - ref[0])[fine] <= (2.0 ** -7 + 2.0 ** -16) * ref[3][fine]).all()
+
+
+# ------------------------------------------------------------------- trees
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 8, 16])
+def test_trees_of_every_group_size(gpu, G, fp8):
+    lens, counts = [300, 17, 0, 64, 1000], [7, 1, 5, 64, 33]
+    c = Cache(lens, H=2, fp8=fp8, part=256, seed=G)
+    r = Rows(c, counts, G, tree=True, seed=G)
+    assert_rows(r.gpu(), r.oracle(), f"G {G}")
+
+
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 63, 64])
+def test_trees_of_every_size(gpu, n):
+    c = Cache([100], H=1, seed=n)
+    r = Rows(c, [n], 4, tree=True, seed=n)
+    assert_rows(r.gpu(pad=8), r.oracle(), f"n {n}")
+
+
+def test_masks_that_leave_rows_empty(gpu):
+    """Rows of empty masks, of bits past the tree, without their own bit, of bit 63;
+    over empty and short caches."""
+    c = Cache([0, 3, 0], H=2, seed=1)
+    r = Rows(c, [64, 4, 3], 4, tree=True, seed=1)
+    m = r.tree_mask
+    m[:] = np.where(np.arange(len(m)) % 3 == 0, 0, m)
+    m[5] = -1                       # every bit
+    m[7] = np.int64(-2 ** 63)       # the last drafted row alone
+    m[64:68] = [0, 1 << 40, 2, -16]
+    m[68:] = [0, 0, 0]
+    got, ref = r.gpu(), r.oracle()
+    assert np.isneginf(ref[1][68:]).all()
+    assert_rows(got, ref)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_trees_over_long_caches_are_split(gpu, fp8):
+    c = Cache([5000, 12000, 100], H=2, fp8=fp8, part=4096, seed=4)
+    r = Rows(c, [9, 16, 2], 4, tree=True, seed=4)
+    assert_rows(r.gpu(head_major=True), r.oracle())
+
+
+def test_hidden_drafts_never_reach_a_row(gpu):
+    c = Cache([40], H=1, seed=5)
+    r = Rows(c, [12], 4, tree=True, seed=5)
+    r.tree_mask[:] = [1 << i for i in range(12)]      # each itself alone
+    r.v_draft[3], r.k_draft[3] = 0x7F80, 0x7FC0
+    r.v_draft[8, :, ::2] = 0x7FC0
+    out, lse, flags = r.gpu()
+    keep = [i for i in range(12) if i not in (3, 8)]
+    ref = r.oracle()
+    assert flags == 0
+    assert_rows((out[keep], lse[keep], 0), (ref[0][keep], ref[1][keep], 0, ref[3][keep]))
+    assert np.isnan(out[3]).all() and np.isnan(lse[3]).all()
+
+
+# ------------------------------------------------------------- bad tables
+def test_bad_pages_reach_the_rows_that_see_them(gpu):
+    for bad in (-1, 1 << 30):
+        c = Cache([200, 100], H=2, part=128, seed=6)
+        r = Rows(c, [200, 100], 3, seed=6)
+        c.page_ids[4] = bad                    # tokens 64 .. 79 of sequence 0
+        got, ref = r.gpu(), r.oracle()
+        assert ref[2] == 4 and np.isnan(ref[0][64:200]).all() and not np.isnan(ref[0][:64]).any()
+        assert_rows(got, ref)
+        t = Rows(c, [4, 6], 3, tree=True, seed=7)
+        assert_rows(t.gpu(), t.oracle())
+
+
+def test_bad_pages_that_no_row_sees_raise_nothing(gpu):
+    c = Cache([200], H=1, seed=6)
+    r = Rows(c, [40], 4, first_pos=[10], seed=6)
+    c.page_ids[4:] = -5                        # tokens 64 and on; the rows reach 49
+    got, ref = r.gpu(), r.oracle()
+    assert ref[2] == 0
+    assert_rows(got, ref)
+
+
+@pytest.mark.parametrize("what", ["seq", "order", "base", "cap", "ids", "most", "csr", "csr_end"])
+def test_bad_routes_reach_their_sequence(gpu, what):
+    c = Cache([100, 90, 60], H=1, part=64, seed=2)
+    r = Rows(c, [20, 30, 10], 2, seed=2)
+    row = c.routes[2]                          # sequence 1
+    if what == "seq":
+        row[0] = 0
+    elif what == "order":
+        row[3] = row[2] - 1
+    elif what == "base":
+        row[4] = -1
+    elif what == "cap":
+        row[5] = 2
+    elif what == "ids":
+        row[4] = len(c.page_ids) - 2
+    elif what == "most":
+        c.max_pages = 3
+    elif what == "csr":
+        c.seq_route_begin[1] = 5
+    else:
+        c.seq_route_begin[3] = 100
+    got, ref = r.gpu(), r.oracle()
+    assert ref[2] == 2 and np.isnan(ref[0]).any()
+    assert_rows(got, ref, what)
+
+
+@pytest.mark.parametrize("begin", [[0, 50, 20, 60], [-1, 20, 50, 60], [0, 20, 50, 61]])
+def test_a_bad_row_table_makes_every_row_nan(gpu, begin):
+    c = Cache([100, 90, 60], H=2, seed=2)
+    for tree in (False, True):
+        r = Rows(c, [20, 30, 10], 2, tree=tree, seed=2)
+        r.row_begin = np.array(begin, np.int32)
+        out, lse, flags = r.gpu()
+        assert flags == 2 and np.isnan(out).all() and np.isnan(lse).all()
+
+
+def test_too_many_drafts_of_one_sequence(gpu):
+    c = Cache([30, 30], H=1, seed=2)
+    r = Rows(c, [65, 64], 2, tree=True, seed=2)
+    got, ref = r.gpu(), r.oracle()
+    assert ref[2] == 2
+    assert_rows(got, ref)
+
+
+# ------------------------------------------------------------ how it is run
+def test_same_bits_for_any_placement_stream_and_repeat(gpu):
+    import torch
+    lens, counts = [3000, 500, 77], [5, 64, 30]
+    for tree in (False, True):
+        c = Cache(lens, H=2, part=1024, seed=3)
+        r = Rows(c, counts, 4, tree=tree, seed=3)
+        a = r.gpu()
+        b = r.gpu(stream=torch.cuda.Stream())
+        d = r.gpu(head_major=True, pad=8)
+        for x in (b, d):
+            assert np.array_equal(a[0], x[0]) and np.array_equal(a[1], x[1])
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_graph_replays(gpu, tree):
+    """A captured call replayed with other queries between eager work."""
+    import torch
+    c = Cache([4000, 300], H=2, part=2048, seed=3)
+    r = Rows(c, [8, 20], 4, tree=tree, seed=3)
+    call, out, lse, err = r.gpu(run=False)
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    q = call._keep[1]
+    for k in range(4):
+        q.copy_(torch.randn(q.shape, device="cuda").to(torch.bfloat16))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        a, b = out.clone(), lse.clone()
+        out.zero_()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(a, out) and torch.equal(b, lse), k
+    assert int(err.item()) == 0
