@@ -488,8 +488,21 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// x of the lane 32 away.
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+// The x of the lower and of the upper of this lane and the one 32 away.  (The
+// compiler's builtin for this instruction returns its first result twice.)
+__device__ __forceinline__ f32x2 both_halves(float x) {
+  float lo = x, hi = x;
+  asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(lo), "+v"(hi));
+  return f32x2{lo, hi};
+}
+__device__ __forceinline__ float max_halves(float x) {
+  const f32x2 u = both_halves(x);
+  return fmaxf(u.x, u.y);
+}
+__device__ __forceinline__ float sum_halves(float x) {
+  const f32x2 u = both_halves(x);
+  return u.x + u.y;
+}
 
 // The visible tokens of a sequence as tiles of 64, route after route.
 struct Walk {
@@ -497,6 +510,7 @@ struct Walk {
   int base, n;    // its first page id's index, its tokens that the row tile sees
   int tb;         // its first token
   int j, tiles;   // next tile of the route, its tiles
+  int ids, ids_next;  // lane i: page ids of its pages 64 (j / 16) + i, and of the 64 behind
 };
 
 // One tile: tokens tok0 .. of a route of which the row tile sees n, and its pages.
@@ -511,13 +525,33 @@ __device__ __forceinline__ int visible(const int32_t* rp, int64_t last_pos) {
   return (int)(see < 0 ? 0 : see < n ? see : n);
 }
 
+// Page ids of the pages `first` + lane of the walk's route, its last page's behind it.
+__device__ __forceinline__ int load_ids(const RowsArgs& a, const Walk& w, int first, int lane) {
+  return a.page_ids[w.base + min(first + lane, (w.n - 1) / kPage)];
+}
+
+// Enters route w.r at tile j.
+__device__ __forceinline__ void walk_enter(const RowsArgs& a, Walk& w, int64_t last_pos, int j,
+                                           int lane) {
+  const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + w.r);
+  w.n = uniform(visible(rp, last_pos));
+  w.tb = uniform(rp[2]);
+  w.base = uniform(rp[4]);
+  w.tiles = (w.n + kKeyTile - 1) / kKeyTile;
+  w.j = j;
+  if (w.tiles > 0) {
+    w.ids = load_ids(a, w, 64 * (j / 16), lane);
+    w.ids_next = load_ids(a, w, 64 * (j / 16 + 1), lane);
+  }
+}
+
 // Positions the walk at key tile k of the sequence; tiles of a route: its
 // visible tokens / 64, rounded up.  Sixty-four routes at a time.
 __device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int r1, int64_t last_pos,
                                         int64_t k, int lane) {
   w.r = w.r_end = r1;
   w.j = w.tiles = 0;
-  w.base = w.n = w.tb = 0;
+  w.base = w.n = w.tb = w.ids = w.ids_next = 0;
   for (int r = r0; r < r1; r += 64) {
     int tiles = 0;
     if (r + lane < r1)
@@ -532,14 +566,8 @@ __device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int 
     const uint64_t found = __ballot(x > k);
     if (found) {
       const int at = __builtin_ctzll(found);
-      const int64_t before = __shfl((long long)(x - tiles), at);
       w.r = uniform(r + at);
-      const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + w.r);
-      w.n = uniform(visible(rp, last_pos));
-      w.tb = uniform(rp[2]);
-      w.base = uniform(rp[4]);
-      w.tiles = (w.n + kKeyTile - 1) / kKeyTile;
-      w.j = uniform((int)(k - before));
+      walk_enter(a, w, last_pos, uniform((int)(k - __shfl((long long)(x - tiles), at))), lane);
       return;
     }
     k -= __shfl((long long)x, 63);
@@ -547,73 +575,83 @@ __device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int 
 }
 
 // The next tile; false at the end of the routes.
-__device__ __forceinline__ bool walk_next(const RowsArgs& a, Walk& w, int64_t last_pos, Tile& t) {
+__device__ __forceinline__ bool walk_next(const RowsArgs& a, Walk& w, int64_t last_pos, int lane,
+                                          Tile& t) {
   while (w.j >= w.tiles) {
     if (w.r >= w.r_end || ++w.r >= w.r_end) return false;
-    const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + w.r);
-    w.n = uniform(visible(rp, last_pos));
-    w.tb = uniform(rp[2]);
-    w.base = uniform(rp[4]);
-    w.tiles = (w.n + kKeyTile - 1) / kKeyTile;
-    w.j = 0;
+    walk_enter(a, w, last_pos, 0, lane);
   }
   t.tok0 = w.j * kKeyTile;
   t.n = w.n;
   t.tb = w.tb;
   t.draft = false;
-  const int last = (w.n - 1) / kPage;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) t.pid[i] = uniform(a.page_ids[w.base + min(4 * w.j + i, last)]);
+  for (int i = 0; i < 4; ++i) t.pid[i] = __builtin_amdgcn_readlane(w.ids, 4 * (w.j & 15) + i);
   w.j += 1;
+  if ((w.j & 15) == 0 && w.j < w.tiles) {
+    w.ids = w.ids_next;
+    w.ids_next = load_ids(a, w, 64 * (w.j / 16 + 1), lane);
+  }
   return true;
 }
 
-// Byte offset of 16-byte chunk c of token row `row` in a K tile in LDS, and of
-// half hh (slots 8 hh ..) of row d of page `page` in a V tile.  The exclusive
-// ors spread the rows that a matrix operand reads at once over all banks.
+// Byte offset of 16-byte chunk c of token row `row` in a K tile in LDS: the
+// exclusive or spreads the rows that a matrix operand reads at once over all
+// banks.
 __device__ __forceinline__ int k_at(int row, int c) { return row * 256 + ((c ^ (row & 15)) << 4); }
+// ... of half hh (slots 8 hh ..) of row d of page `page` in a V tile: the order
+// in which the lanes of a matrix operand read it.
 __device__ __forceinline__ int v_at(int page, int d, int hh) {
-  return page * 4096 + d * 32 + ((hh ^ ((d >> 3) & 1)) << 4);
+  return page * 4096 + (d >> 5) * 1024 + hh * 512 + (d & 31) * 16;
 }
 
-// A tile's K and V as a thread loads them.
-template <bool FP8>
-struct Staged {
-  u32x4 k[FP8 ? 2 : 4], v[FP8 ? 2 : 4];
-  float scale;  // fp8: thread i < 8 the K (i < 4) or V scale of page i % 4
-};
-
-template <bool FP8>
 __device__ __forceinline__ int page_or_0(const RowsArgs& a, int pid) {
   return pid >= 0 && pid < a.num_pages ? pid : 0;
 }
 
-template <bool FP8>
-__device__ __forceinline__ void load_tile(const RowsArgs& a, const Tile& t, int g, int tid,
-                                          Staged<FP8>& s) {
-  const int H = a.num_kv_heads, wave = tid >> 6;
-  if constexpr (!FP8) {
+// fp8: a tile's K and V as a thread loads them.
+struct Staged {
+  u32x4 k[2], v[2];
+  float scale;  // thread i < 8: the K (i < 4) or V scale of page i % 4
+};
+
+// 16 bytes a lane from memory straight into LDS, 1 KiB a wave.
+__device__ __forceinline__ void to_lds(const char* g, char* l) {
+  __builtin_amdgcn_global_load_lds(
+      (const __attribute__((address_space(1))) uint32_t*)g,
+      (__attribute__((address_space(3))) uint32_t*)(__attribute__((address_space(3))) void*)l, 16,
+      0, 0);
+}
+
+// bf16: the tile's pages into LDS.  Wave w takes four token rows of each K page
+// and 32 dims of each V page, each lane the chunk whose place in LDS it fills.
+__device__ __forceinline__ void load_tile(const RowsArgs& a, const Tile& t, int g, int wave,
+                                          uint32_t koff, uint32_t voff, char* lk, char* lv) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const size_t at =
-          slice_of(page_or_0<FP8>(a, t.pid[i]), g, H, a.num_pages, a.head_major) * (kPage * kDim);
-      s.k[i] = ld16(static_cast<const uint16_t*>(a.k_pool) + at + tid * 8);
-      s.v[i] = ld16(static_cast<const uint16_t*>(a.v_pool) + at + tid * 8);
-    }
-  } else {
+  for (int i = 0; i < 4; ++i) {
+    const size_t at = slice_of(page_or_0(a, t.pid[i]), g, a.num_kv_heads, a.num_pages,
+                               a.head_major) * (kPage * kDim * 2);
+    to_lds(static_cast<const char*>(a.k_pool) + at + koff, lk + 4096 * i + 1024 * wave);
+    to_lds(static_cast<const char*>(a.v_pool) + at + voff, lv + 4096 * i + 1024 * wave);
+  }
+}
+
+// fp8: into registers.
+__device__ __forceinline__ void load_tile(const RowsArgs& a, const Tile& t, int g, int wave,
+                                          int tid, Staged& s) {
+  const int H = a.num_kv_heads;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int pid = uniform(wave >> 1 ? t.pid[2 * i + 1] : t.pid[2 * i]);
-      const size_t at =
-          slice_of(page_or_0<FP8>(a, pid), g, H, a.num_pages, a.head_major) * (kPage * kDim);
-      s.k[i] = ld16(static_cast<const uint8_t*>(a.k_pool) + at + (tid & 127) * 16);
-      s.v[i] = ld16(static_cast<const uint8_t*>(a.v_pool) + at + (tid & 127) * 16);
-    }
-    if (tid < 8) {
-      const int i = tid & 3;
-      const int pid = i & 2 ? (i & 1 ? t.pid[3] : t.pid[2]) : (i & 1 ? t.pid[1] : t.pid[0]);
-      s.scale = (tid < 4 ? a.k_scale : a.v_scale)[(size_t)page_or_0<FP8>(a, pid) * H + g];
-    }
+  for (int i = 0; i < 2; ++i) {
+    const int pid = wave >> 1 ? t.pid[2 * i + 1] : t.pid[2 * i];
+    const size_t at =
+        slice_of(page_or_0(a, pid), g, H, a.num_pages, a.head_major) * (kPage * kDim);
+    s.k[i] = ld16(static_cast<const char*>(a.k_pool) + at + (uint32_t)(tid & 127) * 16);
+    s.v[i] = ld16(static_cast<const char*>(a.v_pool) + at + (uint32_t)(tid & 127) * 16);
+  }
+  if (tid < 8) {
+    const int i = tid & 3;
+    const int pid = i & 2 ? (i & 1 ? t.pid[3] : t.pid[2]) : (i & 1 ? t.pid[1] : t.pid[0]);
+    s.scale = (tid < 4 ? a.k_scale : a.v_scale)[(size_t)page_or_0(a, pid) * H + g];
   }
 }
 
@@ -639,39 +677,32 @@ __device__ __forceinline__ u32x4 cut(u32x4 x, int first, int lim) {
   return x;
 }
 
-// Into LDS as bf16; V of slots past the visible tokens is zeroed (they may hold
-// anything, and a weight of 0 does not undo an infinity).
-template <bool FP8>
-__device__ __forceinline__ void store_tile(const Staged<FP8>& s, const Tile& t, int tid, char* lk,
-                                           char* lv, float* scales) {
-  const bool ends = t.tok0 + kKeyTile > t.n;
-  if constexpr (!FP8) {
+// fp8: into LDS as bf16.
+__device__ __forceinline__ void store_tile(const Staged& s, int tid, char* lk, char* lv,
+                                           float* scales) {
+  const int t7 = tid & 127;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      *reinterpret_cast<u32x4*>(lk + k_at(16 * i + (tid >> 4), tid & 15)) = s.k[i];
-      u32x4 v = s.v[i];
-      if (ends) v = cut(v, t.tok0 + 16 * i + 8 * (tid & 1), t.n);
-      *reinterpret_cast<u32x4*>(lv + v_at(i, tid >> 1, tid & 1)) = v;
-    }
-  } else {
-    const int t7 = tid & 127;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int page = 2 * i + (tid >> 7);
-      u32x4 lo, hi;
-      widen(s.k[i], lo, hi);
-      const int row = 16 * page + (t7 >> 3);
-      *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7))) = lo;
-      *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7) + 1)) = hi;
-      widen(s.v[i], lo, hi);
-      if (ends) {
-        lo = cut(lo, t.tok0 + 16 * page, t.n);
-        hi = cut(hi, t.tok0 + 16 * page + 8, t.n);
-      }
-      *reinterpret_cast<u32x4*>(lv + v_at(page, t7, 0)) = lo;
-      *reinterpret_cast<u32x4*>(lv + v_at(page, t7, 1)) = hi;
-    }
-    if (tid < 8) scales[tid] = s.scale;
+  for (int i = 0; i < 2; ++i) {
+    const int page = 2 * i + (tid >> 7);
+    u32x4 lo, hi;
+    widen(s.k[i], lo, hi);
+    const int row = 16 * page + (t7 >> 3);
+    *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7))) = lo;
+    *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7) + 1)) = hi;
+    widen(s.v[i], lo, hi);
+    *reinterpret_cast<u32x4*>(lv + v_at(page, t7, 0)) = lo;
+    *reinterpret_cast<u32x4*>(lv + v_at(page, t7, 1)) = hi;
+  }
+  if (tid < 8) scales[tid] = s.scale;
+}
+
+// Zeroes V of the slots past the visible tokens (they may hold anything, and a
+// weight of 0 does not undo an infinity).
+__device__ __forceinline__ void cut_tile(const Tile& t, int tid, char* lv) {
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    u32x4* v = reinterpret_cast<u32x4*>(lv + 4096 * i) + tid;
+    *v = cut(*v, t.tok0 + 16 * i + 8 * ((tid >> 5) & 1), t.n);
   }
 }
 
@@ -717,13 +748,16 @@ struct State {
 // 16 (i / 2) + 8 half + 4 (i % 2) + j, so that a lane's 16 results are the 8
 // slots 8 half .. of two pages: just the p that the lane feeds to O^T += V^T P^T,
 // whose depth of 16 is one page.  No value crosses lanes between the products.
-// sees: the tokens of this lane's row (MASK); bad: pages outside the pool.
-template <bool FP8, bool MASK>
+// mask: not every row sees every token; sees: the tokens of this lane's row;
+// bad: pages outside the pool.
+template <bool FP8>
 __device__ __forceinline__ void attend(const char* lk, const char* lv, const float* scales,
-                                       const u32x4 (&q)[8], float c, uint64_t sees, int bad,
-                                       int lane, State& st) {
+                                       const u32x4 (&q)[8], float c, bool mask, uint64_t sees,
+                                       int bad, int lane, State& st) {
   const int half = lane >> 5, l32 = lane & 31;
   const int krow = 16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
+  const int ka = k_at(krow, half);
+  const char* va = lv + 16 * lane;
   f32x16 s[2];
 #pragma unroll
   for (int tg = 0; tg < 2; ++tg) {
@@ -731,25 +765,24 @@ __device__ __forceinline__ void attend(const char* lk, const char* lv, const flo
     for (int i = 0; i < 16; ++i) s[tg][i] = 0.0f;
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks)
-      s[tg] = mfma32(*reinterpret_cast<const u32x4*>(lk + k_at(32 * tg + krow, 2 * ks + half)),
-                     q[ks], s[tg]);
+      s[tg] = mfma32(*reinterpret_cast<const u32x4*>(lk + 8192 * tg + (ka ^ (32 * ks))), q[ks],
+                     s[tg]);
   }
-  // scores in base 2: s c (fp8: the page's scale in it)
-  float cs[4];
+  // fp8: the page's scale into the scores, in base 2
+  if constexpr (FP8) {
 #pragma unroll
-  for (int p = 0; p < 4; ++p) cs[p] = FP8 ? c * scales[p] : c;
-  if constexpr (FP8 || MASK) {
-    const uint64_t mine = sees >> (8 * half);
+    for (int tg = 0; tg < 2; ++tg)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[tg][i] *= c * scales[2 * tg + (i >> 3)];
+  }
+  const uint64_t mine = sees >> (8 * half);
+  if (mask) {
 #pragma unroll
     for (int tg = 0; tg < 2; ++tg)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int page = 2 * tg + (i >> 3);
-        if constexpr (FP8) s[tg][i] *= cs[page];
-        if constexpr (MASK) {
-          if (bad >> page & 1) s[tg][i] = qnan();
-          if (!(mine >> (32 * tg + 16 * (i >> 3) + (i & 7)) & 1)) s[tg][i] = neg_inf();
-        }
+        if (bad >> (2 * tg + (i >> 3)) & 1) s[tg][i] = qnan();
+        if (!(mine >> (32 * tg + 16 * (i >> 3) + (i & 7)) & 1)) s[tg][i] = neg_inf();
       }
   }
   float top = neg_inf();
@@ -757,7 +790,7 @@ __device__ __forceinline__ void attend(const char* lk, const char* lv, const flo
   for (int tg = 0; tg < 2; ++tg)
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[tg][i]);
-  top = fmaxf(top, other_half(top));
+  top = max_halves(top);
   if constexpr (!FP8) top *= c;
   // The reference moves only when a score exceeds it by 2^8: exp2 and the sums
   // stay in range, and most tiles leave the outputs unscaled.
@@ -782,27 +815,24 @@ __device__ __forceinline__ void attend(const char* lk, const char* lv, const flo
       const float e0 = FP8 ? exp2_fast(x0 - m) : exp2_fast(__builtin_fmaf(x0, c, -m));
       const float e1 = FP8 ? exp2_fast(x1 - m) : exp2_fast(__builtin_fmaf(x1, c, -m));
       st.l += e0 + e1;
-      if constexpr (FP8) {
-        float y0 = e0 * scales[4 + page], y1 = e1 * scales[4 + page];
-        if constexpr (MASK) {  // nothing, whatever the page's scale
-          const uint64_t mine = sees >> (8 * half + 16 * page + 2 * i);
-          if (!(mine & 1)) y0 = 0.0f;
-          if (!(mine & 2)) y1 = 0.0f;
-        }
-        p[page][i] = pack_bf16(y0, y1);
-      } else {
-        p[page][i] = pack_bf16(e0, e1);
-      }
+      p[page][i] = FP8 ? pack_bf16(e0 * scales[4 + page], e1 * scales[4 + page])
+                       : pack_bf16(e0, e1);
     }
-  if constexpr (MASK) {
+  if (mask) {
+    if constexpr (FP8) {  // a hidden token weighs nothing, whatever its page's scale
+#pragma unroll
+      for (int page = 0; page < 4; ++page)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t two = (uint32_t)(mine >> (16 * page + 2 * i)) & 3u;
+          p[page][i] &= (two & 1 ? 0x0000FFFFu : 0u) | (two & 2 ? 0xFFFF0000u : 0u);
+        }
+    }
     // A row that does not see a token must not meet its infinities: where the
     // tile holds any, its tokens enter one by one, by a select.
     bool any = false;
-#pragma unroll
-    for (int page = 0; page < 4; ++page)
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
-        any |= not_finite(*reinterpret_cast<const u32x4*>(lv + v_at(page, 32 * dt + l32, half)));
+#pragma unroll 1
+    for (int i = 0; i < 16; ++i) any |= not_finite(*reinterpret_cast<const u32x4*>(va + 1024 * i));
     if (__ballot(any)) {
 #pragma unroll 1
       for (int t = 0; t < kKeyTile; ++t) {
@@ -818,7 +848,7 @@ __device__ __forceinline__ void attend(const char* lk, const char* lv, const flo
           f32x16 x;
 #pragma unroll
           for (int i = 0; i < 16; ++i) x[i] = 0.0f;
-          x = mfma32(*reinterpret_cast<const u32x4*>(lv + v_at(page, 32 * dt + l32, half)) & keep,
+          x = mfma32(*reinterpret_cast<const u32x4*>(va + 4096 * page + 1024 * dt) & keep,
                      pp & keep, x);
 #pragma unroll
           for (int i = 0; i < 16; ++i) st.o[dt][i] += see ? x[i] : 0.0f;
@@ -831,8 +861,8 @@ __device__ __forceinline__ void attend(const char* lk, const char* lv, const flo
   for (int page = 0; page < 4; ++page)
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
-      st.o[dt] = mfma32(*reinterpret_cast<const u32x4*>(lv + v_at(page, 32 * dt + l32, half)),
-                        p[page], st.o[dt]);
+      st.o[dt] = mfma32(*reinterpret_cast<const u32x4*>(va + 4096 * page + 1024 * dt), p[page],
+                        st.o[dt]);
 }
 
 // NaN into the outputs of the (row, head) pairs [m0, m1) of KV head g of rows
@@ -849,12 +879,103 @@ __device__ void fill_nan(const RowsArgs& a, int row0, int64_t m0, int64_t m1, in
 }
 
 // One work item of one KV head: four waves of 32 (row, head) pairs each, over
-// K/V tiles of 64 tokens that they share through LDS.
+// K/V tiles of 64 tokens that they share through LDS, one tile on its way while
+// another is worked on.
+template <bool FP8, bool TREE>
+struct Work {
+  const RowsArgs& a;
+  int tid, lane, wave, g;
+  int row0, n_rows;
+  bool any;                  // the wave has rows
+  float c;
+  u32x4 q[8];
+  int64_t pos, pos_min, pos_max, last_pos;  // of the lane's row, the wave's first and last, the tile's last
+  uint64_t draft;            // drafted rows that the lane's row sees
+  Walk walk;
+  int left;                  // tiles of this part still to come
+  bool drafted;              // the drafted tokens have come, or are not this part's
+  uint32_t koff, voff;
+  Staged sg;
+  State st;
+  int flag;
+
+  __device__ __forceinline__ bool next(Tile& t) {
+    if (left > 0 && walk_next(a, walk, last_pos, lane, t)) {
+      if (left != INT32_MAX) --left;
+      return true;
+    }
+    left = 0;
+    if (!TREE || drafted) return false;
+    drafted = true;
+    t.draft = true;
+    t.tok0 = 0;
+    t.n = n_rows;
+    t.tb = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t.pid[i] = 0;
+    return true;
+  }
+
+  // Tile t on its way into (lk, lv): bf16 pages at once, fp8 pages as far as
+  // registers; drafted tokens wait for `arrive`.
+  __device__ __forceinline__ void start(const Tile& t, char* lk, char* lv) {
+    if (TREE && t.draft) return;
+    if constexpr (FP8)
+      load_tile(a, t, g, wave, tid, sg);
+    else
+      load_tile(a, t, g, wave, koff, voff, lk, lv);
+  }
+  __device__ __forceinline__ void arrive(const Tile& t, char* lk, char* lv, float* scales) {
+    if (TREE && t.draft)
+      stage_draft(a, row0, n_rows, g, tid, lk, lv, scales);
+    else if constexpr (FP8)
+      store_tile(sg, tid, lk, lv, scales);
+  }
+
+  // Works on tile `cur` in (lk, lv, scales) while `nxt` comes into (nk, nv, ns);
+  // false if there is none.
+  __device__ __forceinline__ bool step(Tile& cur, const char* __restrict__ lk,
+                                       char* __restrict__ lv, const float* __restrict__ scales,
+                                       char* __restrict__ nk, char* __restrict__ nv,
+                                       float* __restrict__ ns) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's part of `cur` is in LDS
+    __syncthreads();
+    Tile nxt;
+    const bool more = next(nxt);
+    if (more) start(nxt, nk, nv);
+    if (cur.tok0 + kKeyTile > cur.n && !cur.draft) {
+      cut_tile(cur, tid, lv);
+      __syncthreads();
+    }
+    const int64_t n_see = min(pos - cur.tb + 1, (int64_t)cur.n) - cur.tok0;
+    int bad = 0;
+    if (!cur.draft) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (cur.tok0 + 16 * i < cur.n && (cur.pid[i] < 0 || cur.pid[i] >= a.num_pages))
+          bad |= 1 << i;
+      if (bad) flag = KF_EFLAG_BAD_PAGE;
+    }
+    if (any && pos_max - cur.tb >= cur.tok0) {
+      const bool mask = bad || cur.draft || cur.tok0 + kKeyTile > cur.n ||
+                        pos_min - cur.tb < cur.tok0 + kKeyTile - 1;
+      const uint64_t sees = cur.draft ? draft
+                            : n_see <= 0 ? 0
+                            : n_see >= 64 ? ~(uint64_t)0
+                                          : ((uint64_t)1 << n_see) - 1;
+      attend<FP8>(lk, lv, scales, q, c, mask, sees, bad, lane, st);
+    }
+    if (more) arrive(nxt, nk, nv, ns);
+    cur = nxt;
+    return more;
+  }
+};
+
 template <bool FP8, bool TREE>
 __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
-  __shared__ __align__(16) char lk[2][kKeyTile * 256];
-  __shared__ __align__(16) char lv[2][kKeyTile * 256];
-  __shared__ __align__(16) float scales[2][8];
+  __shared__ __align__(16) char k0[kKeyTile * 256], v0[kKeyTile * 256];
+  __shared__ __align__(16) char k1[kKeyTile * 256], v1[kKeyTile * 256];
+  __shared__ __align__(16) float s0[8], s1[8];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
   const int H = a.num_kv_heads, G = a.group;
@@ -876,116 +997,65 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   }
   // this lane's row and head
   const int64_t m = m0 + 32 * wave + l32;
-  const bool mine = m < m1, any = m0 + 32 * wave < m1;
+  const bool mine = m < m1;
   const int64_t mc = mine ? m : m1 - 1;
   const int row = (int)(mc / G), h = g * G + (int)(mc % G);
   const float c0 = a.scale_log2;
-  const float c = c0 == 0.0f ? 1.0f : fabsf(c0);
-  u32x4 q[8];
+  Work<FP8, TREE> w{a};
+  w.tid = tid;
+  w.lane = lane;
+  w.wave = wave;
+  w.g = g;
+  w.row0 = row0;
+  w.n_rows = n_rows;
+  w.any = m0 + 32 * wave < m1;
+  w.c = c0 == 0.0f ? 1.0f : fabsf(c0);
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) {
-    q[ks] = ld16(a.q + (row0 + row) * a.q_stride + (size_t)h * kDim + 16 * ks + 8 * half);
-    if (c0 < 0.0f) q[ks] ^= 0x80008000u;                 // a negative scale turns the row around
-    if (c0 == 0.0f || !mine) q[ks] = u32x4{0, 0, 0, 0};  // a zero one makes all scores equal
+    u32x4 x = ld16(a.q + (row0 + row) * a.q_stride + (size_t)h * kDim + 16 * ks + 8 * half);
+    if (c0 < 0.0f) x ^= 0x80008000u;                 // a negative scale turns the row around
+    if (c0 == 0.0f || !mine) x = u32x4{0, 0, 0, 0};  // a zero one makes all scores equal
+    w.q[ks] = x;
   }
-  int64_t pos = INT32_MAX, pos_min = INT32_MAX, last_pos = INT32_MAX;
-  uint64_t draft = 0;
+  w.pos = w.pos_min = w.pos_max = w.last_pos = INT32_MAX;
+  w.draft = 0;
   if constexpr (TREE) {
-    draft = mine ? a.tree_mask[row0 + row] : 0;
-    if (n_rows < 64) draft &= ((uint64_t)1 << n_rows) - 1;
+    w.draft = mine ? a.tree_mask[row0 + row] : 0;
+    if (n_rows < 64) w.draft &= ((uint64_t)1 << n_rows) - 1;
   } else {
     const int64_t p0 = a.first_pos[b];
-    pos = p0 + row;
-    pos_min = p0 + (m0 + 32 * wave < m1 ? m0 + 32 * wave : m1 - 1) / G;
-    last_pos = p0 + (m1 - 1) / G;
+    w.pos = p0 + row;
+    w.pos_min = p0 + min(m0 + 32 * wave, m1 - 1) / G;
+    w.pos_max = p0 + (min(m1, m0 + 32 * wave + 32) - 1) / G;
+    w.last_pos = p0 + (m1 - 1) / G;
   }
-  const int64_t pos_max = TREE ? INT32_MAX : a.first_pos[b] + (min(m1, m0 + 32 * wave + 32) - 1) / G;
-
-  State st;
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) st.o[dt][i] = 0.0f;
-  st.m = neg_inf();
-  st.l = 0.0f;
+    for (int i = 0; i < 16; ++i) w.st.o[dt][i] = 0.0f;
+  w.st.m = neg_inf();
+  w.st.l = 0.0f;
+  w.flag = 0;
+  const int krow = 4 * wave + (lane >> 4);  // of a page
+  w.koff = 256 * krow + 16 * ((lane & 15) ^ krow);
+  w.voff = 1024 * wave + 32 * l32 + 16 * half;
+  walk_to(a, w.walk, a.seq_route_begin[b], a.seq_route_begin[b + 1], w.last_pos, it.key0, lane);
+  w.left = it.key1 == INT32_MAX ? INT32_MAX : it.key1 - it.key0;
+  w.drafted = it.key1 != INT32_MAX;
 
-  Walk walk;
-  walk_to(a, walk, a.seq_route_begin[b], a.seq_route_begin[b + 1], last_pos, it.key0, lane);
-  // the tiles of this part, the drafted tokens behind the last one
-  int left = it.key1 == INT32_MAX ? INT32_MAX : it.key1 - it.key0;
-  bool drafted = !TREE || it.key1 != INT32_MAX;
-  auto next = [&](Tile& t) -> bool {
-    if (left > 0 && walk_next(a, walk, last_pos, t)) {
-      if (left != INT32_MAX) --left;
-      return true;
-    }
-    left = 0;
-    if (drafted) return false;
-    drafted = true;
-    t.draft = true;
-    t.tok0 = 0;
-    t.n = n_rows;
-    t.tb = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) t.pid[i] = 0;
-    return true;
-  };
-  Tile cur{}, nxt{};
-  Staged<FP8> sg;
-  bool has = next(cur);
-  if (has) {
-    if (cur.draft) {
-      stage_draft(a, row0, n_rows, g, tid, lk[0], lv[0], scales[0]);
-    } else {
-      load_tile<FP8>(a, cur, g, tid, sg);
-      store_tile<FP8>(sg, cur, tid, lk[0], lv[0], scales[0]);
+  Tile cur;
+  if (w.next(cur)) {
+    w.start(cur, k0, v0);
+    w.arrive(cur, k0, v0, s0);
+    while (w.step(cur, k0, v0, s0, k1, v1, s1) && w.step(cur, k1, v1, s1, k0, v0, s0)) {
     }
   }
-  int buf = 0, flag = 0;
-  while (has) {
-    __syncthreads();
-    const bool more = next(nxt);
-    if (more && !nxt.draft) load_tile<FP8>(a, nxt, g, tid, sg);
-    // which of the tile's tokens this lane's row sees
-    const int64_t n_see = min(pos - cur.tb + 1, (int64_t)cur.n) - cur.tok0;
-    int bad = 0;
-    if (!cur.draft) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (cur.tok0 + 16 * i < cur.n && (cur.pid[i] < 0 || cur.pid[i] >= a.num_pages))
-          bad |= 1 << i;
-      if (bad) flag = KF_EFLAG_BAD_PAGE;
-    }
-    if (any && pos_max - cur.tb >= cur.tok0) {
-      const bool mask = bad || cur.draft || cur.tok0 + kKeyTile > cur.n ||
-                        pos_min - cur.tb < cur.tok0 + kKeyTile - 1;
-      if (mask) {
-        const uint64_t sees = cur.draft ? draft
-                              : n_see <= 0 ? 0
-                              : n_see >= 64 ? ~(uint64_t)0
-                                            : ((uint64_t)1 << n_see) - 1;
-        attend<FP8, true>(lk[buf], lv[buf], scales[buf], q, c, sees, bad, lane, st);
-      } else {
-        attend<FP8, false>(lk[buf], lv[buf], scales[buf], q, c, 0, 0, lane, st);
-      }
-    }
-    buf ^= 1;
-    if (more) {
-      if (nxt.draft)
-        stage_draft(a, row0, n_rows, g, tid, lk[buf], lv[buf], scales[buf]);
-      else
-        store_tile<FP8>(sg, nxt, tid, lk[buf], lv[buf], scales[buf]);
-    }
-    cur = nxt;
-    has = more;
-  }
-  if (flag && tid == 0) atomicOr(a.err_flags, flag);
-  if (!any) return;
-  const float l = st.l + other_half(st.l);
+  if (w.flag && tid == 0) atomicOr(a.err_flags, w.flag);
+  if (!mine) return;
+  const State& st = w.st;
+  const float l = sum_halves(st.l);
   if (it.rec >= 0) {
-    const int rm = (int)(m - m0);
-    if (!mine) return;
-    const size_t rec = ((size_t)it.rec * H + g) * a.rec_rows + rm;
+    const size_t rec = ((size_t)it.rec * H + g) * a.rec_rows + (int)(m - m0);
     if (half == 0) *reinterpret_cast<f32x2*>(a.rec_ml + 2 * rec) = f32x2{st.m, l};
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
@@ -995,7 +1065,6 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
             f32x4{st.o[dt][4 * i], st.o[dt][4 * i + 1], st.o[dt][4 * i + 2], st.o[dt][4 * i + 3]};
     return;
   }
-  if (!mine) return;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   const size_t at = (size_t)(row0 + row) * a.num_q_heads + h;
 #pragma unroll
