@@ -7,7 +7,7 @@
 namespace kf {
 
 constexpr int kRowTile = 128;     // (row, query head) pairs of one KV head per workgroup
-constexpr int kKeyTile = 64;      // tokens per step of a workgroup: four pages
+constexpr int kKeyTile = 32;      // tokens per step of a workgroup: two pages
 constexpr int kMaxRecsPerCu = 8;  // records of split work items per compute unit
 
 // ------------------------------------------------------------------- append

@@ -296,7 +296,7 @@ __device__ __forceinline__ int64_t wave_sum(int64_t x) {
 template <bool TREE>
 __device__ __forceinline__ int key_tiles(const RowsArgs& a, int b, int t, int n, int tokens,
                                          int first) {
-  if (TREE) return (tokens + kKeyTile - 1) / kKeyTile + 1;
+  if (TREE) return (tokens + kKeyTile - 1) / kKeyTile + (n + kKeyTile - 1) / kKeyTile;
   const int64_t rows = ((int64_t)(t + 1) * kRowTile - 1) / a.group;
   const int64_t end = a.first_pos[b] + (rows < n ? rows : n - 1) + 1 - first;
   const int64_t see = end < 0 ? 0 : end < tokens ? end : tokens;
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
   int cap = most;
   if (a.max_recs > 1 && (int64_t)T * a.num_kv_heads < 4 * (int64_t)a.slots) {
     const unsigned long long share = (s_work * a.num_kv_heads + a.slots - 1) / a.slots;
-    cap = (int)min((unsigned long long)most, max(share, 8ull));
+    cap = (int)min((unsigned long long)most, max(share, 16ull));
     for (;;) {  // parts of split tiles, until their records fit
       __syncthreads();
       if (tid == 0) s_recs = 0;
@@ -504,59 +504,71 @@ __device__ __forceinline__ float sum_halves(float x) {
   return u.x + u.y;
 }
 
-// The visible tokens of a sequence as tiles of 64, route after route.
+// Tables that no kernel of the launch writes, read through the scalar cache.
+template <class T>
+__device__ __forceinline__ const __attribute__((address_space(4))) T* fixed(const T* p) {
+  return (const __attribute__((address_space(4))) T*)(uintptr_t)p;
+}
+
+// The visible tokens of a sequence as tiles of 32, route after route.
 struct Walk {
   int r, r_end;   // current route, the sequence's last + 1
   int base, n;    // its first page id's index, its tokens that the row tile sees
   int tb;         // its first token
   int j, tiles;   // next tile of the route, its tiles
-  int ids, ids_next;  // lane i: page ids of its pages 64 (j / 16) + i, and of the 64 behind
+  int pid[2];     // page ids of that tile, on their way
 };
 
-// One tile: tokens tok0 .. of a route of which the row tile sees n, and its pages.
+// One tile: its first token's position (of drafted tokens: its first row), how
+// many of its tokens there are (0: there is no such tile), its pages outside the
+// pool (bits 0 and 1), whether it holds drafted tokens.
 struct Tile {
-  int tok0, n, tb;
-  int pid[4];
+  int pos0, left, bad;
   bool draft;
 };
 
-__device__ __forceinline__ int visible(const int32_t* rp, int64_t last_pos) {
-  const int64_t n = (int64_t)rp[3] - rp[2], see = last_pos + 1 - rp[2];
+__device__ __forceinline__ int visible(int begin, int end, int last_pos) {
+  const int64_t n = (int64_t)end - begin, see = (int64_t)last_pos + 1 - begin;
   return (int)(see < 0 ? 0 : see < n ? see : n);
 }
 
-// Page ids of the pages `first` + lane of the walk's route, its last page's behind it.
-__device__ __forceinline__ int load_ids(const RowsArgs& a, const Walk& w, int first, int lane) {
-  return a.page_ids[w.base + min(first + lane, (w.n - 1) / kPage)];
+__device__ __forceinline__ void walk_ids(const RowsArgs& a, Walk& w) {
+  const int last = (w.n - 1) / kPage;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) w.pid[i] = fixed(a.page_ids)[w.base + min(2 * w.j + i, last)];
 }
 
 // Enters route w.r at tile j.
-__device__ __forceinline__ void walk_enter(const RowsArgs& a, Walk& w, int64_t last_pos, int j,
-                                           int lane) {
-  const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + w.r);
-  w.n = uniform(visible(rp, last_pos));
-  w.tb = uniform(rp[2]);
-  w.base = uniform(rp[4]);
+__device__ __forceinline__ void walk_enter(const RowsArgs& a, Walk& w, int last_pos, int j) {
+  const auto* rp = fixed(reinterpret_cast<const int32_t*>(a.routes)) + 6 * (int64_t)w.r;
+  w.n = visible(rp[2], rp[3], last_pos);
+  w.tb = rp[2];
+  w.base = rp[4];
   w.tiles = (w.n + kKeyTile - 1) / kKeyTile;
   w.j = j;
-  if (w.tiles > 0) {
-    w.ids = load_ids(a, w, 64 * (j / 16), lane);
-    w.ids_next = load_ids(a, w, 64 * (j / 16 + 1), lane);
+}
+
+// Behind a route's last tile: the next route that has any.
+__device__ __forceinline__ void walk_on(const RowsArgs& a, Walk& w, int last_pos) {
+  while (w.j >= w.tiles && w.r < w.r_end) {
+    if (++w.r < w.r_end) walk_enter(a, w, last_pos, 0);
   }
+  if (w.r < w.r_end) walk_ids(a, w);
 }
 
 // Positions the walk at key tile k of the sequence; tiles of a route: its
-// visible tokens / 64, rounded up.  Sixty-four routes at a time.
-__device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int r1, int64_t last_pos,
+// visible tokens / 32, rounded up.  Sixty-four routes at a time.
+__device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int r1, int last_pos,
                                         int64_t k, int lane) {
   w.r = w.r_end = r1;
   w.j = w.tiles = 0;
-  w.base = w.n = w.tb = w.ids = w.ids_next = 0;
+  w.base = w.n = w.tb = w.pid[0] = w.pid[1] = 0;
   for (int r = r0; r < r1; r += 64) {
     int tiles = 0;
-    if (r + lane < r1)
-      tiles = (visible(reinterpret_cast<const int32_t*>(a.routes + r + lane), last_pos) +
-               kKeyTile - 1) / kKeyTile;
+    if (r + lane < r1) {
+      const kf_route& row = a.routes[r + lane];
+      tiles = (visible(row.tok_begin, row.tok_end, last_pos) + kKeyTile - 1) / kKeyTile;
+    }
     int64_t x = tiles;
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) {
@@ -567,32 +579,12 @@ __device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int 
     if (found) {
       const int at = __builtin_ctzll(found);
       w.r = uniform(r + at);
-      walk_enter(a, w, last_pos, uniform((int)(k - __shfl((long long)(x - tiles), at))), lane);
+      walk_enter(a, w, last_pos, uniform((int)(k - __shfl((long long)(x - tiles), at))));
+      walk_ids(a, w);
       return;
     }
     k -= __shfl((long long)x, 63);
   }
-}
-
-// The next tile; false at the end of the routes.
-__device__ __forceinline__ bool walk_next(const RowsArgs& a, Walk& w, int64_t last_pos, int lane,
-                                          Tile& t) {
-  while (w.j >= w.tiles) {
-    if (w.r >= w.r_end || ++w.r >= w.r_end) return false;
-    walk_enter(a, w, last_pos, 0, lane);
-  }
-  t.tok0 = w.j * kKeyTile;
-  t.n = w.n;
-  t.tb = w.tb;
-  t.draft = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) t.pid[i] = __builtin_amdgcn_readlane(w.ids, 4 * (w.j & 15) + i);
-  w.j += 1;
-  if ((w.j & 15) == 0 && w.j < w.tiles) {
-    w.ids = w.ids_next;
-    w.ids_next = load_ids(a, w, 64 * (w.j / 16 + 1), lane);
-  }
-  return true;
 }
 
 // Byte offset of 16-byte chunk c of token row `row` in a K tile in LDS: the
@@ -605,54 +597,12 @@ __device__ __forceinline__ int v_at(int page, int d, int hh) {
   return page * 4096 + (d >> 5) * 1024 + hh * 512 + (d & 31) * 16;
 }
 
-__device__ __forceinline__ int page_or_0(const RowsArgs& a, int pid) {
-  return pid >= 0 && pid < a.num_pages ? pid : 0;
-}
-
-// fp8: a tile's K and V as a thread loads them.
-struct Staged {
-  u32x4 k[2], v[2];
-  float scale;  // thread i < 8: the K (i < 4) or V scale of page i % 4
-};
-
 // 16 bytes a lane from memory straight into LDS, 1 KiB a wave.
 __device__ __forceinline__ void to_lds(const char* g, char* l) {
   __builtin_amdgcn_global_load_lds(
       (const __attribute__((address_space(1))) uint32_t*)g,
       (__attribute__((address_space(3))) uint32_t*)(__attribute__((address_space(3))) void*)l, 16,
       0, 0);
-}
-
-// bf16: the tile's pages into LDS.  Wave w takes four token rows of each K page
-// and 32 dims of each V page, each lane the chunk whose place in LDS it fills.
-__device__ __forceinline__ void load_tile(const RowsArgs& a, const Tile& t, int g, int wave,
-                                          uint32_t koff, uint32_t voff, char* lk, char* lv) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const size_t at = slice_of(page_or_0(a, t.pid[i]), g, a.num_kv_heads, a.num_pages,
-                               a.head_major) * (kPage * kDim * 2);
-    to_lds(static_cast<const char*>(a.k_pool) + at + koff, lk + 4096 * i + 1024 * wave);
-    to_lds(static_cast<const char*>(a.v_pool) + at + voff, lv + 4096 * i + 1024 * wave);
-  }
-}
-
-// fp8: into registers.
-__device__ __forceinline__ void load_tile(const RowsArgs& a, const Tile& t, int g, int wave,
-                                          int tid, Staged& s) {
-  const int H = a.num_kv_heads;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int pid = wave >> 1 ? t.pid[2 * i + 1] : t.pid[2 * i];
-    const size_t at =
-        slice_of(page_or_0(a, pid), g, H, a.num_pages, a.head_major) * (kPage * kDim);
-    s.k[i] = ld16(static_cast<const char*>(a.k_pool) + at + (uint32_t)(tid & 127) * 16);
-    s.v[i] = ld16(static_cast<const char*>(a.v_pool) + at + (uint32_t)(tid & 127) * 16);
-  }
-  if (tid < 8) {
-    const int i = tid & 3;
-    const int pid = i & 2 ? (i & 1 ? t.pid[3] : t.pid[2]) : (i & 1 ? t.pid[1] : t.pid[0]);
-    s.scale = (tid < 4 ? a.k_scale : a.v_scale)[(size_t)page_or_0(a, pid) * H + g];
-  }
 }
 
 // 16 E4M3 codes -> two times 8 bf16, exactly.
@@ -669,52 +619,72 @@ __device__ __forceinline__ void widen(u32x4 codes, u32x4& lo, u32x4& hi) {
   hi = u32x4{o[4], o[5], o[6], o[7]};
 }
 
-// Zeroes the bf16 slots first, first + 1 .. of a chunk at and past token `lim`.
-__device__ __forceinline__ u32x4 cut(u32x4 x, int first, int lim) {
+// 4 bytes each of four lanes into LDS.
+__device__ __forceinline__ void to_lds4(const float* g, float* l) {
+  __builtin_amdgcn_global_load_lds(
+      (const __attribute__((address_space(1))) uint32_t*)g,
+      (__attribute__((address_space(3))) uint32_t*)(__attribute__((address_space(3))) void*)l, 4, 0,
+      0);
+}
+
+// A barrier for what the waves wrote to LDS themselves.  (__syncthreads waits
+// for loads on their way into LDS too.)
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Which of 8 bf16 are infinite or NaN: their bits set.
+__device__ __forceinline__ u32x4 not_finite(u32x4 x) {
+  u32x4 m;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    x[i] &= (first + 2 * i < lim ? 0x0000FFFFu : 0u) | (first + 2 * i + 1 < lim ? 0xFFFF0000u : 0u);
-  return x;
+    m[i] = ((x[i] & 0x7F80u) == 0x7F80u ? 0x0000FFFFu : 0u) |
+           ((x[i] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+  return m;
 }
 
-// fp8: into LDS as bf16.
-__device__ __forceinline__ void store_tile(const Staged& s, int tid, char* lk, char* lv,
-                                           float* scales) {
-  const int t7 = tid & 127;
+// The chunks tid, tid + 256 of a V tile in LDS: zeroes the slots from `left` on
+// (they may hold anything, and a weight of 0 does not undo an infinity); whether
+// the others hold infinities or NaN.
+__device__ __forceinline__ bool cut_tile(int left, int tid, char* lv) {
+  u32x4 odd = {0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int page = 2 * i + (tid >> 7);
-    u32x4 lo, hi;
-    widen(s.k[i], lo, hi);
-    const int row = 16 * page + (t7 >> 3);
-    *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7))) = lo;
-    *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7) + 1)) = hi;
-    widen(s.v[i], lo, hi);
-    *reinterpret_cast<u32x4*>(lv + v_at(page, t7, 0)) = lo;
-    *reinterpret_cast<u32x4*>(lv + v_at(page, t7, 1)) = hi;
-  }
-  if (tid < 8) scales[tid] = s.scale;
-}
-
-// Zeroes V of the slots past the visible tokens (they may hold anything, and a
-// weight of 0 does not undo an infinity).
-__device__ __forceinline__ void cut_tile(const Tile& t, int tid, char* lv) {
-#pragma unroll 1
-  for (int i = 0; i < 4; ++i) {
     u32x4* v = reinterpret_cast<u32x4*>(lv + 4096 * i) + tid;
-    *v = cut(*v, t.tok0 + 16 * i + 8 * ((tid >> 5) & 1), t.n);
+    u32x4 x = *v;
+    const int first = 16 * i + 8 * ((tid >> 5) & 1);
+    if (left < kKeyTile) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        x[k] &= (first + 2 * k < left ? 0x0000FFFFu : 0u) |
+                (first + 2 * k + 1 < left ? 0xFFFF0000u : 0u);
+      *v = x;
+    }
+    odd |= not_finite(x);
+  }
+  return (odd[0] | odd[1] | odd[2] | odd[3]) != 0;
+}
+
+// The same chunks: zeroes infinities and NaN.
+__device__ __forceinline__ void tame_tile(int tid, char* lv) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    u32x4* v = reinterpret_cast<u32x4*>(lv + 4096 * i) + tid;
+    *v &= ~not_finite(*v);
   }
 }
 
-// The drafted tokens of a sequence as a tile: V is turned around on its way.
-__device__ __forceinline__ void stage_draft(const RowsArgs& a, int row0, int n, int g, int tid,
-                                            char* lk, char* lv, float* scales) {
+// The drafted tokens t0 .. of a sequence as a tile: V is turned around on its way.
+__device__ __forceinline__ void stage_draft(const RowsArgs& a, int row0, int t0, int n, int g,
+                                            int tid, char* lk, char* lv) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 2; ++i) {
     const int row = 16 * i + (tid >> 4), c = tid & 15;
     u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-    if (row < n) {
-      const size_t at = (size_t)(row0 + row) * a.kv_stride + (size_t)g * kDim + 8 * c;
+    if (t0 + row < n) {
+      const size_t at = (size_t)(row0 + t0 + row) * a.kv_stride + (size_t)g * kDim + 8 * c;
       k = ld16(a.k_draft + at);
       v = ld16(a.v_draft + at);
     }
@@ -724,16 +694,6 @@ __device__ __forceinline__ void stage_draft(const RowsArgs& a, int row0, int n, 
       *reinterpret_cast<uint16_t*>(lv + v_at(i, 8 * c + e, (row & 15) >> 3) + 2 * (row & 7)) =
           (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
   }
-  if (tid < 8) scales[tid] = 1.0f;
-}
-
-// Whether any of 8 bf16 is infinite or NaN.
-__device__ __forceinline__ bool not_finite(u32x4 x) {
-  bool any = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    any |= (x[i] & 0x7F80u) == 0x7F80u || (x[i] & 0x7F800000u) == 0x7F800000u;
-  return any;
 }
 
 // Softmax state of one (row, head) per lane column q = lane % 32, shared by the
@@ -744,52 +704,38 @@ struct State {
   float m, l;
 };
 
-// One tile.  S^T = K Q^T: matrix row 8 i + 4 half + j of 32 is token
-// 16 (i / 2) + 8 half + 4 (i % 2) + j, so that a lane's 16 results are the 8
-// slots 8 half .. of two pages: just the p that the lane feeds to O^T += V^T P^T,
-// whose depth of 16 is one page.  No value crosses lanes between the products.
-// mask: not every row sees every token; sees: the tokens of this lane's row;
-// bad: pages outside the pool.
+// A tile's scores and weights p.  S^T = K Q^T: matrix row 8 i + 4 half + j of 32
+// is token 16 (i / 2) + 8 half + 4 (i % 2) + j, so that a lane's 16 results are
+// the 8 slots 8 half .. of two pages: just the p that the lane feeds to
+// O^T += V^T P^T, whose depth of 16 is one page.  No value crosses lanes between
+// the products.  mask: not every row sees every token; sees: the tokens of this
+// lane's row; bad: pages outside the pool; scales: K and V scales of the pages
+// (fp8).
 template <bool FP8>
-__device__ __forceinline__ void attend(const char* lk, const char* lv, const float* scales,
-                                       const u32x4 (&q)[8], float c, bool mask, uint64_t sees,
-                                       int bad, int lane, State& st) {
-  const int half = lane >> 5, l32 = lane & 31;
-  const int krow = 16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
-  const int ka = k_at(krow, half);
-  const char* va = lv + 16 * lane;
-  f32x16 s[2];
+__device__ __forceinline__ void weigh(const char* lk, f32x4 scales, const u32x4 (&q)[8], float c,
+                                      bool mask, uint32_t sees, int bad, int ka, int half,
+                                      State& st, u32x4 (&p)[2]) {
+  f32x16 s;
 #pragma unroll
-  for (int tg = 0; tg < 2; ++tg) {
+  for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[tg][i] = 0.0f;
+  for (int k = 0; k < 8; ++k)
+    s = mfma32(*reinterpret_cast<const u32x4*>(lk + (ka ^ (32 * k))), q[k], s);
+  if constexpr (FP8) {  // the page's scale into the scores, in base 2
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks)
-      s[tg] = mfma32(*reinterpret_cast<const u32x4*>(lk + 8192 * tg + (ka ^ (32 * ks))), q[ks],
-                     s[tg]);
+    for (int i = 0; i < 16; ++i) s[i] *= c * scales[i >> 3];
   }
-  // fp8: the page's scale into the scores, in base 2
-  if constexpr (FP8) {
-#pragma unroll
-    for (int tg = 0; tg < 2; ++tg)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[tg][i] *= c * scales[2 * tg + (i >> 3)];
-  }
-  const uint64_t mine = sees >> (8 * half);
+  const uint32_t mine = sees >> (8 * half);
   if (mask) {
 #pragma unroll
-    for (int tg = 0; tg < 2; ++tg)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if (bad >> (2 * tg + (i >> 3)) & 1) s[tg][i] = qnan();
-        if (!(mine >> (32 * tg + 16 * (i >> 3) + (i & 7)) & 1)) s[tg][i] = neg_inf();
-      }
+    for (int i = 0; i < 16; ++i) {
+      if (bad >> (i >> 3) & 1) s[i] = qnan();
+      if (!(mine >> (16 * (i >> 3) + (i & 7)) & 1)) s[i] = neg_inf();
+    }
   }
   float top = neg_inf();
 #pragma unroll
-  for (int tg = 0; tg < 2; ++tg)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[tg][i]);
+  for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
   top = max_halves(top);
   if constexpr (!FP8) top *= c;
   // The reference moves only when a score exceeds it by 2^8: exp2 and the sums
@@ -805,64 +751,53 @@ __device__ __forceinline__ void attend(const char* lk, const char* lv, const flo
       for (int i = 0; i < 16; ++i) st.o[dt][i] *= f;
   }
   const float m = st.m == neg_inf() ? 0.0f : st.m;
-  u32x4 p[4];
 #pragma unroll
-  for (int page = 0; page < 4; ++page)
+  for (int page = 0; page < 2; ++page)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int at = 8 * (page & 1) + 2 * i;
-      const float x0 = s[page >> 1][at], x1 = s[page >> 1][at + 1];
+      const float x0 = s[8 * page + 2 * i], x1 = s[8 * page + 2 * i + 1];
       const float e0 = FP8 ? exp2_fast(x0 - m) : exp2_fast(__builtin_fmaf(x0, c, -m));
       const float e1 = FP8 ? exp2_fast(x1 - m) : exp2_fast(__builtin_fmaf(x1, c, -m));
       st.l += e0 + e1;
-      p[page][i] = FP8 ? pack_bf16(e0 * scales[4 + page], e1 * scales[4 + page])
+      p[page][i] = FP8 ? pack_bf16(e0 * scales[2 + page], e1 * scales[2 + page])
                        : pack_bf16(e0, e1);
     }
-  if (mask) {
-    if constexpr (FP8) {  // a hidden token weighs nothing, whatever its page's scale
+  if (FP8 && mask) {  // a hidden token weighs nothing, whatever its page's scale
 #pragma unroll
-      for (int page = 0; page < 4; ++page)
+    for (int page = 0; page < 2; ++page)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t two = (uint32_t)(mine >> (16 * page + 2 * i)) & 3u;
-          p[page][i] &= (two & 1 ? 0x0000FFFFu : 0u) | (two & 2 ? 0xFFFF0000u : 0u);
-        }
-    }
-    // A row that does not see a token must not meet its infinities: where the
-    // tile holds any, its tokens enter one by one, by a select.
-    bool any = false;
-#pragma unroll 1
-    for (int i = 0; i < 16; ++i) any |= not_finite(*reinterpret_cast<const u32x4*>(va + 1024 * i));
-    if (__ballot(any)) {
-#pragma unroll 1
-      for (int t = 0; t < kKeyTile; ++t) {
-        const int page = t >> 4, k = t & 15;
-        const u32x4 pp = page & 2 ? (page & 1 ? p[3] : p[2]) : (page & 1 ? p[1] : p[0]);
-        u32x4 keep = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (half == k >> 3 && i == (k & 7) >> 1) keep[i] = k & 1 ? 0xFFFF0000u : 0x0000FFFFu;
-        const bool see = sees >> t & 1;
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt) {
-          f32x16 x;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] = 0.0f;
-          x = mfma32(*reinterpret_cast<const u32x4*>(va + 4096 * page + 1024 * dt) & keep,
-                     pp & keep, x);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) st.o[dt][i] += see ? x[i] : 0.0f;
-        }
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t two = mine >> (16 * page + 2 * i) & 3u;
+        p[page][i] &= (two & 1 ? 0x0000FFFFu : 0u) | (two & 2 ? 0xFFFF0000u : 0u);
       }
-      return;
-    }
   }
+}
+
+// Infinities and NaN of a V tile into the outputs of the rows that see them (a
+// product would spread them to all 32 rows, whose weights of 0 do not undo them).
+__device__ __forceinline__ void add_odd(const char* lv, uint32_t sees, const u32x4 (&p)[2], int lane,
+                                        State& st) {
+  const int half = lane >> 5;
+#pragma unroll 1
+  for (int t = 0; t < kKeyTile; ++t) {
+    uint32_t two = 0;
 #pragma unroll
-  for (int page = 0; page < 4; ++page)
+    for (int i = 0; i < 8; ++i)
+      if (i == (t >> 4) * 4 + ((t & 7) >> 1)) two = p[i >> 2][i & 3];
+    const uint32_t w = (uint32_t)__shfl((int)two, (lane & 31) + 32 * ((t >> 3) & 1));
+    const float pt = __builtin_bit_cast(float, t & 1 ? w & 0xFFFF0000u : w << 16);
+    const bool see = sees >> t & 1;
+    const char* col = lv + v_at(t >> 4, 4 * half, (t >> 3) & 1) + 2 * (t & 7);
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
-      st.o[dt] = mfma32(*reinterpret_cast<const u32x4*>(va + 4096 * page + 1024 * dt), p[page],
-                        st.o[dt]);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {  // dim 32 dt + 8 (k / 4) + 4 half + k % 4
+        const uint32_t x = *reinterpret_cast<const uint16_t*>(
+            col + 1024 * dt + 16 * (8 * (k >> 2) + (k & 3)));
+        if (see && (x & 0x7F80u) == 0x7F80u)
+          st.o[dt][k] += pt * __builtin_bit_cast(float, x << 16);
+      }
+  }
 }
 
 // NaN into the outputs of the (row, head) pairs [m0, m1) of KV head g of rows
@@ -879,8 +814,10 @@ __device__ void fill_nan(const RowsArgs& a, int row0, int64_t m0, int64_t m1, in
 }
 
 // One work item of one KV head: four waves of 32 (row, head) pairs each, over
-// K/V tiles of 64 tokens that they share through LDS, one tile on its way while
-// another is worked on.
+// K/V tiles of 32 tokens that they share through LDS, three tiles on their way
+// while one is worked on.  bf16 pages go from memory into their tile.  fp8 pages
+// go into a ring of their own (K and V of a tile 8 KiB); the lanes that loaded a
+// chunk widen it into one of two tiles a step before it is needed.
 template <bool FP8, bool TREE>
 struct Work {
   const RowsArgs& a;
@@ -889,93 +826,193 @@ struct Work {
   bool any;                  // the wave has rows
   float c;
   u32x4 q[8];
-  int64_t pos, pos_min, pos_max, last_pos;  // of the lane's row, the wave's first and last, the tile's last
+  // positions: the lane's row, the wave's first and last, the workgroup's first and last
+  int pos, pos_min, pos_max, tile_min, last_pos;
   uint64_t draft;            // drafted rows that the lane's row sees
   Walk walk;
   int left;                  // tiles of this part still to come
-  bool drafted;              // the drafted tokens have come, or are not this part's
+  int drafts;                // drafted tokens still to come
+  int ahead;                 // tiles whose loads are out and not yet waited for
   uint32_t koff, voff;
-  Staged sg;
+  int ka;
   State st;
-  int flag;
+  int flag, steps;
+  int* odd_step;             // LDS: the last step whose tile holds infinities or NaN
 
-  __device__ __forceinline__ bool next(Tile& t) {
-    if (left > 0 && walk_next(a, walk, last_pos, lane, t)) {
+  // The next tile and its pages (0 for one outside the pool); the page ids of the
+  // one behind it are sent for.
+  __device__ __forceinline__ Tile take(int (&pid)[2]) {
+    Tile t{0, 0, 0, false};
+    pid[0] = pid[1] = 0;
+    if (left > 0 && walk.r < walk.r_end) {
       if (left != INT32_MAX) --left;
-      return true;
-    }
-    left = 0;
-    if (!TREE || drafted) return false;
-    drafted = true;
-    t.draft = true;
-    t.tok0 = 0;
-    t.n = n_rows;
-    t.tb = 0;
+      const int tok0 = walk.j * kKeyTile;
+      t.pos0 = walk.tb + tok0;
+      t.left = walk.n - tok0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) t.pid[i] = 0;
-    return true;
+      for (int i = 0; i < 2; ++i) {
+        pid[i] = walk.pid[i];
+        if ((uint32_t)pid[i] >= (uint32_t)a.num_pages) {
+          pid[i] = 0;
+          if (kPage * i < t.left) t.bad |= 1 << i;
+        }
+      }
+      if (++walk.j < walk.tiles)
+        walk_ids(a, walk);
+      else
+        walk_on(a, walk, last_pos);
+    } else if (TREE && drafts > 0) {
+      t.draft = true;
+      t.pos0 = n_rows - drafts;
+      t.left = drafts;
+      drafts -= kKeyTile;
+    }
+    return t;
   }
 
-  // Tile t on its way into (lk, lv): bf16 pages at once, fp8 pages as far as
-  // registers; drafted tokens wait for `arrive`.
-  __device__ __forceinline__ void start(const Tile& t, char* lk, char* lv) {
-    if (TREE && t.draft) return;
-    if constexpr (FP8)
-      load_tile(a, t, g, wave, tid, sg);
+  // The loads of tile t into (lk, lv), for fp8 into the ring, and its scales.
+  __device__ __forceinline__ void start(const Tile& t, const int (&pid)[2], char* __restrict__ lk,
+                                        char* __restrict__ lv, float* __restrict__ ls) {
+    if (t.left == 0 || (TREE && t.draft)) return;
+    ++ahead;
+    const int H = a.num_kv_heads;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const size_t at = slice_of(pid[i], g, H, a.num_pages, a.head_major) * (kPage * kDim);
+      if constexpr (!FP8) {
+        to_lds(static_cast<const char*>(a.k_pool) + 2 * at + koff, lk + 4096 * i + 1024 * wave);
+        to_lds(static_cast<const char*>(a.v_pool) + 2 * at + voff, lv + 4096 * i + 1024 * wave);
+      } else if (i == wave >> 1) {  // two waves a page
+        to_lds(static_cast<const char*>(a.k_pool) + at + koff, lk + 1024 * wave);
+        to_lds(static_cast<const char*>(a.v_pool) + at + koff, lv + 1024 * wave);
+      }
+    }
+    if constexpr (FP8) {  // every wave a copy: K of both pages, then V
+      if (lane < 4)
+        to_lds4((lane & 2 ? a.v_scale : a.k_scale) + (size_t)(lane & 1 ? pid[1] : pid[0]) * H + g,
+                ls + 4 * wave);
+    }
+  }
+
+  // Waits for this wave's loads of the oldest tile that is on its way.
+  __device__ __forceinline__ void wait() {
+    constexpr int kVm0 = 0x0F70;    // s_waitcnt vmcnt(0)
+    constexpr int n = FP8 ? 3 : 4;  // loads of a wave per tile
+    --ahead;
+    if (ahead >= 2)
+      __builtin_amdgcn_s_waitcnt(kVm0 | 2 * n);
+    else if (ahead == 1)
+      __builtin_amdgcn_s_waitcnt(kVm0 | n);
     else
-      load_tile(a, t, g, wave, koff, voff, lk, lv);
-  }
-  __device__ __forceinline__ void arrive(const Tile& t, char* lk, char* lv, float* scales) {
-    if (TREE && t.draft)
-      stage_draft(a, row0, n_rows, g, tid, lk, lv, scales);
-    else if constexpr (FP8)
-      store_tile(sg, tid, lk, lv, scales);
+      __builtin_amdgcn_s_waitcnt(kVm0);
+    asm volatile("" ::: "memory");
   }
 
-  // Works on tile `cur` in (lk, lv, scales) while `nxt` comes into (nk, nv, ns);
-  // false if there is none.
-  __device__ __forceinline__ bool step(Tile& cur, const char* __restrict__ lk,
-                                       char* __restrict__ lv, const float* __restrict__ scales,
-                                       char* __restrict__ nk, char* __restrict__ nv,
-                                       float* __restrict__ ns) {
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's part of `cur` is in LDS
-    __syncthreads();
-    Tile nxt;
-    const bool more = next(nxt);
-    if (more) start(nxt, nk, nv);
-    if (cur.tok0 + kKeyTile > cur.n && !cur.draft) {
-      cut_tile(cur, tid, lv);
-      __syncthreads();
+  // fp8: the wave's own chunks from the ring into a tile.
+  __device__ __forceinline__ void widen_tile(const char* __restrict__ rk,
+                                             const char* __restrict__ rv, char* __restrict__ lk,
+                                             char* __restrict__ lv) {
+    const int t7 = tid & 127, page = tid >> 7, row = 16 * page + (t7 >> 3);
+    u32x4 lo, hi;
+    widen(*(reinterpret_cast<const u32x4*>(rk) + tid), lo, hi);
+    *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7))) = lo;
+    *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7) + 1)) = hi;
+    widen(*(reinterpret_cast<const u32x4*>(rv) + tid), lo, hi);
+    *reinterpret_cast<u32x4*>(lv + v_at(page, t7, 0)) = lo;
+    *reinterpret_cast<u32x4*>(lv + v_at(page, t7, 1)) = hi;
+  }
+
+  // Works on tile t in (lk, lv).
+  __device__ __forceinline__ void work(const Tile& t, const char* __restrict__ lk,
+                                       char* __restrict__ lv, const float* __restrict__ ls) {
+    ++steps;
+    const bool part = t.bad || t.draft || t.left < kKeyTile;
+    bool odd = false;
+    if (part || __builtin_elementwise_sub_sat(tile_min, t.pos0) < kKeyTile - 1) {
+      // some row of the workgroup does not see all of it
+      if (cut_tile(t.left, tid, lv)) *odd_step = steps;
+      lds_barrier();
+      odd = uniform(*odd_step) == steps;
+      if (t.bad) flag = KF_EFLAG_BAD_PAGE;
     }
-    const int64_t n_see = min(pos - cur.tb + 1, (int64_t)cur.n) - cur.tok0;
-    int bad = 0;
-    if (!cur.draft) {
+    const bool busy = any && (t.draft || pos_max >= t.pos0);
+    uint32_t sees = ~0u;
+    u32x4 p[2];
+    if (busy) {
+      const bool mask = part || __builtin_elementwise_sub_sat(pos_min, t.pos0) < kKeyTile - 1;
+      if (mask) {
+        const int e = min(__builtin_elementwise_sub_sat(pos, t.pos0), t.left - 1);
+        sees = e < 0 ? 0 : e >= 31 ? ~0u : (2u << e) - 1;
+        if (TREE && t.draft) sees = (uint32_t)(draft >> t.pos0);
+      }
+      f32x4 scales = {1.0f, 1.0f, 1.0f, 1.0f};
+      if (FP8 && !t.draft) scales = *reinterpret_cast<const f32x4*>(ls + 4 * wave);
+      weigh<FP8>(lk, scales, q, c, mask, sees, t.bad, ka, lane >> 5, st, p);
+      if (odd) add_odd(lv, sees, p, lane, st);
+    }
+    if (odd) {
+      lds_barrier();
+      tame_tile(tid, lv);
+      lds_barrier();
+    }
+    if (busy) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (cur.tok0 + 16 * i < cur.n && (cur.pid[i] < 0 || cur.pid[i] >= a.num_pages))
-          bad |= 1 << i;
-      if (bad) flag = KF_EFLAG_BAD_PAGE;
+      for (int page = 0; page < 2; ++page)
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+          st.o[dt] = mfma32(*reinterpret_cast<const u32x4*>(lv + 16 * lane + 4096 * page + 1024 * dt),
+                            p[page], st.o[dt]);
     }
-    if (any && pos_max - cur.tb >= cur.tok0) {
-      const bool mask = bad || cur.draft || cur.tok0 + kKeyTile > cur.n ||
-                        pos_min - cur.tb < cur.tok0 + kKeyTile - 1;
-      const uint64_t sees = cur.draft ? draft
-                            : n_see <= 0 ? 0
-                            : n_see >= 64 ? ~(uint64_t)0
-                                          : ((uint64_t)1 << n_see) - 1;
-      attend<FP8>(lk, lv, scales, q, c, mask, sees, bad, lane, st);
-    }
-    if (more) arrive(nxt, nk, nv, ns);
-    cur = nxt;
+  }
+
+  // bf16: tile t in (lk, lv), t1 behind it; the loads of t3 into (k3, v3).
+  __device__ __forceinline__ bool step(const Tile& t, const Tile& t1, Tile& t3,
+                                       const char* __restrict__ lk, char* __restrict__ lv,
+                                       char* __restrict__ k1, char* __restrict__ v1,
+                                       char* __restrict__ k3, char* __restrict__ v3) {
+    int pid[2];
+    t3 = take(pid);
+    if (!(TREE && t.draft)) wait();
+    lds_barrier();
+    start(t3, pid, k3, v3, nullptr);
+    work(t, lk, lv, nullptr);
+    if (TREE && t1.draft) stage_draft(a, row0, t1.pos0, n_rows, g, tid, k1, v1);
+    return t1.left > 0;
+  }
+
+  // fp8: tile t in (lk, lv); t1 is widened from (r1k, r1v) into (k1, v1), and the
+  // loads of t4 go into the ring's place of t (r0k, r0v); it then stands in t.
+  __device__ __forceinline__ bool step8(Tile& t, const Tile& t1, char* __restrict__ lk,
+                                        char* __restrict__ lv, char* __restrict__ k1,
+                                        char* __restrict__ v1, const char* __restrict__ r1k,
+                                        const char* __restrict__ r1v, char* __restrict__ r0k,
+                                        char* __restrict__ r0v, float* __restrict__ s0) {
+    int pid[2];
+    const Tile t4 = take(pid);
+    const bool more = t1.left > 0, pages = more && !(TREE && t1.draft);
+    if (pages) wait();
+    lds_barrier();  // (lk, lv) is whole, (k1, v1) free
+    work(t, lk, lv, s0);
+    if (TREE && t1.draft)
+      stage_draft(a, row0, t1.pos0, n_rows, g, tid, k1, v1);
+    else if (pages)
+      widen_tile(r1k, r1v, k1, v1);
+    start(t4, pid, r0k, r0v, s0);
+    t = t4;
     return more;
   }
 };
 
 template <bool FP8, bool TREE>
 __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
-  __shared__ __align__(16) char k0[kKeyTile * 256], v0[kKeyTile * 256];
-  __shared__ __align__(16) char k1[kKeyTile * 256], v1[kKeyTile * 256];
-  __shared__ __align__(16) float s0[8], s1[8];
+  // four tiles (bf16), or two tiles and a ring of four (fp8)
+  constexpr int kTile = kKeyTile * kDim * 2, kRing = FP8 ? kKeyTile * kDim : 16;
+  __shared__ __align__(16) char k0[kTile], v0[kTile], k1[kTile], v1[kTile];
+  __shared__ __align__(16) char k2[FP8 ? kRing : kTile], v2[FP8 ? kRing : kTile];
+  __shared__ __align__(16) char k3[FP8 ? kRing : kTile], v3[FP8 ? kRing : kTile];
+  __shared__ __align__(16) char k4[kRing], v4[kRing], k5[kRing], v5[kRing];
+  __shared__ __align__(16) float s0[16], s1[16], s2[16], s3[16];
+  __shared__ int odd_step;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
   const int H = a.num_kv_heads, G = a.group;
@@ -1017,17 +1054,22 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     if (c0 == 0.0f || !mine) x = u32x4{0, 0, 0, 0};  // a zero one makes all scores equal
     w.q[ks] = x;
   }
-  w.pos = w.pos_min = w.pos_max = w.last_pos = INT32_MAX;
+  w.pos = w.pos_min = w.pos_max = w.tile_min = w.last_pos = INT32_MAX;
   w.draft = 0;
   if constexpr (TREE) {
     w.draft = mine ? a.tree_mask[row0 + row] : 0;
     if (n_rows < 64) w.draft &= ((uint64_t)1 << n_rows) - 1;
   } else {
+    // no token lies behind INT32_MAX
     const int64_t p0 = a.first_pos[b];
-    w.pos = p0 + row;
-    w.pos_min = p0 + min(m0 + 32 * wave, m1 - 1) / G;
-    w.pos_max = p0 + (min(m1, m0 + 32 * wave + 32) - 1) / G;
-    w.last_pos = p0 + (m1 - 1) / G;
+    auto at = [&](int64_t pair) {
+      return (int)min(p0 + min(pair, m1 - 1) / G, (int64_t)INT32_MAX);
+    };
+    w.pos = at(m);
+    w.pos_min = uniform(at(m0 + 32 * wave));
+    w.pos_max = uniform(at(m0 + 32 * wave + 31));
+    w.tile_min = uniform(at(m0));
+    w.last_pos = uniform(at(m1 - 1));
   }
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
@@ -1035,19 +1077,57 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     for (int i = 0; i < 16; ++i) w.st.o[dt][i] = 0.0f;
   w.st.m = neg_inf();
   w.st.l = 0.0f;
-  w.flag = 0;
+  w.flag = w.steps = w.ahead = 0;
+  w.odd_step = &odd_step;
+  if (tid == 0) odd_step = 0;
   const int krow = 4 * wave + (lane >> 4);  // of a page
-  w.koff = 256 * krow + 16 * ((lane & 15) ^ krow);
+  w.koff = FP8 ? 1024 * (wave & 1) + 16 * lane : 256 * krow + 16 * ((lane & 15) ^ krow);
   w.voff = 1024 * wave + 32 * l32 + 16 * half;
+  w.ka = k_at(16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3), half);
   walk_to(a, w.walk, a.seq_route_begin[b], a.seq_route_begin[b + 1], w.last_pos, it.key0, lane);
   w.left = it.key1 == INT32_MAX ? INT32_MAX : it.key1 - it.key0;
-  w.drafted = it.key1 != INT32_MAX;
+  w.drafts = TREE && it.key1 == INT32_MAX ? n_rows : 0;
 
-  Tile cur;
-  if (w.next(cur)) {
-    w.start(cur, k0, v0);
-    w.arrive(cur, k0, v0, s0);
-    while (w.step(cur, k0, v0, s0, k1, v1, s1) && w.step(cur, k1, v1, s1, k0, v0, s0)) {
+  Tile t0, t1, t2, t3;
+  int pid[2];
+  if constexpr (!FP8) {
+    t0 = w.take(pid);
+    w.start(t0, pid, k0, v0, nullptr);
+    t1 = w.take(pid);
+    w.start(t1, pid, k1, v1, nullptr);
+    t2 = w.take(pid);
+    w.start(t2, pid, k2, v2, nullptr);
+    if (t0.left > 0) {
+      if (TREE && t0.draft) stage_draft(a, row0, t0.pos0, n_rows, g, tid, k0, v0);
+      while (w.step(t0, t1, t3, k0, v0, k1, v1, k3, v3) &&
+             w.step(t1, t2, t0, k1, v1, k2, v2, k0, v0) &&
+             w.step(t2, t3, t1, k2, v2, k3, v3, k1, v1) &&
+             w.step(t3, t0, t2, k3, v3, k0, v0, k2, v2)) {
+      }
+    }
+  } else {
+    t0 = w.take(pid);
+    w.start(t0, pid, k2, v2, s0);
+    t1 = w.take(pid);
+    w.start(t1, pid, k3, v3, s1);
+    t2 = w.take(pid);
+    w.start(t2, pid, k4, v4, s2);
+    t3 = w.take(pid);
+    w.start(t3, pid, k5, v5, s3);
+    if (t0.left > 0) {
+      if (TREE && t0.draft) {
+        stage_draft(a, row0, t0.pos0, n_rows, g, tid, k0, v0);
+      } else {
+        --w.ahead;
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+        asm volatile("" ::: "memory");
+        w.widen_tile(k2, v2, k0, v0);
+      }
+      while (w.step8(t0, t1, k0, v0, k1, v1, k3, v3, k2, v2, s0) &&
+             w.step8(t1, t2, k1, v1, k0, v0, k4, v4, k3, v3, s1) &&
+             w.step8(t2, t3, k0, v0, k1, v1, k5, v5, k4, v4, s2) &&
+             w.step8(t3, t0, k1, v1, k0, v0, k2, v2, k5, v5, s3)) {
+      }
     }
   }
   if (w.flag && tid == 0) atomicOr(a.err_flags, w.flag);
