@@ -525,6 +525,7 @@ struct Walk {
 struct Tile {
   int pos0, left, bad;
   bool draft;
+  int pid[2];  // (0 for one outside the pool)
 };
 
 __device__ __forceinline__ int visible(int begin, int end, int last_pos) {
@@ -676,22 +677,31 @@ __device__ __forceinline__ void tame_tile(int tid, char* lv) {
   }
 }
 
-// The drafted tokens t0 .. of a sequence as a tile: V is turned around on its way.
-__device__ __forceinline__ void stage_draft(const RowsArgs& a, int row0, int t0, int n, int g,
-                                            int tid, char* lk, char* lv) {
+// The drafted tokens t0 .. of a sequence as a tile of K, and of V, which is turned
+// around on its way.
+__device__ __forceinline__ u32x4 draft_chunk(const RowsArgs& a, const uint16_t* x, int row0,
+                                             int row, int n, int g, int c) {
+  return row < n ? ld16(x + (size_t)(row0 + row) * a.kv_stride + (size_t)g * kDim + 8 * c)
+                 : u32x4{0, 0, 0, 0};
+}
+__device__ __forceinline__ void draft_k(const RowsArgs& a, int row0, int t0, int n, int g, int tid,
+                                        char* lk) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int row = 16 * i + (tid >> 4), c = tid & 15;
-    u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-    if (t0 + row < n) {
-      const size_t at = (size_t)(row0 + t0 + row) * a.kv_stride + (size_t)g * kDim + 8 * c;
-      k = ld16(a.k_draft + at);
-      v = ld16(a.v_draft + at);
-    }
-    *reinterpret_cast<u32x4*>(lk + k_at(row, c)) = k;
+    *reinterpret_cast<u32x4*>(lk + k_at(row, c)) =
+        draft_chunk(a, a.k_draft, row0, t0 + row, n, g, c);
+  }
+}
+__device__ __forceinline__ void draft_v(const RowsArgs& a, int row0, int t0, int n, int g, int tid,
+                                        char* lv) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int slot = tid >> 4, c = tid & 15;
+    const u32x4 v = draft_chunk(a, a.v_draft, row0, t0 + 16 * i + slot, n, g, c);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      *reinterpret_cast<uint16_t*>(lv + v_at(i, 8 * c + e, (row & 15) >> 3) + 2 * (row & 7)) =
+      *reinterpret_cast<uint16_t*>(lv + v_at(i, 8 * c + e, slot >> 3) + 2 * (slot & 7)) =
           (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
   }
 }
@@ -704,73 +714,21 @@ struct State {
   float m, l;
 };
 
-// A tile's scores and weights p.  S^T = K Q^T: matrix row 8 i + 4 half + j of 32
-// is token 16 (i / 2) + 8 half + 4 (i % 2) + j, so that a lane's 16 results are
-// the 8 slots 8 half .. of two pages: just the p that the lane feeds to
-// O^T += V^T P^T, whose depth of 16 is one page.  No value crosses lanes between
-// the products.  mask: not every row sees every token; sees: the tokens of this
-// lane's row; bad: pages outside the pool; scales: K and V scales of the pages
-// (fp8).
-template <bool FP8>
-__device__ __forceinline__ void weigh(const char* lk, f32x4 scales, const u32x4 (&q)[8], float c,
-                                      bool mask, uint32_t sees, int bad, int ka, int half,
-                                      State& st, u32x4 (&p)[2]) {
+// A tile's scores, S^T = K Q^T: matrix row 8 i + 4 half + j of 32 is token
+// 16 (i / 2) + 8 half + 4 (i % 2) + j, so that a lane's 16 results are the 8 slots
+// 8 half .. of two pages: just the p that the lane feeds to O^T += V^T P^T, whose
+// depth of 16 is one page.  No value crosses lanes between the products.
+__device__ __forceinline__ f32x16 scores(const u32x4 (&k)[8], const u32x4 (&q)[8]) {
   f32x16 s;
 #pragma unroll
   for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
-    s = mfma32(*reinterpret_cast<const u32x4*>(lk + (ka ^ (32 * k))), q[k], s);
-  if constexpr (FP8) {  // the page's scale into the scores, in base 2
+  for (int i = 0; i < 8; ++i) s = mfma32(k[i], q[i], s);
+  return s;
+}
+__device__ __forceinline__ void load_k(const char* lk, int ka, u32x4 (&k)[8]) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] *= c * scales[i >> 3];
-  }
-  const uint32_t mine = sees >> (8 * half);
-  if (mask) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (bad >> (i >> 3) & 1) s[i] = qnan();
-      if (!(mine >> (16 * (i >> 3) + (i & 7)) & 1)) s[i] = neg_inf();
-    }
-  }
-  float top = neg_inf();
-#pragma unroll
-  for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
-  top = max_halves(top);
-  if constexpr (!FP8) top *= c;
-  // The reference moves only when a score exceeds it by 2^8: exp2 and the sums
-  // stay in range, and most tiles leave the outputs unscaled.
-  if (__ballot(top > st.m + 8.0f)) {
-    const float m = fmaxf(st.m, top);
-    const float f = m == neg_inf() ? 1.0f : exp2_fast(st.m - m);
-    st.m = m;
-    st.l *= f;
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) st.o[dt][i] *= f;
-  }
-  const float m = st.m == neg_inf() ? 0.0f : st.m;
-#pragma unroll
-  for (int page = 0; page < 2; ++page)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float x0 = s[8 * page + 2 * i], x1 = s[8 * page + 2 * i + 1];
-      const float e0 = FP8 ? exp2_fast(x0 - m) : exp2_fast(__builtin_fmaf(x0, c, -m));
-      const float e1 = FP8 ? exp2_fast(x1 - m) : exp2_fast(__builtin_fmaf(x1, c, -m));
-      st.l += e0 + e1;
-      p[page][i] = FP8 ? pack_bf16(e0 * scales[2 + page], e1 * scales[2 + page])
-                       : pack_bf16(e0, e1);
-    }
-  if (FP8 && mask) {  // a hidden token weighs nothing, whatever its page's scale
-#pragma unroll
-    for (int page = 0; page < 2; ++page)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t two = mine >> (16 * page + 2 * i) & 3u;
-        p[page][i] &= (two & 1 ? 0x0000FFFFu : 0u) | (two & 2 ? 0xFFFF0000u : 0u);
-      }
-  }
+  for (int i = 0; i < 8; ++i) k[i] = *reinterpret_cast<const u32x4*>(lk + (ka ^ (32 * i)));
 }
 
 // Infinities and NaN of a V tile into the outputs of the rows that see them (a
@@ -792,6 +750,7 @@ __device__ __forceinline__ void add_odd(const char* lv, uint32_t sees, const u32
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
       for (int k = 0; k < 16; ++k) {  // dim 32 dt + 8 (k / 4) + 4 half + k % 4
+        if (k % 4 == 0) asm volatile("" ::: "memory");  // few loads at a time: registers
         const uint32_t x = *reinterpret_cast<const uint16_t*>(
             col + 1024 * dt + 16 * (8 * (k >> 2) + (k & 3)));
         if (see && (x & 0x7F80u) == 0x7F80u)
@@ -802,7 +761,7 @@ __device__ __forceinline__ void add_odd(const char* lv, uint32_t sees, const u32
 
 // NaN into the outputs of the (row, head) pairs [m0, m1) of KV head g of rows
 // row0 ...
-__device__ void fill_nan(const RowsArgs& a, int row0, int64_t m0, int64_t m1, int g, int tid,
+__device__ __forceinline__ void fill_nan(const RowsArgs& a, int row0, int64_t m0, int64_t m1, int g, int tid,
                          int nt) {
   const int G = a.group;
   for (int64_t x = m0 * 16 + tid; x < m1 * 16; x += nt) {
@@ -815,9 +774,11 @@ __device__ void fill_nan(const RowsArgs& a, int row0, int64_t m0, int64_t m1, in
 
 // One work item of one KV head: four waves of 32 (row, head) pairs each, over
 // K/V tiles of 32 tokens that they share through LDS, three tiles on their way
-// while one is worked on.  bf16 pages go from memory into their tile.  fp8 pages
-// go into a ring of their own (K and V of a tile 8 KiB); the lanes that loaded a
-// chunk widen it into one of two tiles a step before it is needed.
+// while one is worked on.  The scores of a tile are computed a step before its
+// weights, beside the weights of the tile before it: the matrix cores take the
+// one while the vector units take the other.  bf16 pages go from memory into
+// their tile.  fp8 pages go into rings of their own (4 KiB); the lanes that loaded
+// a chunk widen it into one of two tiles a step before it is needed.
 template <bool FP8, bool TREE>
 struct Work {
   const RowsArgs& a;
@@ -826,24 +787,22 @@ struct Work {
   bool any;                  // the wave has rows
   float c;
   u32x4 q[8];
-  // positions: the lane's row, the wave's first and last, the workgroup's first and last
-  int pos, pos_min, pos_max, tile_min, last_pos;
+  // positions: the lane's row, the wave's and the workgroup's first, the workgroup's last
+  int pos, pos_min, tile_min, last_pos;
   uint64_t draft;            // drafted rows that the lane's row sees
   Walk walk;
   int left;                  // tiles of this part still to come
   int drafts;                // drafted tokens still to come
-  int ahead;                 // tiles whose loads are out and not yet waited for
   uint32_t koff, voff;
   int ka;
+  f32x16 s;                  // scores of the next tile
   State st;
   int flag, steps;
   int* odd_step;             // LDS: the last step whose tile holds infinities or NaN
 
-  // The next tile and its pages (0 for one outside the pool); the page ids of the
-  // one behind it are sent for.
-  __device__ __forceinline__ Tile take(int (&pid)[2]) {
-    Tile t{0, 0, 0, false};
-    pid[0] = pid[1] = 0;
+  // The next tile; the page ids of the one behind it are sent for.
+  __device__ __forceinline__ Tile take() {
+    Tile t{0, 0, 0, false, {0, 0}};
     if (left > 0 && walk.r < walk.r_end) {
       if (left != INT32_MAX) --left;
       const int tok0 = walk.j * kKeyTile;
@@ -851,9 +810,9 @@ struct Work {
       t.left = walk.n - tok0;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        pid[i] = walk.pid[i];
-        if ((uint32_t)pid[i] >= (uint32_t)a.num_pages) {
-          pid[i] = 0;
+        t.pid[i] = walk.pid[i];
+        if ((uint32_t)t.pid[i] >= (uint32_t)a.num_pages) {
+          t.pid[i] = 0;
           if (kPage * i < t.left) t.bad |= 1 << i;
         }
       }
@@ -870,59 +829,62 @@ struct Work {
     return t;
   }
 
-  // The loads of tile t into (lk, lv), for fp8 into the ring, and its scales.
-  __device__ __forceinline__ void start(const Tile& t, const int (&pid)[2], char* __restrict__ lk,
-                                        char* __restrict__ lv, float* __restrict__ ls) {
-    if (t.left == 0 || (TREE && t.draft)) return;
-    ++ahead;
-    const int H = a.num_kv_heads;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const size_t at = slice_of(pid[i], g, H, a.num_pages, a.head_major) * (kPage * kDim);
-      if constexpr (!FP8) {
-        to_lds(static_cast<const char*>(a.k_pool) + 2 * at + koff, lk + 4096 * i + 1024 * wave);
-        to_lds(static_cast<const char*>(a.v_pool) + 2 * at + voff, lv + 4096 * i + 1024 * wave);
-      } else if (i == wave >> 1) {  // two waves a page
-        to_lds(static_cast<const char*>(a.k_pool) + at + koff, lk + 1024 * wave);
-        to_lds(static_cast<const char*>(a.v_pool) + at + koff, lv + 1024 * wave);
-      }
-    }
-    if constexpr (FP8) {  // every wave a copy: K of both pages, then V
-      if (lane < 4)
-        to_lds4((lane & 2 ? a.v_scale : a.k_scale) + (size_t)(lane & 1 ? pid[1] : pid[0]) * H + g,
-                ls + 4 * wave);
-    }
+  __device__ __forceinline__ bool paged(const Tile& t) const {
+    return t.left > 0 && !(TREE && t.draft);
   }
 
-  // Waits for this wave's loads of the oldest tile that is on its way.
+  // The loads of one operand of tile t into l, for fp8 into its ring.
+  __device__ __forceinline__ void start(const Tile& t, const void* pool, uint32_t off,
+                                        char* __restrict__ l) {
+    if (!paged(t)) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const size_t at =
+          slice_of(t.pid[i], g, a.num_kv_heads, a.num_pages, a.head_major) * (kPage * kDim);
+      if constexpr (!FP8)
+        to_lds(static_cast<const char*>(pool) + 2 * at + off, l + 4096 * i + 1024 * wave);
+      else if (i == wave >> 1)  // two waves a page
+        to_lds(static_cast<const char*>(pool) + at + off, l + 1024 * wave);
+    }
+  }
+  // fp8: the scales of tile t, every wave a copy: K of both pages, then V.
+  __device__ __forceinline__ void start_scales(const Tile& t, float* __restrict__ ls) {
+    if (paged(t) && lane < 4)
+      to_lds4((lane & 2 ? a.v_scale : a.k_scale) +
+                  (size_t)(lane & 1 ? t.pid[1] : t.pid[0]) * a.num_kv_heads + g,
+              ls + 4 * wave);
+  }
+
+  // Waits until at most n loads of this wave are out.
+  template <int n>
   __device__ __forceinline__ void wait() {
-    constexpr int kVm0 = 0x0F70;    // s_waitcnt vmcnt(0)
-    constexpr int n = FP8 ? 3 : 4;  // loads of a wave per tile
-    --ahead;
-    if (ahead >= 2)
-      __builtin_amdgcn_s_waitcnt(kVm0 | 2 * n);
-    else if (ahead == 1)
-      __builtin_amdgcn_s_waitcnt(kVm0 | n);
-    else
-      __builtin_amdgcn_s_waitcnt(kVm0);
+    __builtin_amdgcn_s_waitcnt(0x0F70 | n);  // vmcnt(n)
     asm volatile("" ::: "memory");
   }
 
   // fp8: the wave's own chunks from the ring into a tile.
-  __device__ __forceinline__ void widen_tile(const char* __restrict__ rk,
-                                             const char* __restrict__ rv, char* __restrict__ lk,
-                                             char* __restrict__ lv) {
-    const int t7 = tid & 127, page = tid >> 7, row = 16 * page + (t7 >> 3);
+  __device__ __forceinline__ void widen_k(const char* __restrict__ ring, char* __restrict__ lk) {
+    const int t7 = tid & 127, row = 16 * (tid >> 7) + (t7 >> 3);
     u32x4 lo, hi;
-    widen(*(reinterpret_cast<const u32x4*>(rk) + tid), lo, hi);
+    widen(*(reinterpret_cast<const u32x4*>(ring) + tid), lo, hi);
     *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7))) = lo;
     *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7) + 1)) = hi;
-    widen(*(reinterpret_cast<const u32x4*>(rv) + tid), lo, hi);
-    *reinterpret_cast<u32x4*>(lv + v_at(page, t7, 0)) = lo;
-    *reinterpret_cast<u32x4*>(lv + v_at(page, t7, 1)) = hi;
+  }
+  __device__ __forceinline__ void widen_v(const char* __restrict__ ring, char* __restrict__ lv) {
+    u32x4 lo, hi;
+    widen(*(reinterpret_cast<const u32x4*>(ring) + tid), lo, hi);
+    *reinterpret_cast<u32x4*>(lv + v_at(tid >> 7, tid & 127, 0)) = lo;
+    *reinterpret_cast<u32x4*>(lv + v_at(tid >> 7, tid & 127, 1)) = hi;
   }
 
-  // Works on tile t in (lk, lv).
+  __device__ __forceinline__ void first_scores(const char* __restrict__ lk) {
+    u32x4 k[8];
+    load_k(lk, ka, k);
+    s = scores(k, q);
+  }
+
+  // Works on tile t, whose scores are in s and whose V is in lv; the next tile's
+  // K is in lk.
   __device__ __forceinline__ void work(const Tile& t, const char* __restrict__ lk,
                                        char* __restrict__ lv, const float* __restrict__ ls) {
     ++steps;
@@ -935,77 +897,158 @@ struct Work {
       odd = uniform(*odd_step) == steps;
       if (t.bad) flag = KF_EFLAG_BAD_PAGE;
     }
-    const bool busy = any && (t.draft || pos_max >= t.pos0);
-    uint32_t sees = ~0u;
-    u32x4 p[2];
-    if (busy) {
-      const bool mask = part || __builtin_elementwise_sub_sat(pos_min, t.pos0) < kKeyTile - 1;
-      if (mask) {
-        const int e = min(__builtin_elementwise_sub_sat(pos, t.pos0), t.left - 1);
-        sees = e < 0 ? 0 : e >= 31 ? ~0u : (2u << e) - 1;
-        if (TREE && t.draft) sees = (uint32_t)(draft >> t.pos0);
+    if (!any) {
+      if (odd) {
+        lds_barrier();
+        tame_tile(tid, lv);
+        lds_barrier();
       }
-      f32x4 scales = {1.0f, 1.0f, 1.0f, 1.0f};
-      if (FP8 && !t.draft) scales = *reinterpret_cast<const f32x4*>(ls + 4 * wave);
-      weigh<FP8>(lk, scales, q, c, mask, sees, t.bad, ka, lane >> 5, st, p);
-      if (odd) add_odd(lv, sees, p, lane, st);
+      return;
+    }
+    f32x4 scales = {1.0f, 1.0f, 1.0f, 1.0f};
+    if constexpr (FP8) {  // the pages' scales into the scores, in base 2
+      if (!t.draft) scales = *reinterpret_cast<const f32x4*>(ls + 4 * wave);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] *= c * scales[i >> 3];
+    }
+    const int half = lane >> 5;
+    uint32_t sees = ~0u;
+    const bool mask = part || __builtin_elementwise_sub_sat(pos_min, t.pos0) < kKeyTile - 1;
+    if (mask) {
+      const int e = min(__builtin_elementwise_sub_sat(pos, t.pos0), t.left - 1);
+      sees = e < 0 ? 0 : e >= 31 ? ~0u : (2u << e) - 1;
+      if (TREE && t.draft) sees = (uint32_t)(draft >> t.pos0);
+      const uint32_t mine = sees >> (8 * half);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if (t.bad >> (i >> 3) & 1) s[i] = qnan();
+        if (!(mine >> (16 * (i >> 3) + (i & 7)) & 1)) s[i] = neg_inf();
+      }
+    }
+    u32x4 k[8];
+    load_k(lk, ka, k);
+    float top = neg_inf();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
+    top = max_halves(top);
+    if constexpr (!FP8) top *= c;
+    // The reference moves only when a score exceeds it by 2^8: exp2 and the sums
+    // stay in range, and most tiles leave the outputs unscaled.
+    if (__ballot(top > st.m + 8.0f)) {
+      const float m = fmaxf(st.m, top);
+      const float f = m == neg_inf() ? 1.0f : exp2_fast(st.m - m);
+      st.m = m;
+      st.l *= f;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st.o[dt][i] *= f;
+    }
+    const float m = st.m == neg_inf() ? 0.0f : st.m;
+    u32x4 p[2];
+    const f32x16 next = scores(k, q);
+#pragma unroll
+    for (int page = 0; page < 2; ++page)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x0 = s[8 * page + 2 * i], x1 = s[8 * page + 2 * i + 1];
+        const float e0 = FP8 ? exp2_fast(x0 - m) : exp2_fast(__builtin_fmaf(x0, c, -m));
+        const float e1 = FP8 ? exp2_fast(x1 - m) : exp2_fast(__builtin_fmaf(x1, c, -m));
+        st.l += e0 + e1;
+        p[page][i] = FP8 ? pack_bf16(e0 * scales[2 + page], e1 * scales[2 + page])
+                         : pack_bf16(e0, e1);
+      }
+    s = next;
+    if (mask) {
+      if constexpr (FP8) {  // a hidden token weighs nothing, whatever its page's scale
+        const uint32_t mine = sees >> (8 * half);
+#pragma unroll
+        for (int page = 0; page < 2; ++page)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t two = mine >> (16 * page + 2 * i) & 3u;
+            p[page][i] &= (two & 1 ? 0x0000FFFFu : 0u) | (two & 2 ? 0xFFFF0000u : 0u);
+          }
+      }
     }
     if (odd) {
+      add_odd(lv, sees, p, lane, st);
       lds_barrier();
       tame_tile(tid, lv);
       lds_barrier();
     }
-    if (busy) {
 #pragma unroll
-      for (int page = 0; page < 2; ++page)
+    for (int page = 0; page < 2; ++page)
 #pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-          st.o[dt] = mfma32(*reinterpret_cast<const u32x4*>(lv + 16 * lane + 4096 * page + 1024 * dt),
-                            p[page], st.o[dt]);
-    }
+      for (int dt = 0; dt < 4; ++dt)
+        st.o[dt] = mfma32(*reinterpret_cast<const u32x4*>(lv + 16 * lane + 4096 * page + 1024 * dt),
+                          p[page], st.o[dt]);
   }
 
-  // bf16: tile t in (lk, lv), t1 behind it; the loads of t3 into (k3, v3).
-  __device__ __forceinline__ bool step(const Tile& t, const Tile& t1, Tile& t3,
+  // bf16: tile t, whose place t4 takes, V in lv; the next tile's K in lk.  The
+  // loads of t4's K go into k0, where t's was, those of t3's V into v3; drafted
+  // tokens are written a step before they are needed (k2, v1).
+  __device__ __forceinline__ bool step(Tile& t, const Tile& t1, const Tile& t2, const Tile& t3,
                                        const char* __restrict__ lk, char* __restrict__ lv,
-                                       char* __restrict__ k1, char* __restrict__ v1,
-                                       char* __restrict__ k3, char* __restrict__ v3) {
-    int pid[2];
-    t3 = take(pid);
-    if (!(TREE && t.draft)) wait();
+                                       char* __restrict__ k0, char* __restrict__ v3,
+                                       char* __restrict__ k2, char* __restrict__ v1) {
+    const Tile t4 = take();
+    // in order: V of t1, K of t2, V of t2, K of t3 may still be out
+    if (paged(t3))
+      wait<8>();
+    else if (paged(t2))
+      wait<6>();
+    else if (paged(t1))
+      wait<2>();
+    else
+      wait<0>();
     lds_barrier();
-    start(t3, pid, k3, v3, nullptr);
+    start(t3, a.v_pool, voff, v3);
+    start(t4, a.k_pool, koff, k0);
     work(t, lk, lv, nullptr);
-    if (TREE && t1.draft) stage_draft(a, row0, t1.pos0, n_rows, g, tid, k1, v1);
+    if (TREE && t2.draft) draft_k(a, row0, t2.pos0, n_rows, g, tid, k2);
+    if (TREE && t1.draft) draft_v(a, row0, t1.pos0, n_rows, g, tid, v1);
+    t = t4;
     return t1.left > 0;
   }
 
-  // fp8: tile t in (lk, lv); t1 is widened from (r1k, r1v) into (k1, v1), and the
-  // loads of t4 go into the ring's place of t (r0k, r0v); it then stands in t.
-  __device__ __forceinline__ bool step8(Tile& t, const Tile& t1, char* __restrict__ lk,
-                                        char* __restrict__ lv, char* __restrict__ k1,
-                                        char* __restrict__ v1, const char* __restrict__ r1k,
-                                        const char* __restrict__ r1v, char* __restrict__ r0k,
-                                        char* __restrict__ r0v, float* __restrict__ s0) {
-    int pid[2];
-    const Tile t4 = take(pid);
-    const bool more = t1.left > 0, pages = more && !(TREE && t1.draft);
-    if (pages) wait();
-    lds_barrier();  // (lk, lv) is whole, (k1, v1) free
+  // fp8: tile t, whose place t4 takes, V in lv; the next tile's K in lk.  t2's K is
+  // widened into k2, t1's V into v1, from their rings; the loads of t4 go into the
+  // rings' places of t.
+  __device__ __forceinline__ bool step8(Tile& t, const Tile& t1, const Tile& t2, const Tile& t3,
+                                        const char* __restrict__ lk, char* __restrict__ lv,
+                                        char* __restrict__ k2, char* __restrict__ v1,
+                                        const char* __restrict__ rk2, const char* __restrict__ rv1,
+                                        char* __restrict__ rk0, char* __restrict__ rv0,
+                                        float* __restrict__ s0) {
+    const Tile t4 = take();
+    lds_barrier();
     work(t, lk, lv, s0);
+    start(t4, a.k_pool, koff, rk0);
+    start(t4, a.v_pool, koff, rv0);
+    start_scales(t4, s0);
+    if (paged(t4))
+      wait<6>();
+    else if (paged(t3))
+      wait<3>();
+    else
+      wait<0>();
+    if (TREE && t2.draft)
+      draft_k(a, row0, t2.pos0, n_rows, g, tid, k2);
+    else if (t2.left > 0)
+      widen_k(rk2, k2);
     if (TREE && t1.draft)
-      stage_draft(a, row0, t1.pos0, n_rows, g, tid, k1, v1);
-    else if (pages)
-      widen_tile(r1k, r1v, k1, v1);
-    start(t4, pid, r0k, r0v, s0);
+      draft_v(a, row0, t1.pos0, n_rows, g, tid, v1);
+    else if (t1.left > 0)
+      widen_v(rv1, v1);
     t = t4;
-    return more;
+    return t1.left > 0;
   }
 };
 
 template <bool FP8, bool TREE>
 __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
-  // four tiles (bf16), or two tiles and a ring of four (fp8)
+  // K and V: four tiles each (bf16), or two tiles and a ring of four (fp8)
   constexpr int kTile = kKeyTile * kDim * 2, kRing = FP8 ? kKeyTile * kDim : 16;
   __shared__ __align__(16) char k0[kTile], v0[kTile], k1[kTile], v1[kTile];
   __shared__ __align__(16) char k2[FP8 ? kRing : kTile], v2[FP8 ? kRing : kTile];
@@ -1054,7 +1097,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     if (c0 == 0.0f || !mine) x = u32x4{0, 0, 0, 0};  // a zero one makes all scores equal
     w.q[ks] = x;
   }
-  w.pos = w.pos_min = w.pos_max = w.tile_min = w.last_pos = INT32_MAX;
+  w.pos = w.pos_min = w.tile_min = w.last_pos = INT32_MAX;
   w.draft = 0;
   if constexpr (TREE) {
     w.draft = mine ? a.tree_mask[row0 + row] : 0;
@@ -1067,7 +1110,6 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     };
     w.pos = at(m);
     w.pos_min = uniform(at(m0 + 32 * wave));
-    w.pos_max = uniform(at(m0 + 32 * wave + 31));
     w.tile_min = uniform(at(m0));
     w.last_pos = uniform(at(m1 - 1));
   }
@@ -1077,7 +1119,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     for (int i = 0; i < 16; ++i) w.st.o[dt][i] = 0.0f;
   w.st.m = neg_inf();
   w.st.l = 0.0f;
-  w.flag = w.steps = w.ahead = 0;
+  w.flag = w.steps = 0;
   w.odd_step = &odd_step;
   if (tid == 0) odd_step = 0;
   const int krow = 4 * wave + (lane >> 4);  // of a page
@@ -1088,45 +1130,65 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   w.left = it.key1 == INT32_MAX ? INT32_MAX : it.key1 - it.key0;
   w.drafts = TREE && it.key1 == INT32_MAX ? n_rows : 0;
 
-  Tile t0, t1, t2, t3;
-  int pid[2];
+  Tile t0 = w.take(), t1 = w.take(), t2 = w.take(), t3 = w.take();
   if constexpr (!FP8) {
-    t0 = w.take(pid);
-    w.start(t0, pid, k0, v0, nullptr);
-    t1 = w.take(pid);
-    w.start(t1, pid, k1, v1, nullptr);
-    t2 = w.take(pid);
-    w.start(t2, pid, k2, v2, nullptr);
+    w.start(t0, a.k_pool, w.koff, k0);
+    w.start(t0, a.v_pool, w.voff, v0);
+    w.start(t1, a.k_pool, w.koff, k1);
+    w.start(t1, a.v_pool, w.voff, v1);
+    w.start(t2, a.k_pool, w.koff, k2);
+    w.start(t2, a.v_pool, w.voff, v2);
+    w.start(t3, a.k_pool, w.koff, k3);
     if (t0.left > 0) {
-      if (TREE && t0.draft) stage_draft(a, row0, t0.pos0, n_rows, g, tid, k0, v0);
-      while (w.step(t0, t1, t3, k0, v0, k1, v1, k3, v3) &&
-             w.step(t1, t2, t0, k1, v1, k2, v2, k0, v0) &&
-             w.step(t2, t3, t1, k2, v2, k3, v3, k1, v1) &&
-             w.step(t3, t0, t2, k3, v3, k0, v0, k2, v2)) {
+      if (w.paged(t3))
+        w.template wait<12>();
+      else
+        w.template wait<0>();
+      if (TREE && t0.draft) {
+        draft_k(a, row0, t0.pos0, n_rows, g, tid, k0);
+        draft_v(a, row0, t0.pos0, n_rows, g, tid, v0);
+      }
+      if (TREE && t1.draft) draft_k(a, row0, t1.pos0, n_rows, g, tid, k1);
+      lds_barrier();
+      w.first_scores(k0);
+      while (w.step(t0, t1, t2, t3, k1, v0, k0, v3, k2, v1) &&
+             w.step(t1, t2, t3, t0, k2, v1, k1, v0, k3, v2) &&
+             w.step(t2, t3, t0, t1, k3, v2, k2, v1, k0, v3) &&
+             w.step(t3, t0, t1, t2, k0, v3, k3, v2, k1, v0)) {
       }
     }
   } else {
-    t0 = w.take(pid);
-    w.start(t0, pid, k2, v2, s0);
-    t1 = w.take(pid);
-    w.start(t1, pid, k3, v3, s1);
-    t2 = w.take(pid);
-    w.start(t2, pid, k4, v4, s2);
-    t3 = w.take(pid);
-    w.start(t3, pid, k5, v5, s3);
+    auto start = [&](const Tile& t, char* rk, char* rv, float* ls) {
+      w.start(t, a.k_pool, w.koff, rk);
+      w.start(t, a.v_pool, w.koff, rv);
+      w.start_scales(t, ls);
+    };
+    start(t0, k2, v2, s0);
+    start(t1, k3, v3, s1);
+    start(t2, k4, v4, s2);
+    start(t3, k5, v5, s3);
     if (t0.left > 0) {
+      if (w.paged(t3))
+        w.template wait<6>();
+      else
+        w.template wait<0>();
       if (TREE && t0.draft) {
-        stage_draft(a, row0, t0.pos0, n_rows, g, tid, k0, v0);
+        draft_k(a, row0, t0.pos0, n_rows, g, tid, k0);
+        draft_v(a, row0, t0.pos0, n_rows, g, tid, v0);
       } else {
-        --w.ahead;
-        __builtin_amdgcn_s_waitcnt(0x0F70);
-        asm volatile("" ::: "memory");
-        w.widen_tile(k2, v2, k0, v0);
+        w.widen_k(k2, k0);
+        w.widen_v(v2, v0);
       }
-      while (w.step8(t0, t1, k0, v0, k1, v1, k3, v3, k2, v2, s0) &&
-             w.step8(t1, t2, k1, v1, k0, v0, k4, v4, k3, v3, s1) &&
-             w.step8(t2, t3, k0, v0, k1, v1, k5, v5, k4, v4, s2) &&
-             w.step8(t3, t0, k1, v1, k0, v0, k2, v2, k5, v5, s3)) {
+      if (TREE && t1.draft)
+        draft_k(a, row0, t1.pos0, n_rows, g, tid, k1);
+      else if (t1.left > 0)
+        w.widen_k(k3, k1);
+      lds_barrier();
+      w.first_scores(k0);
+      while (w.step8(t0, t1, t2, t3, k1, v0, k0, v1, k4, v3, k2, v2, s0) &&
+             w.step8(t1, t2, t3, t0, k0, v1, k1, v0, k5, v4, k3, v3, s1) &&
+             w.step8(t2, t3, t0, t1, k1, v0, k0, v1, k2, v5, k4, v4, s2) &&
+             w.step8(t3, t0, t1, t2, k0, v1, k1, v0, k3, v2, k5, v5, s3)) {
       }
     }
   }
