@@ -692,6 +692,9 @@ __device__ __forceinline__ void draft_k(const RowsArgs& a, int row0, int t0, int
     *reinterpret_cast<u32x4*>(lk + k_at(row, c)) =
         draft_chunk(a, a.k_draft, row0, t0 + row, n, g, c);
   }
+  // so that no later register waits for these loads, and with them for all that
+  // are on their way into LDS
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
 }
 __device__ __forceinline__ void draft_v(const RowsArgs& a, int row0, int t0, int n, int g, int tid,
                                         char* lv) {
@@ -704,6 +707,7 @@ __device__ __forceinline__ void draft_v(const RowsArgs& a, int row0, int t0, int
       *reinterpret_cast<uint16_t*>(lv + v_at(i, 8 * c + e, slot >> 3) + 2 * (slot & 7)) =
           (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
   }
+  __builtin_amdgcn_s_waitcnt(0x0F70);
 }
 
 // Softmax state of one (row, head) per lane column q = lane % 32, shared by the
@@ -794,6 +798,7 @@ struct Work {
   int left;                  // tiles of this part still to come
   int drafts;                // drafted tokens still to come
   uint32_t koff, voff;
+  const float* scale_of_head;  // of page 0: lanes 0 and 1 K's, 2 and 3 V's
   int ka;
   f32x16 s;                  // scores of the next tile
   State st;
@@ -850,8 +855,7 @@ struct Work {
   // fp8: the scales of tile t, every wave a copy: K of both pages, then V.
   __device__ __forceinline__ void start_scales(const Tile& t, float* __restrict__ ls) {
     if (paged(t) && lane < 4)
-      to_lds4((lane & 2 ? a.v_scale : a.k_scale) +
-                  (size_t)(lane & 1 ? t.pid[1] : t.pid[0]) * a.num_kv_heads + g,
+      to_lds4(scale_of_head + (size_t)(lane & 1 ? t.pid[1] : t.pid[0]) * a.num_kv_heads,
               ls + 4 * wave);
   }
 
@@ -1125,6 +1129,11 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   const int krow = 4 * wave + (lane >> 4);  // of a page
   w.koff = FP8 ? 1024 * (wave & 1) + 16 * lane : 256 * krow + 16 * ((lane & 15) ^ krow);
   w.voff = 1024 * wave + 32 * l32 + 16 * half;
+  {
+    const uintptr_t ks = reinterpret_cast<uintptr_t>(a.k_scale);
+    const uintptr_t vs = reinterpret_cast<uintptr_t>(a.v_scale);
+    w.scale_of_head = reinterpret_cast<const float*>((lane & 2 ? vs : ks)) + g;
+  }
   w.ka = k_at(16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3), half);
   walk_to(a, w.walk, a.seq_route_begin[b], a.seq_route_begin[b + 1], w.last_pos, it.key0, lane);
   w.left = it.key1 == INT32_MAX ? INT32_MAX : it.key1 - it.key0;
