@@ -519,14 +519,16 @@ struct Walk {
   int pid[2];     // page ids of that tile, on their way
 };
 
-// One tile: its first token's position (of drafted tokens: its first row), how
-// many of its tokens there are (0: there is no such tile), its pages outside the
-// pool (bits 0 and 1), whether it holds drafted tokens.
+// One tile: its first token's position (of drafted tokens: its first row) and how
+// many of its tokens there are (0: there is no such tile).
 struct Tile {
-  int pos0, left, bad;
-  bool draft;
-  int pid[2];  // (0 for one outside the pool)
+  int pos0, left;
+  int kind;        // bits 0 and 1: its pages outside the pool; kDraft, kPart
+  uint64_t at[2];  // its pages in the pools, in bytes (page 0 for one outside)
+  int pid[2];      // fp8: the pages
 };
+constexpr int kDraft = 4;  // drafted tokens
+constexpr int kPart = 8;   // fewer than 32 tokens
 
 __device__ __forceinline__ int visible(int begin, int end, int last_pos) {
   const int64_t n = (int64_t)end - begin, see = (int64_t)last_pos + 1 - begin;
@@ -730,6 +732,10 @@ __device__ __forceinline__ f32x16 scores(const u32x4 (&k)[8], const u32x4 (&q)[8
   for (int i = 0; i < 8; ++i) s = mfma32(k[i], q[i], s);
   return s;
 }
+__device__ __forceinline__ void load_v(const char* lv, int lane, u32x4 (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const u32x4*>(lv + 16 * lane + 1024 * i);
+}
 __device__ __forceinline__ void load_k(const char* lk, int ka, u32x4 (&k)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) k[i] = *reinterpret_cast<const u32x4*>(lk + (ka ^ (32 * i)));
@@ -797,6 +803,8 @@ struct Work {
   Walk walk;
   int left;                  // tiles of this part still to come
   int drafts;                // drafted tokens still to come
+  uint64_t head_at;          // the KV head in page 0, and the distance of two pages
+  uint32_t page_bytes;
   uint32_t koff, voff;
   const float* scale_of_head;  // of page 0: lanes 0 and 1 K's, 2 and 3 V's
   int ka;
@@ -807,49 +815,50 @@ struct Work {
 
   // The next tile; the page ids of the one behind it are sent for.
   __device__ __forceinline__ Tile take() {
-    Tile t{0, 0, 0, false, {0, 0}};
-    if (left > 0 && walk.r < walk.r_end) {
-      if (left != INT32_MAX) --left;
+    Tile t{0, 0, 0, {0, 0}, {0, 0}};
+    if (__builtin_expect(left > 0 && walk.r < walk.r_end, 1)) {
+      --left;  // (from INT32_MAX, where the part has no end, it never comes to 0)
       const int tok0 = walk.j * kKeyTile;
       t.pos0 = walk.tb + tok0;
       t.left = walk.n - tok0;
+      if (t.left < kKeyTile) t.kind = kPart;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        t.pid[i] = walk.pid[i];
-        if ((uint32_t)t.pid[i] >= (uint32_t)a.num_pages) {
-          t.pid[i] = 0;
-          if (kPage * i < t.left) t.bad |= 1 << i;
+        int pid = walk.pid[i];
+        if (__builtin_expect((uint32_t)pid >= (uint32_t)a.num_pages, 0)) {
+          pid = 0;
+          if (kPage * i < t.left) t.kind |= 1 << i;
         }
+        t.at[i] = head_at + (uint64_t)(uint32_t)pid * page_bytes;
+        if constexpr (FP8) t.pid[i] = pid;
       }
-      if (++walk.j < walk.tiles)
+      if (__builtin_expect(++walk.j < walk.tiles, 1))
         walk_ids(a, walk);
       else
         walk_on(a, walk, last_pos);
     } else if (TREE && drafts > 0) {
-      t.draft = true;
       t.pos0 = n_rows - drafts;
       t.left = drafts;
+      t.kind = kDraft;
       drafts -= kKeyTile;
     }
     return t;
   }
 
-  __device__ __forceinline__ bool paged(const Tile& t) const {
-    return t.left > 0 && !(TREE && t.draft);
+  __device__ __forceinline__ static bool paged(const Tile& t) {
+    return TREE ? t.left > 0 && !(t.kind & kDraft) : t.left > 0;
   }
 
   // The loads of one operand of tile t into l, for fp8 into its ring.
   __device__ __forceinline__ void start(const Tile& t, const void* pool, uint32_t off,
                                         char* __restrict__ l) {
-    if (!paged(t)) return;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const size_t at =
-          slice_of(t.pid[i], g, a.num_kv_heads, a.num_pages, a.head_major) * (kPage * kDim);
-      if constexpr (!FP8)
-        to_lds(static_cast<const char*>(pool) + 2 * at + off, l + 4096 * i + 1024 * wave);
-      else if (i == wave >> 1)  // two waves a page
-        to_lds(static_cast<const char*>(pool) + at + off, l + 1024 * wave);
+    if (__builtin_expect(!paged(t), 0)) return;
+    const char* from = static_cast<const char*>(pool);
+    if constexpr (!FP8) {
+      to_lds(from + t.at[0] + off, l + 1024 * wave);
+      to_lds(from + t.at[1] + off, l + 4096 + 1024 * wave);
+    } else {  // two waves a page
+      to_lds(from + (wave >> 1 ? t.at[1] : t.at[0]) + off, l + 1024 * wave);
     }
   }
   // fp8: the scales of tile t, every wave a copy: K of both pages, then V.
@@ -892,14 +901,14 @@ struct Work {
   __device__ __forceinline__ void work(const Tile& t, const char* __restrict__ lk,
                                        char* __restrict__ lv, const float* __restrict__ ls) {
     ++steps;
-    const bool part = t.bad || t.draft || t.left < kKeyTile;
     bool odd = false;
-    if (part || __builtin_elementwise_sub_sat(tile_min, t.pos0) < kKeyTile - 1) {
+    if (__builtin_expect(
+            t.kind || __builtin_elementwise_sub_sat(tile_min, t.pos0) < kKeyTile - 1, 0)) {
       // some row of the workgroup does not see all of it
       if (cut_tile(t.left, tid, lv)) *odd_step = steps;
       lds_barrier();
       odd = uniform(*odd_step) == steps;
-      if (t.bad) flag = KF_EFLAG_BAD_PAGE;
+      if (t.kind & 3) flag = KF_EFLAG_BAD_PAGE;
     }
     if (!any) {
       if (odd) {
@@ -911,26 +920,27 @@ struct Work {
     }
     f32x4 scales = {1.0f, 1.0f, 1.0f, 1.0f};
     if constexpr (FP8) {  // the pages' scales into the scores, in base 2
-      if (!t.draft) scales = *reinterpret_cast<const f32x4*>(ls + 4 * wave);
+      if (!(t.kind & kDraft)) scales = *reinterpret_cast<const f32x4*>(ls + 4 * wave);
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] *= c * scales[i >> 3];
     }
     const int half = lane >> 5;
     uint32_t sees = ~0u;
-    const bool mask = part || __builtin_elementwise_sub_sat(pos_min, t.pos0) < kKeyTile - 1;
-    if (mask) {
+    const bool mask = t.kind || __builtin_elementwise_sub_sat(pos_min, t.pos0) < kKeyTile - 1;
+    if (__builtin_expect(mask, 0)) {
       const int e = min(__builtin_elementwise_sub_sat(pos, t.pos0), t.left - 1);
       sees = e < 0 ? 0 : e >= 31 ? ~0u : (2u << e) - 1;
-      if (TREE && t.draft) sees = (uint32_t)(draft >> t.pos0);
+      if (TREE && (t.kind & kDraft)) sees = (uint32_t)(draft >> t.pos0);
       const uint32_t mine = sees >> (8 * half);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        if (t.bad >> (i >> 3) & 1) s[i] = qnan();
+        if (t.kind >> (i >> 3) & 1) s[i] = qnan();
         if (!(mine >> (16 * (i >> 3) + (i & 7)) & 1)) s[i] = neg_inf();
       }
     }
-    u32x4 k[8];
+    u32x4 k[8], v[8];
     load_k(lk, ka, k);
+    if constexpr (!FP8) load_v(lv, lane, v);  // (fp8 has no registers for it)
     float top = neg_inf();
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
@@ -938,7 +948,7 @@ struct Work {
     if constexpr (!FP8) top *= c;
     // The reference moves only when a score exceeds it by 2^8: exp2 and the sums
     // stay in range, and most tiles leave the outputs unscaled.
-    if (__ballot(top > st.m + 8.0f)) {
+    if (__builtin_expect(__ballot(top > st.m + 8.0f) != 0, 0)) {
       const float m = fmaxf(st.m, top);
       const float f = m == neg_inf() ? 1.0f : exp2_fast(st.m - m);
       st.m = m;
@@ -963,7 +973,7 @@ struct Work {
                          : pack_bf16(e0, e1);
       }
     s = next;
-    if (mask) {
+    if (__builtin_expect(mask, 0)) {
       if constexpr (FP8) {  // a hidden token weighs nothing, whatever its page's scale
         const uint32_t mine = sees >> (8 * half);
 #pragma unroll
@@ -975,18 +985,18 @@ struct Work {
           }
       }
     }
-    if (odd) {
+    if (__builtin_expect(odd, 0)) {
       add_odd(lv, sees, p, lane, st);
       lds_barrier();
       tame_tile(tid, lv);
       lds_barrier();
+      if constexpr (!FP8) load_v(lv, lane, v);
     }
+    if constexpr (FP8) load_v(lv, lane, v);
 #pragma unroll
     for (int page = 0; page < 2; ++page)
 #pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
-        st.o[dt] = mfma32(*reinterpret_cast<const u32x4*>(lv + 16 * lane + 4096 * page + 1024 * dt),
-                          p[page], st.o[dt]);
+      for (int dt = 0; dt < 4; ++dt) st.o[dt] = mfma32(v[4 * page + dt], p[page], st.o[dt]);
   }
 
   // bf16: tile t, whose place t4 takes, V in lv; the next tile's K in lk.  The
@@ -997,21 +1007,17 @@ struct Work {
                                        char* __restrict__ k0, char* __restrict__ v3,
                                        char* __restrict__ k2, char* __restrict__ v1) {
     const Tile t4 = take();
-    // in order: V of t1, K of t2, V of t2, K of t3 may still be out
-    if (paged(t3))
+    // V of t1, K and V of t2, K of t3 may still be out
+    if (__builtin_expect(paged(t3), 1))
       wait<8>();
-    else if (paged(t2))
-      wait<6>();
-    else if (paged(t1))
-      wait<2>();
     else
       wait<0>();
     lds_barrier();
     start(t3, a.v_pool, voff, v3);
     start(t4, a.k_pool, koff, k0);
     work(t, lk, lv, nullptr);
-    if (TREE && t2.draft) draft_k(a, row0, t2.pos0, n_rows, g, tid, k2);
-    if (TREE && t1.draft) draft_v(a, row0, t1.pos0, n_rows, g, tid, v1);
+    if (TREE && (t2.kind & kDraft)) draft_k(a, row0, t2.pos0, n_rows, g, tid, k2);
+    if (TREE && (t1.kind & kDraft)) draft_v(a, row0, t1.pos0, n_rows, g, tid, v1);
     t = t4;
     return t1.left > 0;
   }
@@ -1031,17 +1037,15 @@ struct Work {
     start(t4, a.k_pool, koff, rk0);
     start(t4, a.v_pool, koff, rv0);
     start_scales(t4, s0);
-    if (paged(t4))
+    if (__builtin_expect(paged(t4), 1))
       wait<6>();
-    else if (paged(t3))
-      wait<3>();
     else
       wait<0>();
-    if (TREE && t2.draft)
+    if (TREE && (t2.kind & kDraft))
       draft_k(a, row0, t2.pos0, n_rows, g, tid, k2);
     else if (t2.left > 0)
       widen_k(rk2, k2);
-    if (TREE && t1.draft)
+    if (TREE && (t1.kind & kDraft))
       draft_v(a, row0, t1.pos0, n_rows, g, tid, v1);
     else if (t1.left > 0)
       widen_v(rv1, v1);
@@ -1126,6 +1130,9 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   w.flag = w.steps = 0;
   w.odd_step = &odd_step;
   if (tid == 0) odd_step = 0;
+  const uint32_t head_bytes = kPage * kDim * (FP8 ? 1 : 2);
+  w.page_bytes = a.head_major ? head_bytes : H * head_bytes;
+  w.head_at = (uint64_t)(a.head_major ? (int64_t)g * a.num_pages : g) * head_bytes;
   const int krow = 4 * wave + (lane >> 4);  // of a page
   w.koff = FP8 ? 1024 * (wave & 1) + 16 * lane : 256 * krow + 16 * ((lane & 15) ^ krow);
   w.voff = 1024 * wave + 32 * l32 + 16 * half;
@@ -1153,11 +1160,11 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         w.template wait<12>();
       else
         w.template wait<0>();
-      if (TREE && t0.draft) {
+      if (TREE && (t0.kind & kDraft)) {
         draft_k(a, row0, t0.pos0, n_rows, g, tid, k0);
         draft_v(a, row0, t0.pos0, n_rows, g, tid, v0);
       }
-      if (TREE && t1.draft) draft_k(a, row0, t1.pos0, n_rows, g, tid, k1);
+      if (TREE && (t1.kind & kDraft)) draft_k(a, row0, t1.pos0, n_rows, g, tid, k1);
       lds_barrier();
       w.first_scores(k0);
       while (w.step(t0, t1, t2, t3, k1, v0, k0, v3, k2, v1) &&
@@ -1181,14 +1188,14 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         w.template wait<6>();
       else
         w.template wait<0>();
-      if (TREE && t0.draft) {
+      if (TREE && (t0.kind & kDraft)) {
         draft_k(a, row0, t0.pos0, n_rows, g, tid, k0);
         draft_v(a, row0, t0.pos0, n_rows, g, tid, v0);
       } else {
         w.widen_k(k2, k0);
         w.widen_v(v2, v0);
       }
-      if (TREE && t1.draft)
+      if (TREE && (t1.kind & kDraft))
         draft_k(a, row0, t1.pos0, n_rows, g, tid, k1);
       else if (t1.left > 0)
         w.widen_k(k3, k1);
