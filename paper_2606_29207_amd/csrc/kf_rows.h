@@ -9,6 +9,11 @@ namespace kf {
 constexpr int kRowTile = 128;     // (row, query head) pairs of one KV head per workgroup
 constexpr int kKeyTile = 32;      // tokens per step of a workgroup: two pages
 constexpr int kMaxRecsPerCu = 8;  // records of split work items per compute unit
+constexpr int kMinPart = 4;       // key tiles of a part at least
+constexpr int kUnplannedSteps = 24;  // mean steps of a workgroup up to which a launch needs no plan
+constexpr int kSplitSlots = 4;    // (row tile, KV head) pairs per resident workgroup from which on
+                                  // a launch splits none
+constexpr int kCombineWgsPerSlot = 8;  // workgroups of the combine per resident workgroup at most
 
 // ------------------------------------------------------------------- append
 struct AppendRowsArgs {
@@ -40,7 +45,8 @@ struct RowsItem {
   int32_t tile;   // row tile of the sequence
   int32_t key0, key1;
   int32_t rec;    // record of a split tile's part, -1: the outputs are written
-  int32_t pad[3];
+  int32_t row0, rows, first_pos, route0, route1;  // of the sequence
+  int32_t pad[2];
 };
 
 // The parts of one split row tile.
@@ -83,6 +89,8 @@ struct RowsArgs {
   int32_t max_recs;     // records per KV head
   int32_t rec_rows;     // rows of a record
   int32_t slots;        // resident workgroups
+  int32_t parts;        // > 0: no plan; every row tile in so many parts
+  int32_t may_split;    // a plan may split row tiles: a combine follows
 };
 
 struct RowsLayout {
@@ -92,6 +100,10 @@ struct RowsLayout {
 // total 0: more than a launch takes.
 RowsLayout rows_layout(int32_t num_rows, int32_t num_seqs, int32_t num_kv_heads, int32_t group,
                        int64_t cus);
+
+// Parts per row tile of a launch that runs without a plan, 0 with one.
+int32_t unplanned_parts(const RowsLayout& l, int32_t num_seqs, int32_t num_kv_heads,
+                        int32_t num_routes, int32_t num_page_ids, int64_t slots);
 
 hipError_t launch_rows_attn(const RowsArgs& a, bool fp8, bool tree, hipStream_t stream);
 

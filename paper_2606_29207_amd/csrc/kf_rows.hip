@@ -304,17 +304,36 @@ __device__ __forceinline__ int key_tiles(const RowsArgs& a, int b, int t, int n,
 }
 
 // One workgroup: the row tiles of every sequence, cut into parts of at most
-// `cap` key tiles, largest first.
+// `cap` key tiles, largest first.  Up to kPlanSeqs sequences are gathered by a
+// thread per route and kept in LDS.
+constexpr int kPlanSeqs = 1024;
+
 template <bool TREE>
 __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
   __shared__ unsigned long long s_work;
   __shared__ int s_most, s_recs, s_splits;
   __shared__ int s_count[64], s_scan[16];
+  __shared__ unsigned long long l_tokens[kPlanSeqs];
+  __shared__ int l_tiles[kPlanSeqs + 1], l_info[4 * kPlanSeqs], l_begin[kPlanSeqs + 1];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, B = a.num_seqs;
-  int bad = 0;
+  const bool small = B <= kPlanSeqs;
+  int* const tiles_of = small ? l_tiles : a.seq_tiles;  // first row tile of each sequence
+  int* const info = small ? l_info : a.seq_info;        // tokens, first token, bad, routes seen
+  const int* const begin = small ? l_begin : a.seq_row_begin;
+  int bad = 0, r0 = 0, r1 = 0;
   for (int b = tid; b <= B; b += 1024) {
     const int v = a.seq_row_begin[b];
     bad |= v < 0 || v > a.num_rows || (b > 0 && a.seq_row_begin[b - 1] > v);
+    if (small) l_begin[b] = v;
+  }
+  if (small && tid < B) {
+    r0 = a.seq_route_begin[tid];
+    r1 = a.seq_route_begin[tid + 1];
+    const bool wrong = r0 < 0 || r1 < r0 || r1 > a.num_routes;
+    l_tokens[tid] = 0;
+    l_info[4 * tid + 1] = INT32_MAX;
+    l_info[4 * tid + 2] = wrong;
+    l_info[4 * tid + 3] = 0;
   }
   if (tid == 0) s_work = 0, s_most = 0;
   if (tid < 64) s_count[tid] = 0;
@@ -326,39 +345,62 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
     }
     return;
   }
-  // the sequences' resident tokens, a wave each
-  for (int b = w; b < B; b += 16) {
-    const int n = a.seq_row_begin[b + 1] - a.seq_row_begin[b];
-    if (n == 0) continue;
-    const int r0 = a.seq_route_begin[b], r1 = a.seq_route_begin[b + 1];
-    bool wrong = r0 < 0 || r1 < r0 || r1 > a.num_routes || (TREE && n > KF_MAX_DRAFT);
-    int64_t tokens = 0;
-    int first = INT32_MAX;
-    if (!wrong) {
-      bool mine = true;
-      for (int r = r0 + lane; r < r1; r += 64) {
-        const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + r);
-        mine &= route_ok(a, b, rp);
-        tokens += (int64_t)rp[3] - rp[2];
-        first = min(first, rp[2]);
+  // the sequences' resident tokens: a thread per route, or a wave per sequence
+  if (small) {
+    for (int r = tid; r < a.num_routes; r += 1024) {
+      const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + r);
+      const int b = rp[0];
+      if (b < 0 || b >= B || r < a.seq_route_begin[b] || r >= a.seq_route_begin[b + 1]) continue;
+      if (route_ok(a, b, rp)) {
+        atomicAdd(&l_info[4 * b + 3], 1);
+        atomicAdd(&l_tokens[b], (unsigned long long)(rp[3] - rp[2]));
+        atomicMin(&l_info[4 * b + 1], rp[2]);
       }
-      wrong = __ballot(!mine) != 0;
     }
-    tokens = wave_sum(tokens);
+    __syncthreads();
+    if (tid < B) {
+      const int n = l_begin[tid + 1] - l_begin[tid];
+      // each of its routes has to have been seen
+      const bool wrong = l_info[4 * tid + 2] || l_info[4 * tid + 3] != r1 - r0 ||
+                         (TREE && n > KF_MAX_DRAFT);
+      l_info[4 * tid] = (int)min(l_tokens[tid], (unsigned long long)INT32_MAX - 2 * kKeyTile);
+      l_info[4 * tid + 2] = wrong;
+      if (wrong && n > 0) atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
+    }
+  } else {
+    for (int b = w; b < B; b += 16) {
+      const int n = begin[b + 1] - begin[b];
+      if (n == 0) continue;
+      const int q0 = a.seq_route_begin[b], q1 = a.seq_route_begin[b + 1];
+      bool wrong = q0 < 0 || q1 < q0 || q1 > a.num_routes || (TREE && n > KF_MAX_DRAFT);
+      int64_t tokens = 0;
+      int first = INT32_MAX;
+      if (!wrong) {
+        bool mine = true;
+        for (int r = q0 + lane; r < q1; r += 64) {
+          const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + r);
+          mine &= route_ok(a, b, rp);
+          tokens += (int64_t)rp[3] - rp[2];
+          first = min(first, rp[2]);
+        }
+        wrong = __ballot(!mine) != 0;
+      }
+      tokens = wave_sum(tokens);
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) first = min(first, __shfl_xor(first, m));
-    if (lane == 0) {
-      a.seq_info[4 * b] = (int)min(tokens, (int64_t)INT32_MAX - 2 * kKeyTile);
-      a.seq_info[4 * b + 1] = first;
-      a.seq_info[4 * b + 2] = wrong;
-      if (wrong) atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
+      for (int m = 32; m >= 1; m >>= 1) first = min(first, __shfl_xor(first, m));
+      if (lane == 0) {
+        info[4 * b] = (int)min(tokens, (int64_t)INT32_MAX - 2 * kKeyTile);
+        info[4 * b + 1] = first;
+        info[4 * b + 2] = wrong;
+        if (wrong) atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
+      }
     }
   }
   // their first row tiles
   int sum = 0;
   for (int b0 = 0; b0 < B; b0 += 1024) {
     const int b = b0 + tid;
-    const int64_t n = b < B ? a.seq_row_begin[b + 1] - a.seq_row_begin[b] : 0;
+    const int64_t n = b < B ? begin[b + 1] - begin[b] : 0;
     const int mine = (int)((n * a.group + kRowTile - 1) / kRowTile);
     int x = mine;
 #pragma unroll
@@ -373,26 +415,34 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
       if (i < w) before += s_scan[i];
       sum += s_scan[i];
     }
-    if (b < B) a.seq_tiles[b] = before + x - mine;
+    if (b < B) tiles_of[b] = before + x - mine;
     __syncthreads();
   }
-  if (tid == 0) a.seq_tiles[B] = sum;
+  if (tid == 0) tiles_of[B] = sum;
   __syncthreads();
   const int T = min(sum, a.max_tiles);
   // a tile's sequence and key tiles; a bad sequence's tile has one
-  auto look = [&](int t, int& b, bool& wrong) -> int {
+  auto search = [&](int t, int& b, bool& wrong) -> int {
     int lo = 0, hi = B;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      (a.seq_tiles[mid] <= t ? lo : hi) = mid;
+      (tiles_of[mid] <= t ? lo : hi) = mid;
     }
     b = lo;
-    wrong = a.seq_info[4 * b + 2] != 0;
+    wrong = info[4 * b + 2] != 0;
     if (wrong) return 1;
-    const int k = key_tiles<TREE>(a, b, t - a.seq_tiles[b],
-                                  a.seq_row_begin[b + 1] - a.seq_row_begin[b], a.seq_info[4 * b],
-                                  a.seq_info[4 * b + 1]);
+    const int k = key_tiles<TREE>(a, b, t - tiles_of[b], begin[b + 1] - begin[b], info[4 * b],
+                                  info[4 * b + 1]);
     return k > 0 ? k : 1;
+  };
+  int own_b = 0, own_k = 0;  // this thread's first tile
+  bool own_wrong = false;
+  if (tid < T) own_k = search(tid, own_b, own_wrong);
+  auto look = [&](int t, int& b, bool& wrong) -> int {
+    if (t >= 1024) return search(t, b, wrong);
+    b = own_b;
+    wrong = own_wrong;
+    return own_k;
   };
   unsigned long long work = 0;
   int most = 0;
@@ -413,9 +463,9 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
   __syncthreads();
   most = s_most;
   int cap = most;
-  if (a.max_recs > 1 && (int64_t)T * a.num_kv_heads < 4 * (int64_t)a.slots) {
+  if (a.may_split && (int64_t)T * a.num_kv_heads < kSplitSlots * (int64_t)a.slots) {
     const unsigned long long share = (s_work * a.num_kv_heads + a.slots - 1) / a.slots;
-    cap = (int)min((unsigned long long)most, max(share, 16ull));
+    cap = (int)min((unsigned long long)most, max(share, (unsigned long long)kMinPart));
     for (;;) {  // parts of split tiles, until their records fit
       __syncthreads();
       if (tid == 0) s_recs = 0;
@@ -465,8 +515,14 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
     const int at = atomicAdd(&s_count[place((k + parts - 1) / parts)], parts);
     RowsItem it;
     it.seq = wrong ? -1 - b : b;
-    it.tile = t - a.seq_tiles[b];
+    it.tile = t - tiles_of[b];
     it.rec = -1;
+    it.row0 = begin[b];
+    it.rows = begin[b + 1] - begin[b];
+    it.first_pos = TREE ? 0 : a.first_pos[b];
+    it.route0 = a.seq_route_begin[b];
+    it.route1 = a.seq_route_begin[b + 1];
+    it.pad[0] = it.pad[1] = 0;
     if (parts > 1) {
       it.rec = atomicAdd(&s_recs, parts);
       a.splits[atomicAdd(&s_splits, 1)] = RowsSplit{b, it.tile, it.rec, parts};
@@ -480,6 +536,36 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
   }
   __syncthreads();
   if (tid == 0) a.head[1] = s_splits;
+}
+
+// Without a plan (a.parts > 0: launches of up to 64 sequences and little work):
+// row tile `tile` of the launch, looked up by a wave.  -1: a bad table of rows;
+// 0: there is no such tile; 1: b and its own tile.
+__device__ __forceinline__ int find_tile(const RowsArgs& a, int tile, int lane, int& b, int& own,
+                                         int& row0, int& rows) {
+  int n = 0, i0 = 0;
+  bool bad = false;
+  if (lane < a.num_seqs) {
+    i0 = a.seq_row_begin[lane];
+    const int i1 = a.seq_row_begin[lane + 1];
+    bad = i0 < 0 || i1 < i0 || i1 > a.num_rows;
+    n = bad ? 0 : i1 - i0;
+  }
+  if (__ballot(bad)) return -1;
+  const int mine = (n * a.group + kRowTile - 1) / kRowTile;
+  int x = mine;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int y = __shfl_up(x, m);
+    if (lane >= m) x += y;
+  }
+  const uint64_t found = __ballot(x > tile);
+  if (!found) return 0;
+  b = uniform(__builtin_ctzll(found));
+  own = tile - __builtin_amdgcn_readlane(x - mine, b);
+  row0 = __builtin_amdgcn_readlane(i0, b);
+  rows = __builtin_amdgcn_readlane(n, b);
+  return 1;
 }
 
 // ---------------------------------------------------------------- attention
@@ -523,12 +609,16 @@ struct Walk {
 // many of its tokens there are (0: there is no such tile).
 struct Tile {
   int pos0, left;
-  int kind;        // bits 0 and 1: its pages outside the pool; kDraft, kPart
-  uint64_t at[2];  // its pages in the pools, in bytes (page 0 for one outside)
-  int pid[2];      // fp8: the pages
+  int kind;  // bits 0 and 1: its pages outside the pool; kDraft, kPart
 };
 constexpr int kDraft = 4;  // drafted tokens
 constexpr int kPart = 8;   // fewer than 32 tokens
+// Its pages (0 for one outside the pool), and where they begin in the pools, in
+// bytes.
+struct Pages {
+  int pid[2];
+  uint64_t at[2];
+};
 
 __device__ __forceinline__ int visible(int begin, int end, int last_pos) {
   const int64_t n = (int64_t)end - begin, see = (int64_t)last_pos + 1 - begin;
@@ -559,6 +649,20 @@ __device__ __forceinline__ void walk_on(const RowsArgs& a, Walk& w, int last_pos
   if (w.r < w.r_end) walk_ids(a, w);
 }
 
+// The visible tiles of a sequence's routes; -1 if one of them is bad.
+__device__ __forceinline__ int count_tiles(const RowsArgs& a, int b, int r0, int r1,
+                                           int last_pos, int lane) {
+  int64_t tiles = 0;
+  bool bad = r0 < 0 || r1 < r0 || r1 > a.num_routes;
+  if (bad) return -1;
+  for (int r = r0 + lane; r < r1; r += 64) {
+    const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + r);
+    bad |= !route_ok(a, b, rp);
+    tiles += (visible(rp[2], rp[3], last_pos) + kKeyTile - 1) / kKeyTile;
+  }
+  return __ballot(bad) ? -1 : uniform((int)min(wave_sum(tiles), (int64_t)1 << 30));
+}
+
 // Positions the walk at key tile k of the sequence; tiles of a route: its
 // visible tokens / 32, rounded up.  Sixty-four routes at a time.
 __device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int r1, int last_pos,
@@ -567,11 +671,14 @@ __device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int 
   w.j = w.tiles = 0;
   w.base = w.n = w.tb = w.pid[0] = w.pid[1] = 0;
   for (int r = r0; r < r1; r += 64) {
-    int tiles = 0;
+    int n = 0, tb = 0, base = 0;
     if (r + lane < r1) {
       const kf_route& row = a.routes[r + lane];
-      tiles = (visible(row.tok_begin, row.tok_end, last_pos) + kKeyTile - 1) / kKeyTile;
+      tb = row.tok_begin;
+      base = row.page_base;
+      n = visible(tb, row.tok_end, last_pos);
     }
+    const int tiles = (n + kKeyTile - 1) / kKeyTile;
     int64_t x = tiles;
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) {
@@ -580,9 +687,13 @@ __device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int 
     }
     const uint64_t found = __ballot(x > k);
     if (found) {
-      const int at = __builtin_ctzll(found);
-      w.r = uniform(r + at);
-      walk_enter(a, w, last_pos, uniform((int)(k - __shfl((long long)(x - tiles), at))));
+      const int at = uniform(__builtin_ctzll(found));
+      w.r = r + at;
+      w.n = __builtin_amdgcn_readlane(n, at);
+      w.tb = __builtin_amdgcn_readlane(tb, at);
+      w.base = __builtin_amdgcn_readlane(base, at);
+      w.tiles = __builtin_amdgcn_readlane(tiles, at);
+      w.j = uniform((int)(k - __shfl((long long)(x - tiles), at)));
       walk_ids(a, w);
       return;
     }
@@ -803,6 +914,7 @@ struct Work {
   Walk walk;
   int left;                  // tiles of this part still to come
   int drafts;                // drafted tokens still to come
+  Pages pages;               // of the last tile (bf16: whose V is still to be sent for)
   uint64_t head_at;          // the KV head in page 0, and the distance of two pages
   uint32_t page_bytes;
   uint32_t koff, voff;
@@ -814,8 +926,8 @@ struct Work {
   int* odd_step;             // LDS: the last step whose tile holds infinities or NaN
 
   // The next tile; the page ids of the one behind it are sent for.
-  __device__ __forceinline__ Tile take() {
-    Tile t{0, 0, 0, {0, 0}, {0, 0}};
+  __device__ __forceinline__ Tile take(Pages& pg) {
+    Tile t{0, 0, 0};
     if (__builtin_expect(left > 0 && walk.r < walk.r_end, 1)) {
       --left;  // (from INT32_MAX, where the part has no end, it never comes to 0)
       const int tok0 = walk.j * kKeyTile;
@@ -829,8 +941,8 @@ struct Work {
           pid = 0;
           if (kPage * i < t.left) t.kind |= 1 << i;
         }
-        t.at[i] = head_at + (uint64_t)(uint32_t)pid * page_bytes;
-        if constexpr (FP8) t.pid[i] = pid;
+        pg.at[i] = head_at + (uint64_t)(uint32_t)pid * page_bytes;
+        pg.pid[i] = pid;
       }
       if (__builtin_expect(++walk.j < walk.tiles, 1))
         walk_ids(a, walk);
@@ -850,22 +962,24 @@ struct Work {
   }
 
   // The loads of one operand of tile t into l, for fp8 into its ring.
-  __device__ __forceinline__ void start(const Tile& t, const void* pool, uint32_t off,
-                                        char* __restrict__ l) {
+  __device__ __forceinline__ void start(const Tile& t, const Pages& pg, const void* pool,
+                                        uint32_t off, char* __restrict__ l) {
     if (__builtin_expect(!paged(t), 0)) return;
     const char* from = static_cast<const char*>(pool);
     if constexpr (!FP8) {
-      to_lds(from + t.at[0] + off, l + 1024 * wave);
-      to_lds(from + t.at[1] + off, l + 4096 + 1024 * wave);
+      to_lds(from + pg.at[0] + off, l + 1024 * wave);
+      to_lds(from + pg.at[1] + off, l + 4096 + 1024 * wave);
     } else {  // two waves a page
-      to_lds(from + (wave >> 1 ? t.at[1] : t.at[0]) + off, l + 1024 * wave);
+      const uint64_t x = pg.at[0], y = pg.at[1];
+      to_lds(from + (wave >> 1 ? y : x) + off, l + 1024 * wave);
     }
   }
   // fp8: the scales of tile t, every wave a copy: K of both pages, then V.
-  __device__ __forceinline__ void start_scales(const Tile& t, float* __restrict__ ls) {
+  __device__ __forceinline__ void start_scales(const Tile& t, const Pages& pg,
+                                               float* __restrict__ ls) {
+    const int x = pg.pid[0], y = pg.pid[1];
     if (paged(t) && lane < 4)
-      to_lds4(scale_of_head + (size_t)(lane & 1 ? t.pid[1] : t.pid[0]) * a.num_kv_heads,
-              ls + 4 * wave);
+      to_lds4(scale_of_head + (size_t)(lane & 1 ? y : x) * a.num_kv_heads, ls + 4 * wave);
   }
 
   // Waits until at most n loads of this wave are out.
@@ -1006,15 +1120,17 @@ struct Work {
                                        const char* __restrict__ lk, char* __restrict__ lv,
                                        char* __restrict__ k0, char* __restrict__ v3,
                                        char* __restrict__ k2, char* __restrict__ v1) {
-    const Tile t4 = take();
+    Pages pg4;
+    const Tile t4 = take(pg4);
     // V of t1, K and V of t2, K of t3 may still be out
     if (__builtin_expect(paged(t3), 1))
       wait<8>();
     else
       wait<0>();
     lds_barrier();
-    start(t3, a.v_pool, voff, v3);
-    start(t4, a.k_pool, koff, k0);
+    start(t3, pages, a.v_pool, voff, v3);
+    start(t4, pg4, a.k_pool, koff, k0);
+    pages = pg4;
     work(t, lk, lv, nullptr);
     if (TREE && (t2.kind & kDraft)) draft_k(a, row0, t2.pos0, n_rows, g, tid, k2);
     if (TREE && (t1.kind & kDraft)) draft_v(a, row0, t1.pos0, n_rows, g, tid, v1);
@@ -1031,12 +1147,13 @@ struct Work {
                                         const char* __restrict__ rk2, const char* __restrict__ rv1,
                                         char* __restrict__ rk0, char* __restrict__ rv0,
                                         float* __restrict__ s0) {
-    const Tile t4 = take();
+    Pages pg4;
+    const Tile t4 = take(pg4);
     lds_barrier();
     work(t, lk, lv, s0);
-    start(t4, a.k_pool, koff, rk0);
-    start(t4, a.v_pool, koff, rv0);
-    start_scales(t4, s0);
+    start(t4, pg4, a.k_pool, koff, rk0);
+    start(t4, pg4, a.v_pool, koff, rv0);
+    start_scales(t4, pg4, s0);
     if (__builtin_expect(paged(t4), 1))
       wait<6>();
     else
@@ -1068,26 +1185,75 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   const int half = lane >> 5, l32 = lane & 31;
   const int H = a.num_kv_heads, G = a.group;
   const int g = blockIdx.x % H, item = blockIdx.x / H;
-  const int items = a.head[0];
-  if (items < 0) {  // no row's sequence is known
+  RowsItem it;
+  int found = 1;
+  if (a.parts > 0) {
+    const int tile = item % a.max_tiles;
+    found = find_tile(a, tile, lane, it.seq, it.tile, it.row0, it.rows);
+    if (found > 0) {
+      it.first_pos = TREE ? 0 : fixed(a.first_pos)[it.seq];
+      it.route0 = fixed(a.seq_route_begin)[it.seq];
+      it.route1 = fixed(a.seq_route_begin)[it.seq + 1];
+    }
+    it.rec = a.parts > 1 ? tile * a.parts + item / a.max_tiles : -1;
+  } else {
+    const int items = fixed(a.head)[0];
+    const auto* at = fixed(reinterpret_cast<const int32_t*>(a.items + item));
+    it.seq = at[0];
+    it.tile = at[1];
+    it.key0 = at[2];
+    it.key1 = at[3];
+    it.rec = at[4];
+    it.row0 = at[5];
+    it.rows = at[6];
+    it.first_pos = at[7];
+    it.route0 = at[8];
+    it.route1 = at[9];
+    found = items < 0 ? -1 : item < items;
+  }
+  if (found < 0) {  // no row's sequence is known
     for (int r = item; r < a.num_rows; r += gridDim.x / H) fill_nan(a, r, 0, G, g, tid, 256);
+    if (a.parts > 0 && item == 0 && tid == 0) atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
     return;
   }
-  if (item >= items) return;
-  const RowsItem it = a.items[item];
+  if (found == 0) return;
   const int b = uniform(it.seq < 0 ? -1 - it.seq : it.seq);
-  const int row0 = a.seq_row_begin[b], n_rows = a.seq_row_begin[b + 1] - row0;
-  const int64_t m_all = (int64_t)n_rows * G, m0 = (int64_t)it.tile * kRowTile;
-  const int64_t m1 = min(m_all, m0 + kRowTile);
+  const int row0 = it.row0, n_rows = it.rows;
+  const int m0 = it.tile * kRowTile, m1 = min(n_rows * G, m0 + kRowTile);  // (row, head) pairs
+  // no token lies behind INT32_MAX
+  const int p0 = it.first_pos;
+  auto position = [&](int pair) {
+    return TREE ? INT32_MAX
+                : __builtin_elementwise_add_sat(p0, (int)((uint32_t)min(pair, m1 - 1) / (uint32_t)G));
+  };
+  const int last_pos = uniform(position(m1 - 1));
+  const int route0 = it.route0, route1 = it.route1;
+  if (a.parts > 0) {
+    const int k = TREE && n_rows > KF_MAX_DRAFT
+                      ? -1 : count_tiles(a, b, route0, route1, last_pos, lane);
+    if (k < 0) {
+      it.seq = -1 - b;
+      if (tid == 0) atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
+    } else {
+      const int64_t all = k + (TREE ? (n_rows + kKeyTile - 1) / kKeyTile : 0);
+      const int part = item / a.max_tiles;
+      it.key0 = uniform((int)(all * part / a.parts));
+      it.key1 = part + 1 < a.parts ? uniform((int)(all * (part + 1) / a.parts)) : INT32_MAX;
+    }
+  }
   if (it.seq < 0) {
-    fill_nan(a, row0, m0, m1, g, tid, 256);
+    if (it.rec < 0)
+      fill_nan(a, row0, m0, m1, g, tid, 256);
+    else if (tid < m1 - m0)  // a sum of NaN makes the outputs NaN
+      *reinterpret_cast<f32x2*>(a.rec_ml + 2 * (((size_t)it.rec * H + g) * a.rec_rows + tid)) =
+          f32x2{0.0f, qnan()};
     return;
   }
   // this lane's row and head
-  const int64_t m = m0 + 32 * wave + l32;
+  const int m = m0 + 32 * wave + l32;
   const bool mine = m < m1;
-  const int64_t mc = mine ? m : m1 - 1;
-  const int row = (int)(mc / G), h = g * G + (int)(mc % G);
+  const uint32_t mc = mine ? m : m1 - 1;
+  const int row = mc / (uint32_t)G, h = g * G + mc % (uint32_t)G;
   const float c0 = a.scale_log2;
   Work<FP8, TREE> w{a};
   w.tid = tid;
@@ -1105,21 +1271,16 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     if (c0 == 0.0f || !mine) x = u32x4{0, 0, 0, 0};  // a zero one makes all scores equal
     w.q[ks] = x;
   }
-  w.pos = w.pos_min = w.tile_min = w.last_pos = INT32_MAX;
+  w.pos = w.pos_min = w.tile_min = INT32_MAX;
+  w.last_pos = last_pos;
   w.draft = 0;
   if constexpr (TREE) {
     w.draft = mine ? a.tree_mask[row0 + row] : 0;
     if (n_rows < 64) w.draft &= ((uint64_t)1 << n_rows) - 1;
   } else {
-    // no token lies behind INT32_MAX
-    const int64_t p0 = a.first_pos[b];
-    auto at = [&](int64_t pair) {
-      return (int)min(p0 + min(pair, m1 - 1) / G, (int64_t)INT32_MAX);
-    };
-    w.pos = at(m);
-    w.pos_min = uniform(at(m0 + 32 * wave));
-    w.tile_min = uniform(at(m0));
-    w.last_pos = uniform(at(m1 - 1));
+    w.pos = position(m);
+    w.pos_min = uniform(position(m0 + 32 * wave));
+    w.tile_min = uniform(position(m0));
   }
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
@@ -1142,19 +1303,23 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     w.scale_of_head = reinterpret_cast<const float*>((lane & 2 ? vs : ks)) + g;
   }
   w.ka = k_at(16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3), half);
-  walk_to(a, w.walk, a.seq_route_begin[b], a.seq_route_begin[b + 1], w.last_pos, it.key0, lane);
+  walk_to(a, w.walk, route0, route1, last_pos, it.key0, lane);
   w.left = it.key1 == INT32_MAX ? INT32_MAX : it.key1 - it.key0;
   w.drafts = TREE && it.key1 == INT32_MAX ? n_rows : 0;
 
-  Tile t0 = w.take(), t1 = w.take(), t2 = w.take(), t3 = w.take();
+  Tile t0, t1, t2, t3;
   if constexpr (!FP8) {
-    w.start(t0, a.k_pool, w.koff, k0);
-    w.start(t0, a.v_pool, w.voff, v0);
-    w.start(t1, a.k_pool, w.koff, k1);
-    w.start(t1, a.v_pool, w.voff, v1);
-    w.start(t2, a.k_pool, w.koff, k2);
-    w.start(t2, a.v_pool, w.voff, v2);
-    w.start(t3, a.k_pool, w.koff, k3);
+    t0 = w.take(w.pages);
+    w.start(t0, w.pages, a.k_pool, w.koff, k0);
+    w.start(t0, w.pages, a.v_pool, w.voff, v0);
+    t1 = w.take(w.pages);
+    w.start(t1, w.pages, a.k_pool, w.koff, k1);
+    w.start(t1, w.pages, a.v_pool, w.voff, v1);
+    t2 = w.take(w.pages);
+    w.start(t2, w.pages, a.k_pool, w.koff, k2);
+    w.start(t2, w.pages, a.v_pool, w.voff, v2);
+    t3 = w.take(w.pages);
+    w.start(t3, w.pages, a.k_pool, w.koff, k3);
     if (t0.left > 0) {
       if (w.paged(t3))
         w.template wait<12>();
@@ -1174,15 +1339,17 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
       }
     }
   } else {
-    auto start = [&](const Tile& t, char* rk, char* rv, float* ls) {
-      w.start(t, a.k_pool, w.koff, rk);
-      w.start(t, a.v_pool, w.koff, rv);
-      w.start_scales(t, ls);
+    auto start = [&](char* rk, char* rv, float* ls) __attribute__((always_inline)) {
+      const Tile t = w.take(w.pages);
+      w.start(t, w.pages, a.k_pool, w.koff, rk);
+      w.start(t, w.pages, a.v_pool, w.koff, rv);
+      w.start_scales(t, w.pages, ls);
+      return t;
     };
-    start(t0, k2, v2, s0);
-    start(t1, k3, v3, s1);
-    start(t2, k4, v4, s2);
-    start(t3, k5, v5, s3);
+    t0 = start(k2, v2, s0);
+    t1 = start(k3, v3, s1);
+    t2 = start(k4, v4, s2);
+    t3 = start(k5, v5, s3);
     if (t0.left > 0) {
       if (w.paged(t3))
         w.template wait<6>();
@@ -1213,7 +1380,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   const State& st = w.st;
   const float l = sum_halves(st.l);
   if (it.rec >= 0) {
-    const size_t rec = ((size_t)it.rec * H + g) * a.rec_rows + (int)(m - m0);
+    const size_t rec = ((size_t)it.rec * H + g) * a.rec_rows + (m - m0);
     if (half == 0) *reinterpret_cast<f32x2*>(a.rec_ml + 2 * rec) = f32x2{st.m, l};
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
@@ -1235,40 +1402,66 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   if (half == 0) a.lse[at] = l == 0.0f ? neg_inf() : (st.m + __log2f(l)) * kLn2;
 }
 
-// The parts of a split row tile into its outputs: a wave per (row, head).
+// The parts of a split row tile into its outputs: a wave per (row, head), the
+// records of four parts on their way at a time.
 __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
-  const int H = a.num_kv_heads, G = a.group, g = blockIdx.y;
-  const int split = blockIdx.x / 8;
-  if (split >= a.head[1]) return;
-  const RowsSplit sp = a.splits[split];
-  const int row0 = a.seq_row_begin[sp.seq];
-  const int64_t m_all = (int64_t)(a.seq_row_begin[sp.seq + 1] - row0) * G;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int k = wave; k < kRowTile / 8; k += 4) {
-    const int rm = (blockIdx.x & 7) * (kRowTile / 8) + k;
-    const int64_t m = (int64_t)sp.tile * kRowTile + rm;
-    if (m >= m_all) return;
-    const size_t stride = (size_t)H * a.rec_rows;
+  const int H = a.num_kv_heads, G = a.group;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int splits = a.parts > 0 ? a.max_tiles : fixed(a.head)[1];
+  const size_t stride = (size_t)H * a.rec_rows;
+  for (int64_t u = (int64_t)blockIdx.x * 4 + wave; u < (int64_t)splits * H * a.rec_rows;
+       u += (int64_t)gridDim.x * 4) {
+    const int rm = (int)(u % a.rec_rows), g = (int)(u / a.rec_rows % H);
+    const int split = (int)(u / stride);
+    RowsSplit sp;
+    int row0, rows;
+    if (a.parts > 0) {
+      sp.rec = split * a.parts;
+      sp.parts = a.parts;
+      if (find_tile(a, split, lane, sp.seq, sp.tile, row0, rows) <= 0) return;
+    } else {
+      sp = a.splits[split];
+      row0 = a.seq_row_begin[sp.seq];
+      rows = a.seq_row_begin[sp.seq + 1] - row0;
+    }
+    const int m = sp.tile * kRowTile + rm;
+    if (m >= rows * G) continue;
     const size_t rec = ((size_t)sp.rec * H + g) * a.rec_rows + rm;
-    float top = neg_inf();
-    for (int p = lane; p < sp.parts; p += 64) top = fmaxf(top, a.rec_ml[2 * (rec + p * stride)]);
-    top = wave_max(top);
-    const float ref = top == neg_inf() ? 0.0f : top;
+    const float* ml = a.rec_ml + 2 * rec;
+    const f32x2* ro = reinterpret_cast<const f32x2*>(a.rec_o + rec * kDim) + lane;
+    float ref = neg_inf();  // the largest maximum so far
     float l = 0.0f;
     f32x2 o = {0.0f, 0.0f};
-    for (int p = 0; p < sp.parts; ++p) {
-      const f32x2 ml = *reinterpret_cast<const f32x2*>(a.rec_ml + 2 * (rec + p * stride));
-      const f32x2 x =
-          reinterpret_cast<const f32x2*>(a.rec_o + (rec + p * stride) * kDim)[lane];
-      const float f = exp2_fast(ml.x - ref);
-      l = __builtin_fmaf(f, ml.y, l);
-      o.x = __builtin_fmaf(f, x.x, o.x);
-      o.y = __builtin_fmaf(f, x.y, o.y);
+    for (int p = 0; p < sp.parts; p += 4) {
+      f32x2 x[4], y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int q = min(p + i, sp.parts - 1);
+        x[i] = *reinterpret_cast<const f32x2*>(ml + 2 * q * stride);
+        y[i] = ro[q * stride * (kDim / 2)];
+      }
+      float top = ref;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, x[i].x);
+      const float base = top == neg_inf() ? 0.0f : top;
+      const float f = exp2_fast(ref - base);
+      ref = top;
+      l *= f;
+      o.x *= f;
+      o.y *= f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (p + i >= sp.parts) continue;
+        const float e = exp2_fast(x[i].x - base);
+        l = __builtin_fmaf(e, x[i].y, l);
+        o.x = __builtin_fmaf(e, y[i].x, o.x);
+        o.y = __builtin_fmaf(e, y[i].y, o.y);
+      }
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const size_t at = (row0 + m / G) * a.num_q_heads + g * G + m % G;
+    const size_t at = (size_t)(row0 + m / G) * a.num_q_heads + g * G + m % G;
     reinterpret_cast<uint32_t*>(a.out + at * kDim)[lane] = pack_bf16(o.x * inv, o.y * inv);
-    if (lane == 0) a.lse[at] = l == 0.0f ? neg_inf() : (top + __log2f(l)) * kLn2;
+    if (lane == 0) a.lse[at] = l == 0.0f ? neg_inf() : (ref + __log2f(l)) * kLn2;
   }
 }
 
@@ -1295,13 +1488,16 @@ hipError_t launch_append_rows(const AppendRowsArgs& a, bool fp8, hipStream_t str
 }
 
 hipError_t launch_rows_attn(const RowsArgs& a, bool fp8, bool tree, hipStream_t stream) {
-  if (tree)
-    rows_plan_kernel<true><<<1, 1024, 0, stream>>>(a);
-  else
-    rows_plan_kernel<false><<<1, 1024, 0, stream>>>(a);
-  hipError_t st = hipGetLastError();
-  if (st != hipSuccess) return st;
-  const uint32_t grid = (uint32_t)(a.max_tiles + a.max_recs) * a.num_kv_heads;
+  hipError_t st;
+  if (a.parts == 0) {
+    if (tree)
+      rows_plan_kernel<true><<<1, 1024, 0, stream>>>(a);
+    else
+      rows_plan_kernel<false><<<1, 1024, 0, stream>>>(a);
+    if ((st = hipGetLastError()) != hipSuccess) return st;
+  }
+  const uint32_t grid =
+      (uint32_t)(a.parts > 0 ? a.max_tiles * a.parts : a.max_tiles + a.max_recs) * a.num_kv_heads;
   if (fp8 && tree)
     rows_kernel<true, true><<<grid, 256, 0, stream>>>(a);
   else if (fp8)
@@ -1311,9 +1507,12 @@ hipError_t launch_rows_attn(const RowsArgs& a, bool fp8, bool tree, hipStream_t 
   else
     rows_kernel<false, false><<<grid, 256, 0, stream>>>(a);
   st = hipGetLastError();
-  if (st != hipSuccess || a.max_recs < 2) return st;
-  const uint32_t splits = (uint32_t)min(a.max_tiles, a.max_recs / 2);
-  rows_combine_kernel<<<dim3(splits * 8, a.num_kv_heads), 256, 0, stream>>>(a);
+  if (st != hipSuccess || a.parts == 1 || (a.parts == 0 && !a.may_split)) return st;
+  // a wave per (row, head) and turn; most splits at most
+  const int64_t splits = a.parts > 0 ? a.max_tiles : min(a.max_tiles, a.max_recs / 2);
+  const int64_t waves = splits * a.num_kv_heads * a.rec_rows;
+  const uint32_t wgs = (uint32_t)min((waves + 3) / 4, (int64_t)kCombineWgsPerSlot * a.slots);
+  rows_combine_kernel<<<wgs, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -32,6 +32,7 @@ RowsLayout rows_layout(int32_t num_rows, int32_t num_seqs, int32_t num_kv_heads,
   if (num_kv_heads > kMaxLaunchRoutes) return l;
   // ceil(n_b G / kRowTile) tiles of each sequence that has rows
   const int64_t pairs = (int64_t)num_rows * group;
+  if (pairs > INT32_MAX - kRowTile) return l;
   const int64_t tiles = pairs / kRowTile + std::min(num_seqs, num_rows);
   int64_t recs = kMaxRecsPerCu * cus / num_kv_heads;
   if (recs < 2) recs = 0;
@@ -48,6 +49,21 @@ RowsLayout rows_layout(int32_t num_rows, int32_t num_seqs, int32_t num_kv_heads,
   l.o_off = l.ml_off + round_up(rec * 2 * sizeof(float), 256);
   l.total = l.o_off + rec * kDim * sizeof(float);
   return l;
+}
+
+// The plan's launch costs about as much as eight steps of a workgroup.  Where
+// the row tiles leave workgroups free and an even split of every tile comes to
+// few steps, sequences of different lengths cost less than that, and every
+// workgroup finds its own tile.
+int32_t unplanned_parts(const RowsLayout& l, int32_t num_seqs, int32_t num_kv_heads,
+                        int32_t num_routes, int32_t num_page_ids, int64_t slots) {
+  const int64_t items = (int64_t)l.max_tiles * num_kv_heads;
+  if (num_seqs > 64 || num_seqs < 1 || items > slots) return 0;
+  // mean key tiles of a sequence, as the page table tells it
+  const int64_t keys = ((int64_t)num_page_ids * KF_PAGE_SIZE / kKeyTile + num_routes) / num_seqs + 1;
+  int64_t parts = std::min(slots / items, (keys + kMinPart - 1) / kMinPart);
+  parts = std::max<int64_t>(1, std::min<int64_t>(parts, l.max_recs / l.max_tiles));
+  return keys <= kUnplannedSteps * parts ? (int32_t)parts : 0;
 }
 
 }  // namespace kf
@@ -120,6 +136,11 @@ int prepare_rows(const kf_shape* shape, const void* q, int32_t num_rows, int64_t
   a.max_recs = l.max_recs;
   a.rec_rows = l.rec_rows;
   a.slots = (int32_t)(2 * cus);
+  a.parts = kf::unplanned_parts(l, shape->num_seqs, shape->num_kv_heads, num_routes,
+                                shape->num_page_ids, a.slots);
+  // the row tiles that num_rows comes to if every row belongs to a sequence
+  const int64_t tiles = ((int64_t)num_rows * group + kf::kRowTile - 1) / kf::kRowTile;
+  a.may_split = l.max_recs > 1 && tiles * shape->num_kv_heads < kf::kSplitSlots * (int64_t)a.slots;
   return KF_OK;
 }
 

@@ -196,9 +196,10 @@ def test_bad_pages_that_no_row_sees_raise_nothing(gpu):
 
 
 @pytest.mark.parametrize("what", ["seq", "order", "base", "cap", "ids", "most", "csr", "csr_end"])
-def test_bad_routes_reach_their_sequence(gpu, what):
-    c = Cache([100, 90, 60], H=1, part=64, seed=2)
-    r = Rows(c, [20, 30, 10], 2, seed=2)
+def test_bad_routes_reach_their_sequence(gpu, what, spare=0):
+    """(spare: so many empty sequences more)"""
+    c = Cache([100, 90, 60] + [0] * spare, H=1, part=64, seed=2)
+    r = Rows(c, [20, 30, 10] + [0] * spare, 2, seed=2)
     row = c.routes[2]                          # sequence 1
     if what == "seq":
         row[0] = 0
@@ -215,7 +216,7 @@ def test_bad_routes_reach_their_sequence(gpu, what):
     elif what == "csr":
         c.seq_route_begin[1] = 5
     else:
-        c.seq_route_begin[3] = 100
+        c.seq_route_begin[3] = 100 + spare
     got, ref = r.gpu(), r.oracle()
     assert ref[2] == 2 and np.isnan(ref[0]).any()
     assert_rows(got, ref, what)
@@ -237,6 +238,57 @@ def test_too_many_drafts_of_one_sequence(gpu):
     got, ref = r.gpu(), r.oracle()
     assert ref[2] == 2
     assert_rows(got, ref)
+
+
+# ----------------------------------------------------------- many sequences
+@pytest.mark.parametrize("B", [64, 65, 1024, 1025, 3000])
+@pytest.mark.parametrize("tree", [False, True])
+def test_many_sequences(gpu, B, tree):
+    """Launches that find their tiles themselves (up to 64 sequences) and planned
+    ones, in LDS (up to 1024) and beyond; sequences without rows, bad ones among
+    them."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(0, 60, B)
+    counts = np.minimum(rng.integers(0, 4, B), lens if not tree else 64)
+    c = Cache(lens, H=1, part=32, seed=B)
+    r = Rows(c, counts, 2, tree=tree, seed=B)
+    for b in (3, B // 2, B - 1):
+        counts[b] = max(counts[b], 1)
+    c.routes[c.seq_route_begin[B // 2]][4] = -3
+    c.page_ids[c.routes[-1][4]:][:1] = 1 << 20
+    assert_rows(r.gpu(), r.oracle(), f"B {B}")
+
+
+@pytest.mark.parametrize("what", ["seq", "order", "base", "cap", "ids", "most", "csr", "csr_end"])
+def test_bad_routes_of_planned_launches(gpu, what):
+    test_bad_routes_reach_their_sequence(gpu, what, spare=70)
+
+
+@pytest.mark.parametrize("begin", [[0, 50, 20, 60], [-1, 20, 50, 60], [0, 20, 50, 61]])
+def test_a_bad_row_table_of_planned_launches(gpu, begin):
+    c = Cache([100, 90, 60] + [0] * 70, H=2, seed=2)
+    for tree in (False, True):
+        r = Rows(c, [20, 30, 10] + [0] * 70, 2, tree=tree, seed=2)
+        r.row_begin = np.array(begin + begin[-1:] * 70, np.int32)
+        out, lse, flags = r.gpu()
+        assert flags == 2 and np.isnan(out).all() and np.isnan(lse).all()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("tree", [False, True])
+def test_planned_splits(gpu, fp8, tree):
+    """70 sequences, some long: tiles in parts of different sizes, bad routes and
+    pages among split sequences."""
+    lens = [5000, 20, 0, 2500, 900] + [40] * 65
+    counts = [9, 20, 3 * tree, 33, 4] + [1] * 65
+    c = Cache(lens, H=2, fp8=fp8, part=2048, seed=4)
+    r = Rows(c, counts, 4, tree=tree, seed=4)
+    assert_rows(r.gpu(), r.oracle())
+    c.page_ids[c.routes[1][4] + 5] = -9        # sequence 0, token 2128 on
+    c.routes[c.seq_route_begin[3] + 1][5] = 0  # sequence 3
+    ref = r.oracle()
+    assert ref[2] == 6
+    assert_rows(r.gpu(), ref)
 
 
 # ------------------------------------------------------------ how it is run
