@@ -60,52 +60,83 @@ __device__ __forceinline__ float wave_max(float x) {
   return x;
 }
 
-// One route's check, by a whole workgroup: its tokens before the append, or -1
-// if it takes no rows (flag says why).
+// One route's check: its tokens before the append, or -1 if it takes no rows (flag
+// says why).  WHOLE: by the workgroup together; else by every wave for itself, for
+// calls of a few rows, which are a chain of loads.
+template <bool WHOLE>
 __device__ int append_check(const AppendRowsArgs& a, int r, int& flag) {
-  const int tid = threadIdx.x, nt = blockDim.x;
-  // the whole table of entries: nondecreasing within [0, num_entries]
-  int bad = 0;
-  for (int i = tid; i <= a.num_routes; i += nt) {
-    const int v = a.entry_begin[i];
-    bad |= v < 0 || v > a.num_entries || (i > 0 && a.entry_begin[i - 1] > v);
-  }
-  if (__syncthreads_or(bad)) {
-    flag = KF_EFLAG_BAD_ROUTE;
-    return -1;
-  }
+  const int lane = WHOLE ? threadIdx.x : threadIdx.x & 63, step = WHOLE ? blockDim.x : 64;
+  auto any = [](bool x) -> bool { return WHOLE ? __syncthreads_or(x) : __ballot(x) != 0; };
   const int e0 = a.entry_begin[r], n = a.entry_begin[r + 1] - e0;
-  if (n == 0) return -1;
   const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + r);
   const int seq = rp[0], tb = rp[2], te = rp[3], base = rp[4], cap = rp[5];
+  // the whole table of entries: nondecreasing within [0, num_entries]
+  bool bad = false;
+  for (int i = lane; i < a.num_routes; i += step) {
+    const int x = a.entry_begin[i], y = a.entry_begin[i + 1];
+    bad |= x < 0 || y < x || y > a.num_entries;
+  }
+  flag = any(bad) ? KF_EFLAG_BAD_ROUTE : 0;
+  if (flag || n == 0) return -1;
   const int64_t j0 = (int64_t)te - tb, last = (j0 + n - 1) / kPage;
-  if (seq < 0 || seq >= a.num_seqs || j0 < 0 || (int64_t)te + n > INT32_MAX || j0 + n > INT32_MAX) {
+  if (seq < 0 || seq >= a.num_seqs || j0 < 0 || (int64_t)te + n > INT32_MAX || j0 + n > INT32_MAX)
     flag = KF_EFLAG_BAD_ROUTE;
-    return -1;
-  }
-  if (last >= cap) {
+  else if (last >= cap)
     flag = KF_EFLAG_TAIL_FULL;
-    return -1;
-  }
-  if (base < 0 || base + last >= a.num_page_ids) {
+  else if (base < 0 || base + last >= a.num_page_ids)
     flag = KF_EFLAG_BAD_ROUTE;
-    return -1;
-  }
-  bad = 0;
-  for (int64_t p = j0 / kPage + tid; p <= last; p += nt) {
-    const int id = a.page_ids[base + p];
-    if (id < 0 || id >= a.num_pages) bad |= KF_EFLAG_BAD_PAGE;
-  }
-  if (a.row_list) {
-    for (int i = tid; i < n; i += nt) {
-      const int row = a.row_list[e0 + i];
-      if (row < 0 || row >= a.num_rows) bad |= KF_EFLAG_BAD_ROUTE;
-    }
-  }
-  const int page = __syncthreads_or(bad & KF_EFLAG_BAD_PAGE);
-  const int row = __syncthreads_or(bad & KF_EFLAG_BAD_ROUTE);
-  flag = page ? KF_EFLAG_BAD_PAGE : row ? KF_EFLAG_BAD_ROUTE : 0;
+  if (flag) return -1;
+  bool page = false, row = false;
+  for (int64_t p = j0 / kPage + lane; p <= last; p += step)
+    page |= (uint32_t)a.page_ids[base + p] >= (uint32_t)a.num_pages;
+  if (a.row_list)
+    for (int i = lane; i < n; i += step) row |= (uint32_t)a.row_list[e0 + i] >= (uint32_t)a.num_rows;
+  flag = any(page) ? KF_EFLAG_BAD_PAGE : any(row) ? KF_EFLAG_BAD_ROUTE : 0;
   return flag ? -1 : (int)j0;
+}
+
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// Sizes of the two bf16 of x as integers, which order as the values do (an
+// infinity is 0x7F80, a NaN more); the larger of two such pairs, place by place.
+__device__ __forceinline__ uint32_t sizes(uint32_t x) { return x & 0x7FFF7FFFu; }
+__device__ __forceinline__ uint32_t larger(uint32_t x, uint32_t y) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x),
+                                                                __builtin_bit_cast(u16x2, y)));
+}
+__device__ __forceinline__ uint32_t both_places(uint32_t x) { return larger(x, x >> 16) & 0xFFFFu; }
+
+// The scale of an fp8 page after an append, if its rule is one scale for all of
+// the call's tokens: sizes of the token at slot 0 (first, if the page begins with
+// the call) and of all of them (most).  Negative where it is not: a token beyond
+// 448 times the scale re-encodes the page; and where the quick quotient below is
+// not exact: infinities, NaN, scales near the ends of float32.
+__device__ __forceinline__ float one_scale(bool begins, uint32_t first, uint32_t most,
+                                           const float* scale_at) {
+  float scale;
+  if (begins) {
+    const float amax = __builtin_bit_cast(float, first << 16);
+    scale = amax > 0.0f ? amax / 28.0f : 1.0f;
+  } else {
+    scale = *scale_at;
+  }
+  const bool ok = most < 0x7F80u && __builtin_bit_cast(float, most << 16) <= 448.0f * scale &&
+                  scale >= 0x1p-60f && scale <= 0x1p60f;
+  return ok ? scale : -1.0f;
+}
+
+// x / scale, correctly rounded, clamped to +-448: inv is 1 / scale, correctly
+// rounded, so that one step from x inv by its remainder gives the nearest float
+// (Markstein).  Remainders stay in range where the quotient is not far below
+// E4M3's smallest value; there any quotient rounds to the same zero.
+__device__ __forceinline__ float quotient(float x, float scale, float inv) {
+  const float q = x * inv;
+  return __builtin_amdgcn_fmed3f(__builtin_fmaf(__builtin_fmaf(-q, scale, x), inv, q), -448.0f,
+                                 448.0f);
+}
+__device__ __forceinline__ float lo_bf16(uint32_t x) { return __builtin_bit_cast(float, x << 16); }
+__device__ __forceinline__ float hi_bf16(uint32_t x) {
+  return __builtin_bit_cast(float, x & 0xFFFF0000u);
 }
 
 // The slots [s0, s1) of one page of one KV head, K or V, filled from the rows of
@@ -131,6 +162,50 @@ __device__ void append_page(const AppendRowsArgs& a, int page, int g, bool is_v,
     }
     return;
   }
+  uint8_t* pool = FP8 ? static_cast<uint8_t*>(is_v ? a.v_pool : a.k_pool) + head * (kPage * kDim)
+                      : nullptr;
+  float* scale_at = FP8 ? (is_v ? a.v_scale : a.k_scale) + (size_t)page * H + g : nullptr;
+  if (FP8 && !is_v) {  // four lanes a row: eight dims of every 32
+    const int s = lane >> 2, c = lane & 3;
+    const bool mine = s >= s0 && s < s1;
+    u32x4 x[4] = {};
+    if (mine) {
+      const uint16_t* row = rows + row_of(s);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = ld16(row + 32 * i + 8 * c);
+    }
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) most = larger(most, sizes(x[i][k]));
+    most = both_places(most);
+    most |= s == 0 ? most << 16 : 0;  // the token at slot 0 in the upper half
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) most = larger(most, (uint32_t)__shfl_xor((int)most, m));
+    const float scale = one_scale(s0 == 0, most >> 16, most & 0xFFFFu, scale_at);
+    if (scale > 0.0f) {
+      const float inv = 1.0f / scale;
+      if (mine) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          u32x2 codes;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t u = x[i][2 * k], v = x[i][2 * k + 1];
+            int w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(lo_bf16(u), scale, inv),
+                                                    quotient(hi_bf16(u), scale, inv), 0, false);
+            w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(lo_bf16(v), scale, inv),
+                                                quotient(hi_bf16(v), scale, inv), w, true);
+            codes[k] = (uint32_t)w;
+          }
+          *reinterpret_cast<u32x2*>(pool + kDim * s + 32 * i + 8 * c) = codes;
+        }
+      }
+      if (lane == 0) *scale_at = scale;
+      return;
+    }
+  }
   uint32_t x[kPage];  // dims 2 lane, 2 lane + 1 of each token
 #pragma unroll
   for (int s = 0; s < kPage; ++s)
@@ -154,25 +229,56 @@ __device__ void append_page(const AppendRowsArgs& a, int page, int g, bool is_v,
       }
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = r[i];
-  } else {
+    return;
+  }
+  u32x4 old[2] = {};  // V: the lane's two rows of sixteen slots
+  if (FP8 && is_v) {
+    if (s1 - s0 < kPage) {
+#pragma unroll
+      for (int d = 0; d < 2; ++d) old[d] = ld16(pool + (2 * lane + d) * kPage);
+    }
+    uint32_t most = 0;
+#pragma unroll
+    for (int s = 0; s < kPage; ++s) most = larger(most, sizes(x[s]));
+    most = both_places(most) | both_places(sizes(x[0])) << 16;
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) most = larger(most, (uint32_t)__shfl_xor((int)most, m));
+    const float scale = one_scale(s0 == 0, most >> 16, most & 0xFFFFu, scale_at);
+    if (scale > 0.0f) {
+      const float inv = 1.0f / scale;
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        u32x4 r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float q[4];
+          uint32_t keep = 0;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int s = 4 * i + k;
+            q[k] = quotient(d ? hi_bf16(x[s]) : lo_bf16(x[s]), scale, inv);
+            if (s < s0 || s >= s1) keep |= 0xFFu << (8 * k);
+          }
+          int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+          w = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
+          r[i] = ((uint32_t)w & ~keep) | (old[d][i] & keep);
+        }
+        *reinterpret_cast<u32x4*>(pool + (2 * lane + d) * kPage) = r;
+      }
+      if (lane == 0) *scale_at = scale;
+      return;
+    }
+  }
+  if constexpr (FP8) {
     // The E4M3 append rule, token after token, in float32: the token at slot 0
     // sets scale = amax / 28; a later one beyond 448 scale re-encodes the slots
     // before it to amax / 28; each is stored as RNE(x / scale).
-    uint8_t* pool = static_cast<uint8_t*>(is_v ? a.v_pool : a.k_pool) + head * (kPage * kDim);
-    float* scale_at = (is_v ? a.v_scale : a.k_scale) + (size_t)page * H + g;
     uint16_t* codes = lds + lane;  // [slot][lane]: the code pairs of this lane's dims
     if (is_v) {
-      uint32_t w[8];
-#pragma unroll
-      for (int d = 0; d < 2; ++d) {
-        const u32x4 r = ld16(pool + (2 * lane + d) * kPage);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[4 * d + i] = r[i];
-      }
 #pragma unroll
       for (int s = 0; s < kPage; ++s)
-        codes[64 * s] = (uint16_t)((w[s >> 2] >> (8 * (s & 3)) & 0xFFu) |
-                                   (w[4 + (s >> 2)] >> (8 * (s & 3)) & 0xFFu) << 8);
+        codes[64 * s] = (uint16_t)((old[0][s >> 2] >> (8 * (s & 3)) & 0xFFu) |
+                                   (old[1][s >> 2] >> (8 * (s & 3)) & 0xFFu) << 8);
     } else {
       for (int s = 0; s < s0; ++s) codes[64 * s] = reinterpret_cast<uint16_t*>(pool)[64 * s + lane];
     }
@@ -180,8 +286,7 @@ __device__ void append_page(const AppendRowsArgs& a, int page, int g, bool is_v,
 #pragma unroll
     for (int s = 0; s < kPage; ++s) {
       if (s < s0 || s >= s1) continue;
-      const float x0 = __builtin_bit_cast(float, x[s] << 16);
-      const float x1 = __builtin_bit_cast(float, x[s] & 0xFFFF0000u);
+      const float x0 = lo_bf16(x[s]), x1 = hi_bf16(x[s]);
       const float amax = wave_max(fmaxf(fabsf(x0), fabsf(x1)));
       if (s == 0) {
         scale = amax > 0.0f ? amax / 28.0f : 1.0f;
@@ -189,8 +294,8 @@ __device__ void append_page(const AppendRowsArgs& a, int page, int g, bool is_v,
         const float fresh = amax / 28.0f;
 #pragma unroll 1
         for (int t = 0; t < s; ++t) {
-          const f32x2 old = e4m3_values(codes[64 * t]);
-          codes[64 * t] = (uint16_t)e4m3_pair(old.x * scale / fresh, old.y * scale / fresh);
+          const f32x2 was = e4m3_values(codes[64 * t]);
+          codes[64 * t] = (uint16_t)e4m3_pair(was.x * scale / fresh, was.y * scale / fresh);
         }
         scale = fresh;
       }
@@ -215,11 +320,11 @@ __device__ void append_page(const AppendRowsArgs& a, int page, int g, bool is_v,
 // One workgroup per route: the check; the plan of its pages, or with DIRECT the
 // pages themselves; the route's new end.
 template <bool FP8, bool DIRECT>
-__global__ __launch_bounds__(512) void append_plan_kernel(AppendRowsArgs a) {
-  __shared__ uint16_t lds[FP8 && DIRECT ? 8 * kPage * 64 : 1];
+__global__ __launch_bounds__(1024) void append_plan_kernel(AppendRowsArgs a) {
+  __shared__ uint16_t lds[FP8 && DIRECT ? 16 * kPage * 64 : 1];
   const int r = blockIdx.x;
   int flag = 0;
-  const int j0 = append_check(a, r, flag);
+  const int j0 = append_check<!DIRECT>(a, r, flag);
   if (threadIdx.x == 0 && flag) atomicOr(a.err_flags, flag);
   if (!DIRECT && threadIdx.x == 0) a.plan[4 * r] = j0;
   if (j0 < 0) return;
@@ -228,7 +333,7 @@ __global__ __launch_bounds__(512) void append_plan_kernel(AppendRowsArgs a) {
   if constexpr (DIRECT) {
     const int p0 = j0 / kPage, pages = (j0 + n - 1) / kPage - p0 + 1, w = threadIdx.x >> 6;
     const int units = 2 * a.num_kv_heads;
-    for (int64_t u = w; u < (int64_t)pages * units; u += 8) {
+    for (int64_t u = w; u < (int64_t)pages * units; u += 16) {
       const int p = p0 + (int)(u / units), k = (int)(u % units);
       const int s0 = p == p0 ? j0 % kPage : 0;
       const int s1 = min(kPage, j0 + n - p * kPage);
@@ -1470,9 +1575,9 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
 hipError_t launch_append_rows(const AppendRowsArgs& a, bool fp8, hipStream_t stream) {
   if (a.num_entries <= 256) {
     if (fp8)
-      append_plan_kernel<true, true><<<a.num_routes, 512, 0, stream>>>(a);
+      append_plan_kernel<true, true><<<a.num_routes, 1024, 0, stream>>>(a);
     else
-      append_plan_kernel<false, true><<<a.num_routes, 512, 0, stream>>>(a);
+      append_plan_kernel<false, true><<<a.num_routes, 1024, 0, stream>>>(a);
     return hipGetLastError();
   }
   append_plan_kernel<false, false><<<a.num_routes, 512, 0, stream>>>(a);
