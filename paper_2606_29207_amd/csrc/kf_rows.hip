@@ -1099,17 +1099,20 @@ struct Work {
     asm volatile("" ::: "memory");
   }
 
-  // fp8: the wave's own chunks from the ring into a tile.
-  __device__ __forceinline__ void widen_k(const char* __restrict__ ring, char* __restrict__ lk) {
+  // fp8: the lane's chunk of a ring widened into a tile.
+  __device__ __forceinline__ u32x4 chunk(const char* __restrict__ ring) const {
+    return *(reinterpret_cast<const u32x4*>(ring) + tid);
+  }
+  __device__ __forceinline__ void widen_k(u32x4 x, char* __restrict__ lk) {
     const int t7 = tid & 127, row = 16 * (tid >> 7) + (t7 >> 3);
     u32x4 lo, hi;
-    widen(*(reinterpret_cast<const u32x4*>(ring) + tid), lo, hi);
+    widen(x, lo, hi);
     *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7))) = lo;
     *reinterpret_cast<u32x4*>(lk + k_at(row, 2 * (t7 & 7) + 1)) = hi;
   }
-  __device__ __forceinline__ void widen_v(const char* __restrict__ ring, char* __restrict__ lv) {
+  __device__ __forceinline__ void widen_v(u32x4 x, char* __restrict__ lv) {
     u32x4 lo, hi;
-    widen(*(reinterpret_cast<const u32x4*>(ring) + tid), lo, hi);
+    widen(x, lo, hi);
     *reinterpret_cast<u32x4*>(lv + v_at(tid >> 7, tid & 127, 0)) = lo;
     *reinterpret_cast<u32x4*>(lv + v_at(tid >> 7, tid & 127, 1)) = hi;
   }
@@ -1123,7 +1126,7 @@ struct Work {
   // Works on tile t, whose scores are in s and whose V is in lv; the next tile's
   // K is in lk.
   __device__ __forceinline__ void work(const Tile& t, const char* __restrict__ lk,
-                                       char* __restrict__ lv, const float* __restrict__ ls) {
+                                       char* __restrict__ lv, f32x4 scales) {
     ++steps;
     bool odd = false;
     if (__builtin_expect(
@@ -1142,11 +1145,18 @@ struct Work {
       }
       return;
     }
-    f32x4 scales = {1.0f, 1.0f, 1.0f, 1.0f};
-    if constexpr (FP8) {  // the pages' scales into the scores, in base 2
-      if (!(t.kind & kDraft)) scales = *reinterpret_cast<const f32x4*>(ls + 4 * wave);
+    // what a score is multiplied by, page by page: c, with the K scale of an fp8 page
+    float cs[2] = {c, c};
+    if constexpr (FP8) {
+      if (TREE && (t.kind & kDraft)) scales = f32x4{1.0f, 1.0f, 1.0f, 1.0f};
+      cs[0] *= scales[0];
+      cs[1] *= scales[1];
+      if (__builtin_expect(__ballot(!(cs[0] > 0.0f && cs[1] > 0.0f)) != 0, 0)) {
+        // the largest score is not the largest product's: multiply first
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] *= c * scales[i >> 3];
+        for (int i = 0; i < 16; ++i) s[i] *= cs[i >> 3];
+        cs[0] = cs[1] = 1.0f;
+      }
     }
     const int half = lane >> 5;
     uint32_t sees = ~0u;
@@ -1165,11 +1175,19 @@ struct Work {
     u32x4 k[8], v[8];
     load_k(lk, ka, k);
     if constexpr (!FP8) load_v(lv, lane, v);  // (fp8 has no registers for it)
-    float top = neg_inf();
+    float top = neg_inf(), top1 = neg_inf();
+    if constexpr (FP8) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
-    top = max_halves(top);
-    if constexpr (!FP8) top *= c;
+      for (int i = 0; i < 8; ++i) {
+        top = fmaxf(top, s[i]);
+        top1 = fmaxf(top1, s[8 + i]);
+      }
+      top = max_halves(fmaxf(top * cs[0], top1 * cs[1]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
+      top = max_halves(top) * c;
+    }
     // The reference moves only when a score exceeds it by 2^8: exp2 and the sums
     // stay in range, and most tiles leave the outputs unscaled.
     if (__builtin_expect(__ballot(top > st.m + 8.0f) != 0, 0)) {
@@ -1190,8 +1208,8 @@ struct Work {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float x0 = s[8 * page + 2 * i], x1 = s[8 * page + 2 * i + 1];
-        const float e0 = FP8 ? exp2_fast(x0 - m) : exp2_fast(__builtin_fmaf(x0, c, -m));
-        const float e1 = FP8 ? exp2_fast(x1 - m) : exp2_fast(__builtin_fmaf(x1, c, -m));
+        const float e0 = exp2_fast(__builtin_fmaf(x0, cs[page], -m));
+        const float e1 = exp2_fast(__builtin_fmaf(x1, cs[page], -m));
         st.l += e0 + e1;
         p[page][i] = FP8 ? pack_bf16(e0 * scales[2 + page], e1 * scales[2 + page])
                          : pack_bf16(e0, e1);
@@ -1241,7 +1259,7 @@ struct Work {
     start(t3, pages, a.v_pool, voff, v3);
     start(t4, pg4, a.k_pool, koff, k0);
     pages = pg4;
-    work(t, lk, lv, nullptr);
+    work(t, lk, lv, f32x4{1.0f, 1.0f, 1.0f, 1.0f});
     if (TREE && (t2.kind & kDraft)) draft_k(a, row0, t2.pos0, n_rows, g, tid, k2);
     if (TREE && (t1.kind & kDraft)) draft_v(a, row0, t1.pos0, n_rows, g, tid, v1);
     t = t4;
@@ -1259,8 +1277,9 @@ struct Work {
                                         float* __restrict__ s0) {
     Pages pg4;
     const Tile t4 = take(pg4);
-    lds_barrier();
-    work(t, lk, lv, s0);
+    // the rings are each wave's own: what stood in t's places has been read
+    const f32x4 scales = *reinterpret_cast<const f32x4*>(s0 + 4 * wave);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     start(t4, pg4, a.k_pool, koff, rk0);
     start(t4, pg4, a.v_pool, koff, rv0);
     start_scales(t4, pg4, s0);
@@ -1268,14 +1287,17 @@ struct Work {
       wait<6>();
     else
       wait<0>();
+    const u32x4 ck = chunk(rk2), cv = chunk(rv1);
+    lds_barrier();
     if (TREE && (t2.kind & kDraft))
       draft_k(a, row0, t2.pos0, n_rows, g, tid, k2);
     else if (t2.left > 0)
-      widen_k(rk2, k2);
+      widen_k(ck, k2);
     if (TREE && (t1.kind & kDraft))
       draft_v(a, row0, t1.pos0, n_rows, g, tid, v1);
     else if (t1.left > 0)
-      widen_v(rv1, v1);
+      widen_v(cv, v1);
+    work(t, lk, lv, scales);
     t = t4;
     return t1.left > 0;
   }
@@ -1469,13 +1491,13 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         draft_k(a, row0, t0.pos0, n_rows, g, tid, k0);
         draft_v(a, row0, t0.pos0, n_rows, g, tid, v0);
       } else {
-        w.widen_k(k2, k0);
-        w.widen_v(v2, v0);
+        w.widen_k(w.chunk(k2), k0);
+        w.widen_v(w.chunk(v2), v0);
       }
       if (TREE && (t1.kind & kDraft))
         draft_k(a, row0, t1.pos0, n_rows, g, tid, k1);
       else if (t1.left > 0)
-        w.widen_k(k3, k1);
+        w.widen_k(w.chunk(k3), k1);
       lds_barrier();
       w.first_scores(k0);
       while (w.step8(t0, t1, t2, t3, k1, v0, k0, v1, k4, v3, k2, v2, s0) &&
