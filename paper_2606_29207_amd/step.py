@@ -4,8 +4,9 @@ Holds the query batch, the paged K/V pools, the routing table (token-range
 routes and page ids) and the output buffers as torch device tensors, and runs
 one decode step as the paper orders it (Section 3.2, steps 3-4; Section 5.1):
 the tail routes append the step's K/V token, every route computes its partial,
-and the partials of each sequence are merged.  Marshalling only: the three
-calls are the library's HIP kernels, enqueued on the current stream.  Their
+and the partials of each sequence are merged.  Prompts, drafted trees and
+accepted rows go over the same buffers (append_rows, prompt_attn, tree_attn).
+Marshalling only: the calls are the library's HIP kernels, enqueued on the current stream.  Their
 arguments are checked and marshalled once, when the state is built.
 """
 from __future__ import annotations
@@ -189,6 +190,50 @@ class DecodeState:
         self._qf_tail_done.record(self.stream_b)
         cur.wait_event(self._qf_tail_done)
         self.merge(cur)
+
+    # ------------------------------------------------- operators on whole rows
+    def append_rows(self, k_rows: torch.Tensor, v_rows: torch.Tensor,
+                    route_entry_begin: torch.Tensor, row_list: torch.Tensor | None = None,
+                    stream=None):
+        """Several tokens per route into the cache (kf_kv_append_rows): a prompt's
+        K/V before prompt_attn, or the accepted rows of a tree after tree_attn."""
+        with torch.cuda.stream(stream):   # (None: the current stream)
+            kf.kv_append_rows(self.shape, self.k_pool, self.v_pool, k_rows, v_rows, self.routes,
+                              route_entry_begin, self.page_ids, self.err_flags, row_list,
+                              self.k_scale, self.v_scale)
+
+    def _rows_buffers(self, q: torch.Tensor):
+        n = q.shape[0]
+        return (torch.empty((n, self.shape.num_q_heads, kf.HEAD_DIM), dtype=torch.bfloat16,
+                            device=self.device),
+                torch.empty((n, self.shape.num_q_heads), dtype=torch.float32, device=self.device),
+                kf.alloc_rows_workspace(self.shape, n, self.device))
+
+    def prompt_attn(self, q: torch.Tensor, first_pos: torch.Tensor, seq_row_begin: torch.Tensor,
+                    stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+        """Causal attention of packed prompt rows over this state's cache
+        (kf_prompt_attn), their own K/V appended before.  Returns out bf16
+        [N, Hq, 128] and lse float32 [N, Hq]."""
+        with torch.cuda.stream(stream):
+            out, lse, ws = self._rows_buffers(q)
+            kf.prompt_attn(self.shape, q, first_pos, self.k_pool, self.v_pool, self.routes,
+                           self.max_pages_per_route, self.page_ids, self.seq_route_begin,
+                           seq_row_begin, out, lse, ws, self.err_flags, self.k_scale,
+                           self.v_scale)
+        return out, lse
+
+    def tree_attn(self, q: torch.Tensor, k_draft: torch.Tensor, v_draft: torch.Tensor,
+                  tree_mask: torch.Tensor, seq_row_begin: torch.Tensor,
+                  stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+        """Attention of drafted trees over this state's cache and their own
+        ancestors (kf_tree_attn).  Returns out and lse as prompt_attn."""
+        with torch.cuda.stream(stream):
+            out, lse, ws = self._rows_buffers(q)
+            kf.tree_attn(self.shape, q, k_draft, v_draft, tree_mask, self.k_pool, self.v_pool,
+                         self.routes, self.max_pages_per_route, self.page_ids,
+                         self.seq_route_begin, seq_row_begin, out, lse, ws, self.err_flags,
+                         self.k_scale, self.v_scale)
+        return out, lse
 
     def flags(self) -> int:
         return int(self.err_flags.item())
