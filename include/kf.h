@@ -361,7 +361,7 @@ int kf_decode_step_no_alloc(const kf_shape* shape, const void* q, void* k_pool, 
  * token, in this order, would leave them (fp8 pools: its E4M3 rule), and
  * routes[r].tok_end grows by the route's entries.  route_entry_begin has
  * num_routes + 1 values; num_entries bounds them (the length of row_list; at
- * most num_rows without one).
+ * most num_rows without one).  At most 65535 routes in a call.
  * A route takes all of its rows or none.  Device checks (flag, that route
  * unchanged): its row of the table (0 <= seq < num_seqs, tok_end >= tok_begin,
  * page_base >= 0, pages in page_ids), its reserved pages (KF_EFLAG_TAIL_FULL),

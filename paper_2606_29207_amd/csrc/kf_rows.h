@@ -8,12 +8,25 @@ namespace kf {
 
 constexpr int kRowTile = 128;     // (row, query head) pairs of one KV head per workgroup
 constexpr int kKeyTile = 32;      // tokens per step of a workgroup: two pages
-constexpr int kMaxRecsPerCu = 8;  // records of split work items per compute unit
-constexpr int kMinPart = 4;       // key tiles of a part at least
-constexpr int kUnplannedSteps = 24;  // mean steps of a workgroup up to which a launch needs no plan
+constexpr int kMaxRecsPerCu = 4;  // records of split work items per compute unit (twice and four
+                                  // times as many: the same within 0.5 %, and 68 MB each time)
+constexpr int kMinPart = 4;       // key tiles of a part at least: 8 drafted tokens over 700 tokens
+                                  // 15.4 us, 18.2 in parts of 8; over 300 14.3 in parts of 2, but
+                                  // 64 rows over 1000 26.1 instead of 21.3
+constexpr int kMeanSteps = 24;    // steps of a workgroup up to which a launch needs no plan:
+constexpr int kMostSteps = 96;    // mean, and at most
 constexpr int kSplitSlots = 4;    // (row tile, KV head) pairs per resident workgroup from which on
-                                  // a launch splits none
+                                  // a launch splits none (2, 4 and 8: prompts of 6K .. 16K tokens
+                                  // the same within 1 %; 8 packed ones 145, 144 and 148 us)
+constexpr int64_t kMaxWgs = 0xFFFFFF;  // of 256 threads, in a launch: 32 bits of threads
 constexpr int kCombineWgsPerSlot = 8;  // workgroups of the combine per resident workgroup at most
+                                       // (2 and 32: the same)
+// One launch appends up to kDirectEntries entries, and up to kDirectMean a route (a
+// workgroup each): 1 row 7.3 us, 8.7 with a plan; a row for each of 16 routes 7.4 and
+// 9.0, of 64 7.7 and 9.7, three for each of 16 9.1 and 10.1 (fp8); but 16 rows of one
+// route 11.1 and 9.1, two for each of 64 12.0 and 10.6 (fp8).
+constexpr int kDirectEntries = 64;
+constexpr int kDirectMean = 3;
 
 // ------------------------------------------------------------------- append
 struct AppendRowsArgs {
@@ -51,7 +64,8 @@ struct RowsItem {
 
 // The parts of one split row tile.
 struct RowsSplit {
-  int32_t seq, tile, rec, parts;
+  int32_t tile, rec, parts, row0, rows;
+  int32_t pad[3];
 };
 
 struct RowsArgs {
@@ -78,7 +92,8 @@ struct RowsArgs {
   int32_t head_major;
   float scale_log2;
   // workspace
-  int32_t* head;        // [0] items (-1: every row becomes NaN), [1] split tiles
+  int32_t* head;        // [0] items (-1: every row becomes NaN), [1] split tiles,
+                        // [2] (row, head) pairs of the largest
   int32_t* seq_tiles;   // [num_seqs + 1] first row tile of each sequence
   int32_t* seq_info;    // [num_seqs][4] tokens, smallest tok_begin, bad
   RowsItem* items;
@@ -103,7 +118,8 @@ RowsLayout rows_layout(int32_t num_rows, int32_t num_seqs, int32_t num_kv_heads,
 
 // Parts per row tile of a launch that runs without a plan, 0 with one.
 int32_t unplanned_parts(const RowsLayout& l, int32_t num_seqs, int32_t num_kv_heads,
-                        int32_t num_routes, int32_t num_page_ids, int64_t slots);
+                        int32_t num_routes, int32_t num_page_ids, int32_t max_pages_per_route,
+                        int64_t slots);
 
 hipError_t launch_rows_attn(const RowsArgs& a, bool fp8, bool tree, hipStream_t stream);
 

@@ -416,7 +416,7 @@ constexpr int kPlanSeqs = 1024;
 template <bool TREE>
 __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
   __shared__ unsigned long long s_work;
-  __shared__ int s_most, s_recs, s_parts, s_splits;
+  __shared__ int s_most, s_recs, s_parts, s_splits, s_pairs;
   __shared__ int s_count[64], s_scan[16];
   __shared__ unsigned long long l_tokens[kPlanSeqs];
   __shared__ int l_tiles[kPlanSeqs + 1], l_info[4 * kPlanSeqs], l_begin[kPlanSeqs + 1];
@@ -456,6 +456,7 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
     if (tid == 0) {
       a.head[0] = -1;
       a.head[1] = 0;
+      a.head[2] = 1;
       atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
     }
     return;
@@ -585,10 +586,12 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
     const unsigned long long share = (s_work * a.num_kv_heads + a.slots - 1) / a.slots;
     cap = (int)min((unsigned long long)most, max(share, (unsigned long long)kMinPart));
     // An even share per workgroup, in one round.  Where that leaves more parts than
-    // workgroups (tiles of different lengths), halves of it pack better: agentic
-    // trees 817 -> 746 us; thirds and quarters the same, and with as many tiles as
-    // workgroups (multi-head prompts) halves cost 94 -> 131.
-    bool halved = (int64_t)T * a.num_kv_heads >= a.slots;
+    // workgroups (tiles of different lengths), smaller ones pack better: 48 agentic
+    // trees 817 us with the share itself, 736 with 1/2 of it, 688 with 5/8, 694 with
+    // 11/16, 699 with 3/4; 40 short prompts over 1K .. 30K tokens 359 (9/16) and 345
+    // (5/8).  With as many tiles as workgroups (multi-head prompts) halves cost
+    // 94 -> 131.
+    bool cut = (int64_t)T * a.num_kv_heads >= a.slots;
     for (;;) {  // until the records of split tiles fit
       __syncthreads();
       if (tid == 0) s_recs = s_parts = 0;
@@ -614,17 +617,17 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
       }
       __syncthreads();
       const bool more = (int64_t)s_parts * a.num_kv_heads > a.slots;
-      if (!halved && more && cap > kMinPart)
-        cap = max(cap / 2, kMinPart);
+      if (!cut && more && cap > kMinPart)
+        cap = max((int)((int64_t)cap * 5 / 8), kMinPart);
       else if (s_recs <= a.max_recs)
         break;
       else
         cap += cap / 4 + 1;
-      halved = true;
+      cut = true;
     }
   }
   __syncthreads();
-  if (tid == 0) s_recs = 0, s_splits = 0;
+  if (tid == 0) s_recs = 0, s_splits = 0, s_pairs = 1;
   const int per = max(1, min(cap, most));
   // by size of their parts, largest first
   auto place = [&](int part) { return 63 - (int)((int64_t)part * 63 / per); };
@@ -664,7 +667,10 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
     it.pad[0] = it.pad[1] = 0;
     if (parts > 1) {
       it.rec = atomicAdd(&s_recs, parts);
-      a.splits[atomicAdd(&s_splits, 1)] = RowsSplit{b, it.tile, it.rec, parts};
+      const int64_t pairs = (int64_t)it.rows * a.group - (int64_t)it.tile * kRowTile;
+      a.splits[atomicAdd(&s_splits, 1)] =
+          RowsSplit{it.tile, it.rec, parts, it.row0, it.rows, {0, 0, 0}};
+      atomicMax(&s_pairs, (int)min(pairs, (int64_t)kRowTile));
     }
     for (int p = 0; p < parts; ++p) {
       it.key0 = (int)((int64_t)k * p / parts);
@@ -674,7 +680,10 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
     }
   }
   __syncthreads();
-  if (tid == 0) a.head[1] = s_splits;
+  if (tid == 0) {
+    a.head[1] = s_splits;
+    a.head[2] = s_pairs;
+  }
 }
 
 // Without a plan (a.parts > 0: launches of up to 64 sequences and little work):
@@ -1578,60 +1587,72 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   if (half == 0) a.lse[at] = l == 0.0f ? neg_inf() : (st.m + __log2f(l)) * kLn2;
 }
 
-// The parts of a split row tile into its outputs: a wave per (row, head), the
-// records of four parts on their way at a time.
+// The parts of a split row tile into its outputs: a wave per (row, head), a lane
+// per part's maximum and sum, then the parts' outputs, eight on their way at a time.
 __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
   const int H = a.num_kv_heads, G = a.group;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const int splits = a.parts > 0 ? a.max_tiles : fixed(a.head)[1];
+  const bool planned = a.parts == 0;
+  const int splits = planned ? fixed(a.head)[1] : a.max_tiles;
+  const int pairs = planned ? fixed(a.head)[2] : a.rec_rows;  // of a tile at most
   const size_t stride = (size_t)H * a.rec_rows;
-  for (int64_t u = (int64_t)blockIdx.x * 4 + wave; u < (int64_t)splits * H * a.rec_rows;
-       u += (int64_t)gridDim.x * 4) {
-    const int rm = (int)(u % a.rec_rows), g = (int)(u / a.rec_rows % H);
-    const int split = (int)(u / stride);
+  // (records per compute unit and workgroups are few: all of this fits 32 bits)
+  for (uint32_t u = blockIdx.x * 4 + wave; u < (uint32_t)splits * H * pairs; u += gridDim.x * 4) {
+    const int rm = (int)(u % (uint32_t)pairs), g = (int)(u / (uint32_t)pairs % (uint32_t)H);
+    const int split = uniform((int)(u / ((uint32_t)pairs * (uint32_t)H)));
     RowsSplit sp;
-    int row0, rows;
-    if (a.parts > 0) {
+    if (planned) {
+      const auto* at = fixed(reinterpret_cast<const int32_t*>(a.splits + split));
+      sp.tile = at[0];
+      sp.rec = at[1];
+      sp.parts = at[2];
+      sp.row0 = at[3];
+      sp.rows = at[4];
+    } else {
+      int b;
       sp.rec = split * a.parts;
       sp.parts = a.parts;
-      if (find_tile(a, split, lane, sp.seq, sp.tile, row0, rows) <= 0) return;
-    } else {
-      sp = a.splits[split];
-      row0 = a.seq_row_begin[sp.seq];
-      rows = a.seq_row_begin[sp.seq + 1] - row0;
+      if (find_tile(a, split, lane, b, sp.tile, sp.row0, sp.rows) <= 0) return;
     }
-    const int m = sp.tile * kRowTile + rm;
-    if (m >= rows * G) continue;
+    const int row0 = sp.row0, m = sp.tile * kRowTile + rm;
+    if (m >= sp.rows * G) continue;
     const size_t rec = ((size_t)sp.rec * H + g) * a.rec_rows + rm;
     const float* ml = a.rec_ml + 2 * rec;
     const f32x2* ro = reinterpret_cast<const f32x2*>(a.rec_o + rec * kDim) + lane;
     float ref = neg_inf();  // the largest maximum so far
     float l = 0.0f;
     f32x2 o = {0.0f, 0.0f};
-    for (int p = 0; p < sp.parts; p += 4) {
-      f32x2 x[4], y[4];
+    for (int p = 0; p < sp.parts; p += 64) {
+      const int n = min(64, sp.parts - p);
+      f32x2 y[8];
+      auto load = [&](int i0) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int q = min(p + i, sp.parts - 1);
-        x[i] = *reinterpret_cast<const f32x2*>(ml + 2 * q * stride);
-        y[i] = ro[q * stride * (kDim / 2)];
-      }
-      float top = ref;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top = fmaxf(top, x[i].x);
+        for (int i = 0; i < 8; ++i) y[i] = ro[(size_t)(p + min(i0 + i, n - 1)) * stride * (kDim / 2)];
+      };
+      load(0);
+      f32x2 x = {neg_inf(), 0.0f};  // of part p + lane
+      if (lane < n) x = *reinterpret_cast<const f32x2*>(ml + (size_t)(p + lane) * stride * 2);
+      const float top = fmaxf(ref, wave_max(x.x));
       const float base = top == neg_inf() ? 0.0f : top;
-      const float f = exp2_fast(ref - base);
+      const float f = exp2_fast(ref - base), e = exp2_fast(x.x - base);
       ref = top;
-      l *= f;
+      float sum = e * x.y;
+#pragma unroll
+      for (int k = 32; k >= 1; k >>= 1) sum += __shfl_xor(sum, k);
+      l = __builtin_fmaf(l, f, sum);
       o.x *= f;
       o.y *= f;
+      for (int i0 = 0;;) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (p + i >= sp.parts) continue;
-        const float e = exp2_fast(x[i].x - base);
-        l = __builtin_fmaf(e, x[i].y, l);
-        o.x = __builtin_fmaf(e, y[i].x, o.x);
-        o.y = __builtin_fmaf(e, y[i].y, o.y);
+        for (int i = 0; i < 8; ++i) {
+          if (i0 + i >= n) continue;
+          const float w = __builtin_bit_cast(
+              float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, e), i0 + i));
+          o.x = __builtin_fmaf(w, y[i].x, o.x);
+          o.y = __builtin_fmaf(w, y[i].y, o.y);
+        }
+        if ((i0 += 8) >= n) break;
+        load(i0);
       }
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -1644,7 +1665,7 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
 }  // namespace
 
 hipError_t launch_append_rows(const AppendRowsArgs& a, bool fp8, hipStream_t stream) {
-  if (a.num_entries <= 256) {
+  if (a.num_entries <= kDirectEntries && a.num_entries <= kDirectMean * a.num_routes) {
     if (fp8)
       append_plan_kernel<true, true><<<a.num_routes, 1024, 0, stream>>>(a);
     else

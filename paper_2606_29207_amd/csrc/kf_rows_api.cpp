@@ -30,13 +30,14 @@ RowsLayout rows_layout(int32_t num_rows, int32_t num_seqs, int32_t num_kv_heads,
                        int64_t cus) {
   RowsLayout l{};
   if (num_kv_heads > kMaxLaunchRoutes) return l;
-  // ceil(n_b G / kRowTile) tiles of each sequence that has rows
+  // ceil(n_b G / kRowTile) tiles of each sequence that has rows (one, and so a
+  // grid, where there are none)
   const int64_t pairs = (int64_t)num_rows * group;
   if (pairs > INT32_MAX - kRowTile) return l;
-  const int64_t tiles = pairs / kRowTile + std::min(num_seqs, num_rows);
+  const int64_t tiles = pairs / kRowTile + std::max(1, std::min(num_seqs, num_rows));
   int64_t recs = kMaxRecsPerCu * cus / num_kv_heads;
   if (recs < 2) recs = 0;
-  if ((tiles + recs) * num_kv_heads > INT32_MAX) return l;
+  if ((tiles + recs) * num_kv_heads > kMaxWgs) return l;
   l.max_tiles = (int32_t)tiles;
   l.max_recs = (int32_t)recs;
   l.rec_rows = (int32_t)std::min<int64_t>(kRowTile, (pairs + 31) / 32 * 32);
@@ -51,19 +52,29 @@ RowsLayout rows_layout(int32_t num_rows, int32_t num_seqs, int32_t num_kv_heads,
   return l;
 }
 
-// The plan's launch costs about as much as eight steps of a workgroup.  Where
-// the row tiles leave workgroups free and an even split of every tile comes to
-// few steps, sequences of different lengths cost less than that, and every
-// workgroup finds its own tile.
+// A plan and the combine of its parts cost 15 to 20 us.  Where the row tiles leave
+// workgroups free and an even split of every tile comes to few steps (0.7 us each),
+// on the mean or for the longest sequence, sequences of different lengths cost less
+// than that, and every workgroup finds its own tile.  With a plan and without, us:
+// 64 rows 18.1 and 10.0; 8 drafted tokens over 2K tokens 27.9 and 18.1; 48 of those
+// over 300 .. 1500 tokens 69 and 49, over 800 .. 2500 95 and 76 (up to kMostSteps).
 int32_t unplanned_parts(const RowsLayout& l, int32_t num_seqs, int32_t num_kv_heads,
-                        int32_t num_routes, int32_t num_page_ids, int64_t slots) {
+                        int32_t num_routes, int32_t num_page_ids, int32_t max_pages_per_route,
+                        int64_t slots) {
   const int64_t items = (int64_t)l.max_tiles * num_kv_heads;
   if (num_seqs > 64 || num_seqs < 1 || items > slots) return 0;
   // mean key tiles of a sequence, as the page table tells it
   const int64_t keys = ((int64_t)num_page_ids * KF_PAGE_SIZE / kKeyTile + num_routes) / num_seqs + 1;
   int64_t parts = std::min(slots / items, (keys + kMinPart - 1) / kMinPart);
+  // steps go down with the parts, the combine's turns up: 8 drafted tokens over 8K
+  // tokens, 8 KV heads, 24.7 us in parts of kMinPart, 21.9 in 2 sqrt(keys) parts,
+  // one KV head over 30K 36 and 29.6
+  parts = std::min(parts, (int64_t)(2.0 * sqrt((double)keys)));
   parts = std::max<int64_t>(1, std::min<int64_t>(parts, l.max_recs / l.max_tiles));
-  return keys <= kUnplannedSteps * parts ? (int32_t)parts : 0;
+  // the longest sequence's at most
+  const int64_t most = ((int64_t)max_pages_per_route * KF_PAGE_SIZE / kKeyTile + 1) *
+                       std::max(1, num_routes - num_seqs + 1);
+  return keys <= kMeanSteps * parts || most <= kMostSteps * parts ? (int32_t)parts : 0;
 }
 
 }  // namespace kf
@@ -137,7 +148,7 @@ int prepare_rows(const kf_shape* shape, const void* q, int32_t num_rows, int64_t
   a.rec_rows = l.rec_rows;
   a.slots = (int32_t)(2 * cus);
   a.parts = kf::unplanned_parts(l, shape->num_seqs, shape->num_kv_heads, num_routes,
-                                shape->num_page_ids, a.slots);
+                                shape->num_page_ids, max_pages_per_route, a.slots);
   // the row tiles that num_rows comes to if every row belongs to a sequence
   const int64_t tiles = ((int64_t)num_rows * group + kf::kRowTile - 1) / kf::kRowTile;
   a.may_split = l.max_recs > 1 && tiles * shape->num_kv_heads < kf::kSplitSlots * (int64_t)a.slots;
@@ -176,7 +187,9 @@ int kf_kv_append_rows(const kf_shape* shape, void* k_pool, void* v_pool, float* 
     if (p && !aligned(p, 4)) return KF_ERR_INVALID_ARG;
   // a wave per (page, KV head, K or V); the pages of num_routes routes
   const int64_t tiles = (int64_t)num_entries / KF_PAGE_SIZE + 2 * (int64_t)num_routes;
-  if (tiles * 2 > ((int64_t)INT32_MAX * 4 - 3) / shape->num_kv_heads) return KF_ERR_UNSUPPORTED;
+  if (num_routes > kf::kMaxLaunchRoutes || shape->num_kv_heads > kf::kMaxLaunchRoutes ||
+      tiles * 2 * shape->num_kv_heads > 4 * kf::kMaxWgs)
+    return KF_ERR_UNSUPPORTED;
   if (!workspace || !aligned(workspace, 16) ||
       workspace_bytes < kf_kv_append_rows_workspace_bytes(num_routes))
     return KF_ERR_WORKSPACE;
@@ -220,7 +233,8 @@ int kf_prompt_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64
                    const int32_t* page_ids, const int32_t* seq_route_begin, void* out, float* lse,
                    void* workspace, size_t workspace_bytes, int32_t* err_flags, void* stream) {
   kf::RowsArgs a{};
-  if (num_rows > 0 && (!first_pos || !aligned(first_pos, 4))) return KF_ERR_INVALID_ARG;
+  if (num_rows > 0 && ((shape && shape->num_seqs > 0 && !first_pos) || !aligned(first_pos, 4)))
+    return KF_ERR_INVALID_ARG;
   const int st = prepare_rows(shape, q, num_rows, q_stride, seq_row_begin, k_pool, v_pool, k_scale,
                               v_scale, routes, num_routes, max_pages_per_route, page_ids,
                               seq_route_begin, out, lse, workspace, workspace_bytes, err_flags, a);

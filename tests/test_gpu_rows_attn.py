@@ -85,6 +85,18 @@ def test_rows_of_no_sequence_are_left_alone(gpu):
         assert np.isnan(x[:2]).all() and np.isnan(x[72:]).all()
 
 
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("H", [2, 1500])
+def test_rows_without_any_sequence(gpu, tree, H):
+    c = Cache([], H=H)
+    r = Rows(c, [], 1, tree=tree)
+    r.q = bits(np.random.default_rng(0).standard_normal((3, H, DIM)))
+    if tree:
+        r.k_draft, r.v_draft, r.tree_mask = r.q, r.q, np.zeros(3, np.int64)
+    out, lse, flags = r.gpu()
+    assert flags == 0 and np.isnan(out).all() and np.isnan(lse).all()
+
+
 def test_hidden_tokens_never_reach_a_row(gpu):
     """Infinities and NaN in tokens that a row does not see: same bits."""
     n = 150
