@@ -59,7 +59,8 @@ struct RowsItem {
   int32_t key0, key1;
   int32_t rec;    // record of a split tile's part, -1: the outputs are written
   int32_t row0, rows, first_pos, route0, route1;  // of the sequence
-  int32_t pad[2];
+  int32_t tok_begin, tok_end, page_base;          // of its first route
+  int32_t pad[3];
 };
 
 // The parts of one split row tile.

@@ -629,13 +629,26 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
   __syncthreads();
   if (tid == 0) s_recs = 0, s_splits = 0, s_pairs = 1;
   const int per = max(1, min(cap, most));
-  // by size of their parts, largest first
+  // by size of their parts, largest first; prompts that stay whole sequence after
+  // sequence, the longest first, so that the tiles that run at a time read the same
+  // tokens (64 prompts of 420 tokens 239 -> 226 us, of 128 tokens 66 -> 60)
+  const bool by_seq = !TREE && small && cap >= most;
   auto place = [&](int part) { return 63 - (int)((int64_t)part * 63 / per); };
-  for (int t = tid; t < T; t += 1024) {
-    int b;
-    bool wrong;
-    const int k = look(t, b, wrong), parts = (k + per - 1) / per;
-    atomicAdd(&s_count[place((k + parts - 1) / parts)], parts);
+  int own_size = 0;  // by_seq: of this thread's sequence
+  if (by_seq) {
+    if (tid < B && l_tiles[tid + 1] > l_tiles[tid]) {
+      int b;
+      bool wrong;
+      own_size = search(min(l_tiles[tid + 1], T) - 1, b, wrong);
+      atomicAdd(&s_count[place(own_size)], l_tiles[tid + 1] - l_tiles[tid]);
+    }
+  } else {
+    for (int t = tid; t < T; t += 1024) {
+      int b;
+      bool wrong;
+      const int k = look(t, b, wrong), parts = (k + per - 1) / per;
+      atomicAdd(&s_count[place((k + parts - 1) / parts)], parts);
+    }
   }
   __syncthreads();
   if (w == 0) {
@@ -650,11 +663,18 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
     if (lane == 63) a.head[0] = x;
   }
   __syncthreads();
+  if (by_seq) {
+    // l_tokens: where a sequence's items begin
+    if (own_size > 0)
+      l_tokens[tid] = atomicAdd(&s_count[place(own_size)], l_tiles[tid + 1] - l_tiles[tid]);
+    __syncthreads();
+  }
   for (int t = tid; t < T; t += 1024) {
     int b;
     bool wrong;
     const int k = look(t, b, wrong), parts = (k + per - 1) / per;
-    const int at = atomicAdd(&s_count[place((k + parts - 1) / parts)], parts);
+    const int at = by_seq ? (int)l_tokens[b] + l_tiles[b + 1] - 1 - t
+                          : atomicAdd(&s_count[place((k + parts - 1) / parts)], parts);
     RowsItem it;
     it.seq = wrong ? -1 - b : b;
     it.tile = t - tiles_of[b];
@@ -664,7 +684,14 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
     it.first_pos = TREE ? 0 : pos[b];
     it.route0 = route[b];
     it.route1 = route[b + 1];
-    it.pad[0] = it.pad[1] = 0;
+    it.tok_begin = it.tok_end = it.page_base = 0;
+    if (!wrong && it.route0 < it.route1) {
+      const kf_route& first = a.routes[it.route0];
+      it.tok_begin = first.tok_begin;
+      it.tok_end = first.tok_end;
+      it.page_base = first.page_base;
+    }
+    it.pad[0] = it.pad[1] = it.pad[2] = 0;
     if (parts > 1) {
       it.rec = atomicAdd(&s_recs, parts);
       const int64_t pairs = (int64_t)it.rows * a.group - (int64_t)it.tile * kRowTile;
@@ -797,17 +824,23 @@ __device__ __forceinline__ void walk_on(const RowsArgs& a, Walk& w, int last_pos
   if (w.r < w.r_end) walk_ids(a, w);
 }
 
-// The visible tiles of a sequence's routes; -1 if one of them is bad.
-__device__ __forceinline__ int count_tiles(const RowsArgs& a, int b, int r0, int r1,
-                                           int last_pos, int lane) {
+// The visible tiles of a sequence's routes; -1 if one of them is bad.  The first
+// route of a sequence goes into its item.
+__device__ __forceinline__ int count_tiles(const RowsArgs& a, int b, int r0, int r1, int last_pos,
+                                           int lane, RowsItem& it) {
+  it.tok_begin = it.tok_end = it.page_base = 0;
   int64_t tiles = 0;
   bool bad = r0 < 0 || r1 < r0 || r1 > a.num_routes;
   if (bad) return -1;
-  if (r1 - r0 == 1) {
+  if (r1 > r0) {
     const auto* at = fixed(reinterpret_cast<const int32_t*>(a.routes)) + 6 * (int64_t)r0;
     const int32_t row[6] = {at[0], at[1], at[2], at[3], at[4], at[5]};
-    return route_ok(a, b, row)
-               ? (visible(row[2], row[3], last_pos) + kKeyTile - 1) / kKeyTile : -1;
+    it.tok_begin = row[2];
+    it.tok_end = row[3];
+    it.page_base = row[4];
+    if (r1 - r0 == 1)
+      return route_ok(a, b, row)
+                 ? (visible(row[2], row[3], last_pos) + kKeyTile - 1) / kKeyTile : -1;
   }
   for (int r = r0 + lane; r < r1; r += 64) {
     const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + r);
@@ -1125,12 +1158,18 @@ struct Work {
                                         uint32_t off, char* __restrict__ l) {
     if (__builtin_expect(!paged(t), 0)) return;
     const char* from = static_cast<const char*>(pool);
+    // Its place in LDS, added up anew every time: the sixteen of the bf16 rings, kept,
+    // would cost the scalar registers that the walk needs (16K-token prompts 2200 ->
+    // 2146 us); the eight of fp8 fit (chunks 2790, 2846 with it).
+    int own = 1024 * wave;
+    if constexpr (!FP8) asm volatile("" : "+s"(own));
+    l += own;
     if constexpr (!FP8) {
-      to_lds<TREE>(from + pg.at[0] + off, l + 1024 * wave);
-      to_lds<TREE>(from + pg.at[1] + off, l + 4096 + 1024 * wave);
+      to_lds<TREE>(from + pg.at[0] + off, l);
+      to_lds<TREE>(from + pg.at[1] + off, l + 4096);
     } else {  // two waves a page
       const uint64_t x = pg.at[0], y = pg.at[1];
-      to_lds<TREE>(from + (wave >> 1 ? y : x) + off, l + 1024 * wave);
+      to_lds<TREE>(from + (wave >> 1 ? y : x) + off, l);
     }
   }
   // fp8: the scales of tile t, every wave a copy: K of both pages, then V.
@@ -1394,6 +1433,9 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     it.first_pos = at[7];
     it.route0 = at[8];
     it.route1 = at[9];
+    it.tok_begin = at[10];
+    it.tok_end = at[11];
+    it.page_base = at[12];
     found = items < 0 ? -1 : item < items;
   }
   if (found < 0) {  // no row's sequence is known
@@ -1415,7 +1457,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   const int route0 = it.route0, route1 = it.route1;
   if (a.parts > 0) {
     const int k = TREE && n_rows > KF_MAX_DRAFT
-                      ? -1 : count_tiles(a, b, route0, route1, last_pos, lane);
+                      ? -1 : count_tiles(a, b, route0, route1, last_pos, lane, it);
     if (k < 0) {
       it.seq = -1 - b;
       if (tid == 0) atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
@@ -1451,10 +1493,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   w.c = c0 == 0.0f ? 1.0f : fabsf(c0);
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) {
-    u32x4 x = ld16(a.q + (row0 + row) * a.q_stride + (size_t)h * kDim + 16 * ks + 8 * half);
-    if (c0 < 0.0f) x ^= 0x80008000u;                 // a negative scale turns the row around
-    if (c0 == 0.0f || !mine) x = u32x4{0, 0, 0, 0};  // a zero one makes all scores equal
-    w.q[ks] = x;
+    w.q[ks] = ld16(a.q + (row0 + row) * a.q_stride + (size_t)h * kDim + 16 * ks + 8 * half);
   }
   w.pos = w.pos_min = w.tile_min = INT32_MAX;
   w.last_pos = last_pos;
@@ -1488,7 +1527,28 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     w.scale_of_head = reinterpret_cast<const float*>((lane & 2 ? vs : ks)) + g;
   }
   w.ka = k_at(16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3), half);
-  walk_to(a, w.walk, route0, route1, last_pos, it.key0, lane);
+  // (the pages of the first tile are on their way before q is waited for)
+  // A part that begins in its sequence's first route has that in its item (packed
+  // prompts 183 -> 180 us, one short one 8.9 -> 8.0; fp8's kernel has no registers for
+  // it, chunks 2704 -> 2779).
+  const int see = route0 < route1 ? visible(it.tok_begin, it.tok_end, last_pos) : 0;
+  if (!FP8 && it.key0 < (see + kKeyTile - 1) / kKeyTile) {
+    w.walk.r = route0;
+    w.walk.r_end = route1;
+    w.walk.n = see;
+    w.walk.tb = it.tok_begin;
+    w.walk.base = it.page_base;
+    w.walk.tiles = (see + kKeyTile - 1) / kKeyTile;
+    w.walk.j = it.key0;
+    walk_ids(a, w.walk);
+  } else {
+    walk_to(a, w.walk, route0, route1, last_pos, it.key0, lane);
+  }
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks) {
+    if (c0 < 0.0f) w.q[ks] ^= 0x80008000u;                 // a negative scale turns the row around
+    if (c0 == 0.0f || !mine) w.q[ks] = u32x4{0, 0, 0, 0};  // a zero one makes all scores equal
+  }
   w.left = it.key1 == INT32_MAX ? INT32_MAX : it.key1 - it.key0;
   w.drafts = TREE && it.key1 == INT32_MAX ? n_rows : 0;
 
@@ -1693,8 +1753,9 @@ hipError_t launch_rows_attn(const RowsArgs& a, bool fp8, bool tree, hipStream_t 
       rows_plan_kernel<false><<<1, 1024, 0, stream>>>(a);
     if ((st = hipGetLastError()) != hipSuccess) return st;
   }
-  const uint32_t grid =
-      (uint32_t)(a.parts > 0 ? a.max_tiles * a.parts : a.max_tiles + a.max_recs) * a.num_kv_heads;
+  // (a workgroup without an item still takes its place on a compute unit)
+  const int items = a.parts > 0 ? a.max_tiles * a.parts : a.max_tiles + (a.may_split ? a.max_recs : 0);
+  const uint32_t grid = (uint32_t)items * a.num_kv_heads;
   if (fp8 && tree)
     rows_kernel<true, true><<<grid, 256, 0, stream>>>(a);
   else if (fp8)
