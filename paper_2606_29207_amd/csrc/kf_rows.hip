@@ -60,6 +60,14 @@ __device__ __forceinline__ float wave_max(float x) {
   return x;
 }
 
+// Appends move 512 bytes in and 512 (fp8 256) out per token and KV head, and nothing
+// else: memory bounds them.  A wave takes one page of one KV head, K or V, so that the
+// whole page is written at once (V's rows of sixteen slots turn around in registers)
+// and its fp8 scale is one wave's decision.  16K rows of 8 KV heads (134 MB): 28 us,
+// 4.9 TB/s, a copy's rate; prompts into fp8 pages (260 MB) 58 us, 4.5 TB/s; the plan
+// before them 5 us.  Appends of a few rows are one launch, bound by its chain of
+// loads (7.3 us a pass).
+//
 // One route's check: its tokens before the append, or -1 if it takes no rows (flag
 // says why).  WHOLE: by the workgroup together; else by every wave for itself, for
 // calls of a few rows, which are a chain of loads.
@@ -408,9 +416,12 @@ __device__ __forceinline__ int key_tiles(const RowsArgs& a, int pos, int t, int 
   return (int)((see + kKeyTile - 1) / kKeyTile);
 }
 
-// One workgroup: the row tiles of every sequence, cut into parts of at most
-// `cap` key tiles, largest first.  Up to kPlanSeqs sequences are gathered by a
-// thread per route and kept in LDS.
+// One workgroup: the row tiles of every sequence, cut into parts of at most `cap` key
+// tiles, largest first (the grid is dealt out in order, so the last ones are small).
+// Up to kPlanSeqs sequences are gathered by a thread per route and kept in LDS: 9 to
+// 13 us, a chain of table reads, scans and one write.  More are read from memory by a
+// wave per sequence: trees of 1000 sequences 588 us that way and 504 with a thread per
+// route, of 64 267 and 262.
 constexpr int kPlanSeqs = 1024;
 
 template <bool TREE>
@@ -631,7 +642,8 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
   const int per = max(1, min(cap, most));
   // by size of their parts, largest first; prompts that stay whole sequence after
   // sequence, the longest first, so that the tiles that run at a time read the same
-  // tokens (64 prompts of 420 tokens 239 -> 226 us, of 128 tokens 66 -> 60)
+  // tokens (64 prompts of 420 tokens 249 -> 237 us, of 128 tokens 65 -> 60,
+  // 16 of 100 .. 2000 tokens the same within 2 %)
   const bool by_seq = !TREE && small && cap >= most;
   auto place = [&](int part) { return 63 - (int)((int64_t)part * 63 / per); };
   int own_size = 0;  // by_seq: of this thread's sequence
@@ -1092,6 +1104,23 @@ __device__ __forceinline__ void fill_nan(const RowsArgs& a, int row0, int64_t m0
 // one while the vector units take the other.  bf16 pages go from memory into
 // their tile.  fp8 pages go into rings of their own (4 KiB); the lanes that loaded
 // a chunk widen it into one of two tiles a step before it is needed.
+//
+// One pass over the keys: m is a reference near the largest score so far, l = sum
+// 2^(s - m), o = sum 2^(s - m) v, scores in units of log2; out = o / l, lse =
+// (m + log2 l) ln 2.  l and o are float32; the weights are rounded to bf16 for their
+// product with V, each by at most 2^-8 of it, the output's own rounding, and
+// independently of each other.
+//
+// 128 pairs a workgroup and two workgroups a compute unit: the outputs, scores and
+// operands of 32 pairs a wave take 248 of 256 registers, and the rings 64 of 80 KiB.
+// A step of 64 tokens (one buffer) took 2500 us where this takes 2200, rings of five
+// tiles the same.  16K-token prompt, 32 / 8 heads: 2150 .. 2330 us on different
+// cards, 0.95 .. 1.02 PFLOP/s of its causal work, where the largest plain product
+// reaches 1.28 .. 1.40.  A wave's step issues 106 vector, 85 scalar, 16 LDS and 16
+// matrix instructions; the matrix cores are busy 48 % of the time, LDS, the vector
+// units and the waits for each other share the rest.  fp8 chunks over 32K tokens, 64 /
+// 8 heads: 2690 .. 2800 us, 0.80 PFLOP/s; widening adds the difference.  Trees of few
+// rows wait for memory: 48 over 2K .. 64K tokens, 4.1 GB, 671 us, 6.1 TB/s.
 template <bool FP8, bool TREE>
 struct Work {
   const RowsArgs& a;
@@ -1649,6 +1678,8 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
 
 // The parts of a split row tile into its outputs: a wave per (row, head), a lane
 // per part's maximum and sum, then the parts' outputs, eight on their way at a time.
+// Bound by its chain of loads: 4 us for one tile, 8 us for 48 trees in 2 to 4 parts,
+// 14 .. 18 us for 128 and 256 full tiles in 4 and 2.
 __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
   const int H = a.num_kv_heads, G = a.group;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);

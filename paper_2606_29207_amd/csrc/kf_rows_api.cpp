@@ -71,7 +71,7 @@ int32_t unplanned_parts(const RowsLayout& l, int32_t num_seqs, int32_t num_kv_he
   // one KV head over 30K 36 and 29.6
   parts = std::min(parts, (int64_t)(2.0 * sqrt((double)keys)));
   parts = std::max<int64_t>(1, std::min<int64_t>(parts, l.max_recs / l.max_tiles));
-  // the longest sequence's at most
+  // the longest sequence's at most, where every sequence has a route
   const int64_t most = ((int64_t)max_pages_per_route * KF_PAGE_SIZE / kKeyTile + 1) *
                        std::max(1, num_routes - num_seqs + 1);
   return keys <= kMeanSteps * parts || most <= kMostSteps * parts ? (int32_t)parts : 0;
