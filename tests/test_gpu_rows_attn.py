@@ -303,6 +303,31 @@ def test_planned_splits(gpu, fp8, tree):
     assert_rows(r.gpu(), ref)
 
 
+@pytest.mark.parametrize("seed", range(24))
+def test_random_batches(gpu, seed):
+    """Drawn batches: with a plan and without, split and whole, several routes that a
+    row sees all of, in part or not at all."""
+    rng = np.random.default_rng(100 + seed)
+    tree, fp8 = bool(seed & 1), bool(seed & 2)
+    B = int(rng.choice([1, 3, 20, 64, 70, 130]))
+    H, G = int(rng.integers(1, 4)), int(rng.choice([1, 2, 3, 4, 5, 8]))
+    lens = np.exp(rng.uniform(0, np.log([60, 400, 6000][int(rng.integers(3))]), B)).astype(int)
+    lens[rng.random(B) < 0.1] = 0
+    lens[rng.integers(B)] += int(rng.integers(0, 5000))
+    counts = np.exp(rng.uniform(0, np.log(64), B)).astype(int)
+    counts[rng.random(B) < 0.1] = 0
+    budget = 300_000   # (row, token) pairs that the oracle works through
+    while (counts * (lens + 1)).sum() > budget:
+        counts //= 2
+    c = Cache(lens, H=H, fp8=fp8, part=int(rng.choice([16, 48, 500, 1 << 20])), seed=seed,
+              first=rng.integers(0, 3, B) * 32)
+    first_pos = [int(rng.integers(-2, n + 70)) for n in lens]
+    r = Rows(c, counts, G, tree=tree, first_pos=first_pos, seed=seed)
+    if seed % 3 == 0 and tree:
+        r.tree_mask = rng.integers(-2 ** 63, 2 ** 63 - 1, len(r.tree_mask))  # any bits
+    assert_rows(r.gpu(head_major=bool(seed & 4)), r.oracle(), f"seed {seed}")
+
+
 # ------------------------------------------------------------ how it is run
 def test_same_bits_for_any_placement_stream_and_repeat(gpu):
     import torch
