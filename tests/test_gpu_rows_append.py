@@ -186,6 +186,93 @@ def test_a_route_takes_all_of_its_rows_or_none(gpu, many):
         assert ref[2][0][3] == (5 if "csr" in what else 5 + n), what
 
 
+# A call of up to 64 entries, at most three a route on the mean, is one launch.
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("head_major", [False, True])
+@pytest.mark.parametrize("H", [1, 3, 8])
+def test_a_few_rows_for_each_of_many_routes(gpu, H, head_major, fp8):
+    for seed in range(4):
+        rng = np.random.default_rng(seed)
+        B = int(rng.choice([1, 20, 22, 64, 500]))
+        counts = rng.multinomial(min(64, 3 * B) - seed % 2, np.ones(B) / B)
+        if seed == 3 and B > 1:
+            counts = np.sort(counts)
+            counts[-1], counts[:-1] = counts.sum(), 0      # one route takes them all
+        c = Cache(rng.integers(0, 60, B), H=H, fp8=fp8, spare=6, seed=seed)
+        begin = np.concatenate([[0], np.cumsum(counts)])
+        n = int(begin[-1])
+        k, v = _rows(2 * n, H, seed, spread=1.0 if seed < 2 else 500.0)
+        _check(c, k, v, begin, rng.permutation(2 * n)[:n], head_major=head_major, pad=8 * (seed & 1))
+
+
+@pytest.mark.parametrize("n", [64, 65])
+def test_both_sides_of_one_launch(gpu, n):
+    counts = [2] * 31 + [n - 62]
+    c = Cache([14] * 32, H=2, fp8=True, spare=2, seed=n)
+    _check(c, *_rows(n, 2, n, spread=50.0), np.concatenate([[0], np.cumsum(counts)]))
+
+
+def test_all_or_none_in_one_launch(gpu):
+    n, rest = 20, [0] * 20
+    k, v = _rows(3 * n, 2, 1)
+    for what, flags in (("full", 1), ("page", 4), ("row", 2), ("seq", 2), ("order", 2),
+                        ("base", 2), ("csr", 2), ("far", 2)):
+        c = Cache([5, 6, 7] + rest, H=2, spare=n // 16 + 2, seed=4)
+        begin, lst = [0, n, 2 * n, 3 * n] + [3 * n] * 20, list(range(3 * n))
+        if what == "full":
+            c.routes[1][5] = (6 + n - 1) // 16
+        elif what == "page":
+            c.page_ids[c.routes[1][4] + 1] = c.k_pool.shape[0]
+        elif what == "row":
+            lst[2 * n - 1] = 3 * n
+        elif what == "seq":
+            c.routes[1][0] = 23
+        elif what == "order":
+            c.routes[1][3] = -1
+        elif what == "base":
+            c.routes[1][4] = len(c.page_ids) - 1
+        elif what == "csr":
+            begin[-1] = 3 * n + 1
+        else:
+            c.routes[1][2:4] = 2 ** 31 - 10, 2 ** 31 - 4
+        ref = _check(c, k, v, begin, lst, flags=flags)
+        assert ref[2][0][3] == (5 if what == "csr" else 5 + n), what
+
+
+def test_captured_appends_of_single_rows(gpu):
+    """Four replays beside four eager calls: the routes move, the pages are crossed."""
+    import torch
+    from paper_2606_29207_amd import kf
+    from paper_2606_29207_amd.step import _to_dev
+    c = Cache([13, 14, 31, 0], H=2, fp8=True, spare=4, seed=4)
+    begin = _to_dev(np.arange(0, 9, 2, dtype=np.int32), "cuda")
+    sides = []
+    for _ in range(2):
+        d = c.device()
+        k, v = (_to_dev(x, "cuda") for x in _rows(8, 2, 0))
+        sides.append((d, k, v, kf.bind_kv_append_rows(
+            c.shape(2), d["k_pool"], d["v_pool"], k, v, d["routes"], begin, d["page_ids"], d["err"],
+            k_scale=d["k_scale"], v_scale=d["v_scale"])))
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        sides[1][3]()
+    torch.cuda.synchronize()
+    for step in range(4):
+        x = _rows(8, 2, step + 1, spread=100.0)
+        for d, k, v, _ in sides:
+            k.copy_(_to_dev(x[0], "cuda"))
+            v.copy_(_to_dev(x[1], "cuda"))
+        sides[0][3]()
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in ("k_pool", "v_pool", "routes", "err", "k_scale", "v_scale"):
+            a, b = (s[0][n].view(torch.int32) if s[0][n].dtype == torch.float32 else s[0][n]
+                    for s in sides)
+            assert torch.equal(a, b), (n, step)
+    assert int(sides[0][0]["err"].item()) == 0
+
+
 def test_captured_appends(gpu):
     import torch
     from paper_2606_29207_amd import kf
