@@ -368,3 +368,41 @@ def test_graph_replays(gpu, tree):
         torch.cuda.synchronize()
         assert torch.equal(a, out) and torch.equal(b, lse), k
     assert int(err.item()) == 0
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_graph_replays_of_planned_launches(gpu, tree):
+    """The plan is made anew at every replay: the routes grow and the rows move
+    between sequences."""
+    import torch
+    lens, counts = [5000, 900, 40] + [30] * 67, [4, 20, 0] + [1] * 67
+    c = Cache(lens, H=2, part=2048, seed=3)
+    r = Rows(c, counts, 4, tree=tree, seed=3)
+    # the long sequence begins short: its last route's tokens come later
+    last = c.seq_route_begin[1] - 1
+    ends = [int(c.routes[last][2]) + n for n in (5, 300, 900, 904)]
+    call, out, lse, err = r.gpu(run=False)
+    routes, begin = call._keep[6], call._keep[9]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        call()
+    torch.cuda.synchronize()
+    for k, end in enumerate(ends):
+        c.routes[last][3] = end
+        routes[last, 3] = end
+        r.row_begin[1] = 4 + k
+        begin[1] = 4 + k
+        if not tree:
+            r.first_pos[0] = end - 4 - k
+            call._keep[-1].copy_(torch.from_numpy(r.first_pos))
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        a, b = out.clone(), lse.clone()
+        assert_rows((a.double().cpu().numpy(), b.double().cpu().numpy(), int(err.item())),
+                    r.oracle(), f"replay {k}")
+        out.fill_(float("nan"))
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(a, out) and torch.equal(b, lse), k
