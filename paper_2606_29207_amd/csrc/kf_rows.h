@@ -8,8 +8,9 @@ namespace kf {
 
 constexpr int kRowTile = 128;     // (row, query head) pairs of one KV head per workgroup
 constexpr int kKeyTile = 32;      // tokens per step of a workgroup: two pages
-constexpr int kMaxRecsPerCu = 4;  // records of split work items per compute unit (twice and four
-                                  // times as many: the same within 0.5 %, and 68 MB each time)
+constexpr int kMaxRecsPerCu = 8;  // records of split work items per compute unit, 136 MB at most (with
+                                  // 4, 3 chunks of 512 rows behind 30K tokens 915 us instead of
+                                  // 816, 7 of them 1928 and 1864; with 16 the same within 1.5 %)
 constexpr int kMinPart = 4;       // key tiles of a part at least: 8 drafted tokens over 700 tokens
                                   // 15.4 us, 18.2 in parts of 8; over 300 14.3 in parts of 2, but
                                   // 64 rows over 1000 26.1 instead of 21.3
@@ -18,6 +19,11 @@ constexpr int kMostSteps = 96;    // mean, and at most
 constexpr int kSplitSlots = 4;    // (row tile, KV head) pairs per resident workgroup from which on
                                   // a launch splits none (2, 4 and 8: prompts of 6K .. 16K tokens
                                   // the same within 1 %; 8 packed ones 145, 144 and 148 us)
+// Key tiles from which on tiles of one length are split for a shorter last round: 5
+// chunks of 512 rows behind 30K tokens 1743 -> 1314 us, behind 1.7K (54 tiles and on)
+// 144 -> 127; 80 trees of 32 rows over 8K 566 -> 520, over 1.5K (48) 136 -> 133; but
+// over 1K (33) 103 -> 110.
+constexpr int kEqualSteps = 48;
 constexpr int64_t kMaxWgs = 0xFFFFFF;  // of 256 threads, in a launch: 32 bits of threads
 constexpr int kCombineWgsPerSlot = 8;  // workgroups of the combine per resident workgroup at most
                                        // (2 and 32: the same)

@@ -427,7 +427,7 @@ constexpr int kPlanSeqs = 1024;
 template <bool TREE>
 __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
   __shared__ unsigned long long s_work;
-  __shared__ int s_most, s_recs, s_parts, s_splits, s_pairs;
+  __shared__ int s_most, s_least, s_recs, s_parts, s_splits, s_pairs;
   __shared__ int s_count[64], s_scan[16];
   __shared__ unsigned long long l_tokens[kPlanSeqs];
   __shared__ int l_tiles[kPlanSeqs + 1], l_info[4 * kPlanSeqs], l_begin[kPlanSeqs + 1];
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
     l_info[4 * tid + 2] = wrong;
     l_info[4 * tid + 3] = 0;
   }
-  if (tid == 0) s_work = 0, s_most = 0;
+  if (tid == 0) s_work = 0, s_most = 0, s_least = INT32_MAX;
   if (tid < 64) s_count[tid] = 0;
   if (__syncthreads_or(bad)) {
     if (tid == 0) {
@@ -573,27 +573,48 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
     return own_k;
   };
   unsigned long long work = 0;
-  int most = 0;
+  int most = 0, least = INT32_MAX;
   for (int t = tid; t < T; t += 1024) {
     int b;
     bool wrong;
     const int k = look(t, b, wrong);
     work += k;
     most = max(most, k);
+    least = min(least, k);
   }
   if (64 * w < T) {
     if (a.may_split) work = (unsigned long long)wave_sum((int64_t)work);
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) most = max(most, __shfl_xor(most, m));
+    for (int m = 32; m >= 1; m >>= 1) {
+      most = max(most, __shfl_xor(most, m));
+      least = min(least, __shfl_xor(least, m));
+    }
     if (lane == 0) {
       atomicAdd(&s_work, work);
       atomicMax(&s_most, most);
+      atomicMin(&s_least, least);
     }
   }
   __syncthreads();
   most = s_most;
+  least = s_least;
   int cap = most;
-  if (a.may_split && (int64_t)T * a.num_kv_heads < kSplitSlots * (int64_t)a.slots) {
+  const bool may_split = a.may_split && (int64_t)T * a.num_kv_heads < kSplitSlots * (int64_t)a.slots;
+  // Tiles of much the same length that do not fill whole rounds of the workgroups:
+  // the rounds' tiles stay whole and the others (all of them, below one round) are cut
+  // into `tail` parts, so that the last round is a shorter one.
+  const int round = max(1, a.slots / a.num_kv_heads), whole = T / round * round;
+  int tail = 1;
+  if (may_split && least >= kEqualSteps && (int64_t)least * 4 >= (int64_t)most * 3) {
+    const int r = T / round, left = T - whole;
+    int turns = left > 0;  // of the last round, in parts
+    for (int p = 2; p <= 8 && left * p <= a.max_recs; ++p) {
+      const int n = (left * p + round - 1) / round;
+      if (n * tail < turns * p) turns = n, tail = p;
+    }
+    if ((r * tail + turns) * 10 > 9 * (r + 1) * tail) tail = 1;
+  }
+  if (may_split && tail == 1) {
     const unsigned long long share = (s_work * a.num_kv_heads + a.slots - 1) / a.slots;
     cap = (int)min((unsigned long long)most, max(share, (unsigned long long)kMinPart));
     // An even share per workgroup, in one round.  Where that leaves more parts than
@@ -672,7 +693,7 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
       if (lane >= m) x += y;
     }
     s_count[lane] = x - mine;
-    if (lane == 63) a.head[0] = x;
+    if (lane == 63) a.head[0] = x + (tail - 1) * (T - whole);
   }
   __syncthreads();
   if (by_seq) {
@@ -684,9 +705,14 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
   for (int t = tid; t < T; t += 1024) {
     int b;
     bool wrong;
-    const int k = look(t, b, wrong), parts = (k + per - 1) / per;
-    const int at = by_seq ? (int)l_tokens[b] + l_tiles[b + 1] - 1 - t
+    const int k = look(t, b, wrong);
+    int parts = (k + per - 1) / per;
+    int at = by_seq ? (int)l_tokens[b] + l_tiles[b + 1] - 1 - t
                           : atomicAdd(&s_count[place((k + parts - 1) / parts)], parts);
+    if (tail > 1 && at >= whole) {  // (every other tile is whole)
+      parts = tail;
+      at = whole + (at - whole) * tail;
+    }
     RowsItem it;
     it.seq = wrong ? -1 - b : b;
     it.tile = t - tiles_of[b];

@@ -303,6 +303,23 @@ def test_planned_splits(gpu, fp8, tree):
     assert_rows(r.gpu(), ref)
 
 
+@pytest.mark.parametrize("B,rows,n,tree,fp8", [
+    (10, 1, 1600, True, False), (10, 2, 1600, False, True), (5, 1, 3200, True, True),
+    (5, 130, 1750, False, False)])
+def test_equal_tiles_in_a_shorter_last_round(gpu, B, rows, n, tree, fp8):
+    """Tiles of one length that fill no whole rounds of the workgroups (64 KV heads, so
+    that a round has few): those of the last one are split."""
+    c = Cache([n] * B, H=64, fp8=fp8, part=1500, seed=B)
+    r = Rows(c, [rows] * B, 1, tree=tree, seed=rows)
+    assert_rows(r.gpu(), r.oracle())
+    if rows < 100:
+        c.page_ids[c.routes[3][4] + 1] = -1       # sequence 1, second route
+        c.routes[2 * B - 2][4] = -1               # the last sequence
+        ref = r.oracle()
+        assert ref[2] == 6
+        assert_rows(r.gpu(), ref)
+
+
 @pytest.mark.parametrize("seed", range(24))
 def test_random_batches(gpu, seed):
     """Drawn batches: with a plan and without, split and whole, several routes that a
