@@ -136,11 +136,12 @@ __device__ __forceinline__ float one_scale(bool begins, uint32_t first, uint32_t
 // x / scale, correctly rounded, clamped to +-448: inv is 1 / scale, correctly
 // rounded, so that one step from x inv by its remainder gives the nearest float
 // (Markstein).  Remainders stay in range where the quotient is not far below
-// E4M3's smallest value; there any quotient rounds to the same zero.
+// E4M3's smallest value; there any quotient rounds to the same zero.  The remainder
+// of -0 is +0, and +0 - 0 is +0: the sign is x's own (scales are positive).
 __device__ __forceinline__ float quotient(float x, float scale, float inv) {
   const float q = x * inv;
-  return __builtin_amdgcn_fmed3f(__builtin_fmaf(__builtin_fmaf(-q, scale, x), inv, q), -448.0f,
-                                 448.0f);
+  const float y = __builtin_fmaf(__builtin_fmaf(-q, scale, x), inv, q);
+  return __builtin_copysignf(fminf(fabsf(y), 448.0f), x);
 }
 __device__ __forceinline__ float lo_bf16(uint32_t x) { return __builtin_bit_cast(float, x << 16); }
 __device__ __forceinline__ float hi_bf16(uint32_t x) {

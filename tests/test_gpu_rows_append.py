@@ -308,3 +308,38 @@ def test_captured_appends(gpu):
                              x.view(torch.int32) if x.dtype == torch.float32 else x) for x in (a, b))
                     assert torch.equal(a, b), (n, step)
             assert int(sides[0][0]["err"].item()) == 0
+
+
+@pytest.mark.parametrize("n", [6, 21, 90])      # one launch, and planned ones
+@pytest.mark.parametrize("start", [0, 9])       # a page that begins with the call, or goes on
+def test_zeros_keep_their_sign(gpu, n, start):
+    """-0.0 beside ordinary values, on pages whose scale stays: 0x80, as single
+    appends store it; a page of zeros alone (scale 1) too."""
+    import torch
+    from paper_2606_29207_amd import kf
+    from paper_2606_29207_amd.step import _to_dev
+    H, routes = 2, 4
+    rng = np.random.default_rng(n + start)
+    k, v = _rows(routes * n, H, n)
+    for x in (k, v):
+        x[rng.random(x.shape) < 0.2] = 0x8000
+        x[rng.random(x.shape) < 0.1] = 0x0000
+        x[rng.random(x.shape) < 0.05] = 0x8001           # rounds to a zero of its sign
+        x[-n:] = np.where(rng.random(x[-n:].shape) < 0.5, 0x8000, 0)
+    begin = np.arange(routes + 1) * n
+    c = Cache([start] * routes, H=H, fp8=True, spare=7, seed=n)
+    c.k_scale *= 16                                      # room, as appends leave it
+    c.v_scale *= 16
+    ref = _check(c, k, v, begin)
+    assert (ref[0] == 0x80).sum() > 100 and (ref[1] == 0x80).sum() > 100
+    d = c.device()
+    tail = torch.arange(routes, dtype=torch.int32, device="cuda")
+    for i in range(n):
+        pick = begin[:-1] + i
+        kf.kv_append(c.shape(H), d["k_pool"], d["v_pool"], _to_dev(k[pick], "cuda"),
+                     _to_dev(v[pick], "cuda"), d["routes"], tail, d["page_ids"], d["err"],
+                     k_scale=d["k_scale"], v_scale=d["v_scale"])
+    torch.cuda.synchronize()
+    assert int(d["err"].item()) == 0
+    assert np.array_equal(d["k_pool"].cpu().numpy(), ref[0])
+    assert np.array_equal(d["v_pool"].cpu().numpy(), ref[1])
