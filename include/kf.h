@@ -404,6 +404,8 @@ size_t kf_rows_attn_workspace_bytes(const kf_shape* shape, int32_t num_rows);
  * A row that sees no token gives out = 0, lse = -inf.  A token that a row does
  * not see never changes the row, whatever it holds.  The weights enter their
  * product with V as bfloat16 (their sum as float32): the output's own precision.
+ * The same arguments give the same bits; where a row's keys are split, and so its
+ * last bits, follows from all the lengths of the launch.
  * q and out are [num_rows][num_q_heads][128] bfloat16 (q with q_stride elements
  * between rows), lse [num_rows][num_q_heads]; rows outside
  * [seq_row_begin[0], seq_row_begin[num_seqs]) are left as they were.

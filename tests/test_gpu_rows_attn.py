@@ -423,3 +423,43 @@ def test_graph_replays_of_planned_launches(gpu, tree):
         call()
         torch.cuda.synchronize()
         assert torch.equal(a, out) and torch.equal(b, lse), k
+
+
+@pytest.mark.parametrize("B", [700, 1100])      # the plan's tables in LDS, in memory
+@pytest.mark.parametrize("tree", [False, True])
+def test_same_bits_of_tiles_in_a_shorter_last_round(gpu, tree, B):
+    """Tiles of one length, more than a round of the workgroups: which of them are
+    split, and so rounded in another order, follows from the arguments alone."""
+    import torch
+    from paper_2606_29207_amd import kf
+    G, n, pages, rows = 4, 1600, 3000, 4
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+
+    def normal(*size):
+        return torch.randn(size, generator=gen, device="cuda").to(torch.bfloat16)
+
+    def ints(x):
+        return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+    k_pool, v_pool = normal(pages, 1, 16, DIM), normal(pages, 1, DIM, 16)
+    page_ids = torch.randint(0, pages, (B * n // 16,), generator=gen, device="cuda").to(torch.int32)
+    routes = ints([[b, 0, 0, n, b * n // 16, n // 16] for b in range(B)])
+    q, kd, vd = normal(B * rows, G, DIM), normal(B * rows, 1, DIM), normal(B * rows, 1, DIM)
+    shape = kf.make_shape(B, G, 1, kf.KV_BF16, pages, B * n // 16, DIM ** -0.5)
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    first = None
+    for k in range(12):
+        out = torch.full((B * rows, G, DIM), float("nan"), dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((B * rows, G), float("nan"), device="cuda")
+        tail = (k_pool, v_pool, routes, n // 16, page_ids, ints(range(B + 1)),
+                ints([rows * b for b in range(B + 1)]), out, lse,
+                kf.alloc_rows_workspace(shape, B * rows), err)
+        if tree:
+            kf.tree_attn(shape, q, kd, vd, torch.full((B * rows,), 15, device="cuda"), *tail)
+        else:
+            kf.prompt_attn(shape, q, ints([n - rows] * B), *tail)
+        torch.cuda.synchronize()
+        first = first or (out, lse)
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1]), k
+    assert int(err.item()) == 0 and not out.isnan().any()
