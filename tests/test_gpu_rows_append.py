@@ -343,3 +343,18 @@ def test_zeros_keep_their_sign(gpu, n, start):
     assert int(d["err"].item()) == 0
     assert np.array_equal(d["k_pool"].cpu().numpy(), ref[0])
     assert np.array_equal(d["v_pool"].cpu().numpy(), ref[1])
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("counts", [[56, 96, 8, 0], [2, 1, 3, 2], [0, 30, 20, 60]])
+def test_a_prompt_over_several_routes_of_a_sequence(gpu, counts, fp8):
+    """Rows into three routes of one sequence in one call: a partly filled range, two
+    empty ones behind it, and another sequence's."""
+    c = Cache([200, 10], H=2, fp8=fp8, part=96, spare=5, seed=2)
+    assert [list(r[:1]) for r in c.routes] == [[0], [0], [0], [1]]
+    for r, end in enumerate((40, 96, 192)):
+        c.routes[r][3] = end
+    begin = np.concatenate([[0], np.cumsum(counts)])
+    k, v = _rows(int(begin[-1]), 2, 6, spread=30.0)
+    ref = _check(c, k, v, begin)
+    assert list(ref[-2][:, 3]) == [40 + counts[0], 96 + counts[1], 192 + counts[2], 10 + counts[3]]

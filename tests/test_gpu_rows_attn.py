@@ -463,3 +463,139 @@ def test_same_bits_of_tiles_in_a_shorter_last_round(gpu, tree, B):
         first = first or (out, lse)
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1]), k
     assert int(err.item()) == 0 and not out.isnan().any()
+
+
+# ------------------------------------------------- exceptional values over fp8
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1.5])
+def test_scales_over_fp8_pages(gpu, scale):
+    c = Cache([150], H=2, fp8=True, seed=1)
+    r = Rows(c, [150], 4, seed=2)
+    got, ref = r.gpu(scale), r.oracle(scale)
+    wide = max(1.0, abs(scale) / 0.0884)       # as test_scales
+    assert np.abs(got[1] - ref[1]).max() <= 1e-4 * wide
+    bound = 2.0 ** -8 * np.abs(ref[0]) + (2.0 ** -8 + 2.0 ** -16 + 4e-4 * (wide > 1)) * ref[3]
+    assert np.all(np.abs(got[0] - ref[0]) <= bound + 1e-30)
+
+
+def test_hidden_fp8_tokens_never_reach_a_row(gpu):
+    n = 150
+    c = Cache([n], H=2, fp8=True, part=96, seed=11)
+    r = Rows(c, [n], 4, seed=11)
+    clean = r.gpu()
+    for t in (100, 101, 103, 149):
+        pid, slot = c.at(0, t)
+        c.k_pool[pid, :, slot] = 0x7F
+        c.v_pool[pid, :, ::3, slot] = 0xFF
+    out, lse, flags = r.gpu()
+    ref = r.oracle()
+    assert flags == 0 and not np.isnan(ref[0][:100]).any()
+    # rows up to 95 share no tile with them
+    assert np.array_equal(out[:64], clean[0][:64]) and np.array_equal(lse[:64], clean[1][:64])
+    assert_rows((out[:100], lse[:100], 0), (ref[0][:100], ref[1][:100], 0, ref[3][:100]))
+    assert np.isnan(out[100:]).all() and np.isnan(lse[100:]).all()
+
+
+@pytest.mark.parametrize("G", [1, 3, 4])
+def test_fp8_nan_values_reach_exactly_the_rows_that_see_them(gpu, G):
+    """NaN codes in single dims of V: those dims of the rows that see the token, no
+    other output; the page's V scale stays in the others."""
+    n = 170
+    c = Cache([n, 40], H=2, fp8=True, part=112, seed=13)
+    r = Rows(c, [n, 40], G, seed=13)
+    for t, dims, code in ((70, [5, 77], 0x7F), (71, [127], 0xFF), (75, [0], 0x7F), (130, [64], 0x7F)):
+        pid, slot = c.at(0, t)
+        c.v_pool[pid, 0, dims, slot] = code
+    ref = r.oracle()
+    assert np.isnan(ref[0][70:170, :G, 5]).all() and not np.isnan(ref[0][:70]).any()
+    assert not np.isnan(ref[0][:, G:]).any() and not np.isnan(ref[1]).any()
+    assert_rows(r.gpu(), ref)
+
+
+def test_drafts_that_are_not_finite_over_fp8_pages(gpu):
+    """Hidden ones never reach a row; a visible infinity reaches its dims of exactly
+    the rows that see it."""
+    c = Cache([45], H=2, fp8=True, seed=5)
+    r = Rows(c, [40], 4, tree=True, seed=5)
+    m = r.tree_mask
+    m[:] = [1 << i for i in range(40)]         # each itself alone
+    m[20:24] |= 1 << 10
+    r.v_draft[3], r.k_draft[3] = 0x7F80, 0x7FC0
+    r.v_draft[35, :, ::2] = 0x7FC0
+    r.v_draft[10, :, 9] = 0x7F80
+    r.v_draft[10, :, 40] = 0xFF80
+    got, ref = r.gpu(), r.oracle()
+    sees_inf = [10, 20, 21, 22, 23]
+    assert np.isposinf(ref[0][sees_inf, :, 9]).all() and np.isneginf(ref[0][sees_inf, :, 40]).all()
+    for sign in (np.isposinf, np.isneginf):
+        assert np.array_equal(sign(got[0]), sign(ref[0]))
+    assert np.isnan(got[0][3]).all() and np.isnan(got[1][3]).all()
+    # the rest within its bound (infinities taken out on both sides)
+    out, want, spread = (np.where(np.isinf(ref[0]), 0.0, x) for x in (got[0], ref[0], ref[3]))
+    assert_rows((out, got[1], got[2]), (want, *ref[1:3], spread))
+
+
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("k, v", [(0.0, 1.0), (-1.0, 1.0), (1.0, 0.0), (1.0, -1.0), (-1.0, -2.0),
+                                  (0.0, 0.0)])
+def test_fp8_page_scales_of_zero_and_below(gpu, tree, k, v):
+    """Such pages among ordinary ones, beside one in their tile and alone in it."""
+    lens = [200, 33, 90]
+    c = Cache(lens, H=2, fp8=True, part=112, seed=21)
+    for b, t in ((0, 20), (0, 130), (1, 32), (2, 10), (2, 17), (2, 89)):
+        pid = c.at(b, t)[0]
+        c.k_scale[pid] *= np.float32(k)
+        c.v_scale[pid, 1] *= np.float32(v)
+    r = Rows(c, [20, 33, 30] if tree else lens, 4, tree=tree, seed=22)
+    assert_rows(r.gpu(), r.oracle())
+
+
+@pytest.mark.parametrize("which", ["k_scale", "v_scale"])
+def test_a_nan_page_scale_reaches_the_rows_that_see_the_page(gpu, which):
+    n = 120
+    c = Cache([n], H=2, fp8=True, seed=23)
+    getattr(c, which)[c.at(0, 80)[0], 1] = np.nan      # tokens 80 .. 95, the second of a tile's pages
+    r = Rows(c, [n], 2, seed=24)
+    ref = r.oracle()
+    assert np.isnan(ref[0][80:, 2:]).all() and not np.isnan(ref[0][:80]).any()
+    assert_rows(r.gpu(), ref)
+
+
+# -------------------------------------- many sequences, bad ones that rows see
+@pytest.mark.parametrize("B", [64, 65, 1024, 1025, 3000])
+@pytest.mark.parametrize("tree", [False, True])
+def test_many_sequences_with_bad_ones_that_have_rows(gpu, B, tree):
+    rng = np.random.default_rng(B)
+    lens, counts = rng.integers(0, 60, B), rng.integers(0, 4, B)
+    marked = [3, B // 2, B - 1]
+    lens[marked], counts[marked] = [40, 50, 37], [1, 3, 2]
+    if not tree:
+        counts = np.minimum(counts, lens)
+    c = Cache(lens, H=1, part=32, seed=B)
+    r = Rows(c, counts, 2, tree=tree, seed=B)
+    c.routes[c.seq_route_begin[B // 2]][4] = -3
+    c.page_ids[c.routes[-1][4]] = 1 << 20              # of the last sequence's last route
+    ref = r.oracle()
+    assert ref[2] == 6
+    begin = r.row_begin
+    for b, bad in ((3, False), (B // 2, True), (B - 1, True)):
+        assert np.isnan(ref[0][begin[b]:begin[b + 1]]).all() == bad
+    assert_rows(r.gpu(), ref, f"B {B}")
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("B", [1025, 2500])
+@pytest.mark.parametrize("tree", [False, True])
+def test_splits_among_more_sequences_than_the_plan_keeps_in_lds(gpu, tree, B, fp8):
+    """Few rows over long sequences among a thousand that have none or are short."""
+    lens, counts = np.full(B, 3), np.zeros(B, int)
+    counts[::40] = 1
+    for b, n, rows in ((7, 4000, 1), (B // 3, 6000, 2), (B // 2, 2500, 30), (B - 2, 5000, 2), (B - 1, 700, 1)):
+        lens[b], counts[b] = n, rows
+    c = Cache(lens, H=2, fp8=fp8, part=2048, seed=B)
+    r = Rows(c, counts, 4, tree=tree, seed=B)
+    assert_rows(r.gpu(), r.oracle())
+    c.page_ids[c.routes[c.seq_route_begin[7]][4] + 9] = -1
+    c.routes[c.seq_route_begin[B - 2] + 1][5] = 0
+    ref = r.oracle()
+    assert ref[2] == 6
+    assert_rows(r.gpu(), ref)
