@@ -33,6 +33,15 @@ constexpr int kCombineWgsPerSlot = 8;  // workgroups of the combine per resident
 // route 11.1 and 9.1, two for each of 64 12.0 and 10.6 (fp8).
 constexpr int kDirectEntries = 64;
 constexpr int kDirectMean = 3;
+// The one launch has a workgroup per route, each of whose waves reads the whole table
+// of entries, up to kDirectRoutes routes, and from there on a workgroup per entry that
+// reads it once: 64 entries in 64 routes 8.4 us and 8.9, in 128 9.1 and 9.0, in 256 10.5
+// and 9.0, in 1024 28 and 9.0, in 65535 32,000 and 20.
+constexpr int kDirectRoutes = 128;
+// The plan's workgroups, one a route, read the table each up to kPlanRoutes routes; from
+// there on a launch before it does: 200 entries in 1024 routes 15.2 and 17.5, in 2048
+// 18.0 and 17.7, in 4096 25 and 18, in 65535 1820 and 53.
+constexpr int kPlanRoutes = 2048;
 
 // ------------------------------------------------------------------- append
 struct AppendRowsArgs {

@@ -68,23 +68,28 @@ __device__ __forceinline__ float wave_max(float x) {
 // before them 5 us.  Appends of a few rows are one launch, bound by its chain of
 // loads (7.3 us a pass).
 //
+// Whether row i of the table of entries decreases or leaves [0, num_entries].
+__device__ __forceinline__ bool bad_entries(const AppendRowsArgs& a, int i) {
+  const int x = a.entry_begin[i], y = a.entry_begin[i + 1];
+  return x < 0 || y < x || y > a.num_entries;
+}
+
 // One route's check: its tokens before the append, or -1 if it takes no rows (flag
 // says why).  WHOLE: by the workgroup together; else by every wave for itself, for
-// calls of a few rows, which are a chain of loads.
+// calls of a few rows, which are a chain of loads.  table: the table of entries too.
 template <bool WHOLE>
-__device__ int append_check(const AppendRowsArgs& a, int r, int& flag) {
+__device__ int append_check(const AppendRowsArgs& a, int r, bool table, int& flag) {
   const int lane = WHOLE ? threadIdx.x : threadIdx.x & 63, step = WHOLE ? blockDim.x : 64;
   auto any = [](bool x) -> bool { return WHOLE ? __syncthreads_or(x) : __ballot(x) != 0; };
   const int e0 = a.entry_begin[r], n = a.entry_begin[r + 1] - e0;
   const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + r);
   const int seq = rp[0], tb = rp[2], te = rp[3], base = rp[4], cap = rp[5];
-  // the whole table of entries: nondecreasing within [0, num_entries]
-  bool bad = false;
-  for (int i = lane; i < a.num_routes; i += step) {
-    const int x = a.entry_begin[i], y = a.entry_begin[i + 1];
-    bad |= x < 0 || y < x || y > a.num_entries;
+  flag = 0;
+  if (table) {
+    bool bad = false;
+    for (int i = lane; i < a.num_routes; i += step) bad |= bad_entries(a, i);
+    flag = any(bad) ? KF_EFLAG_BAD_ROUTE : 0;
   }
-  flag = any(bad) ? KF_EFLAG_BAD_ROUTE : 0;
   if (flag || n == 0) return -1;
   const int64_t j0 = (int64_t)te - tb, last = (j0 + n - 1) / kPage;
   if (seq < 0 || seq >= a.num_seqs || j0 < 0 || (int64_t)te + n > INT32_MAX || j0 + n > INT32_MAX)
@@ -326,14 +331,47 @@ __device__ void append_page(const AppendRowsArgs& a, int page, int g, bool is_v,
   }
 }
 
+// The table of entries of a call of many routes, by one workgroup, before the plan:
+// -1 into every route's row of it, or 0.
+__global__ __launch_bounds__(1024) void append_table_kernel(AppendRowsArgs a) {
+  bool bad = false;
+#pragma unroll 8
+  for (int i = threadIdx.x; i < a.num_routes; i += 1024) bad |= bad_entries(a, i);
+  bad = __syncthreads_or(bad);
+  for (int i = threadIdx.x; i < a.num_routes; i += 1024) a.plan[4 * i] = bad ? -1 : 0;
+  if (bad && threadIdx.x == 0) atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
+}
+
 // One workgroup per route: the check; the plan of its pages, or with DIRECT the
-// pages themselves; the route's new end.
+// pages themselves; the route's new end.  With DIRECT and many routes a workgroup
+// per entry: the first one of a route works on it.
 template <bool FP8, bool DIRECT>
 __global__ __launch_bounds__(1024) void append_plan_kernel(AppendRowsArgs a) {
   __shared__ uint16_t lds[FP8 && DIRECT ? 16 * kPage * 64 : 1];
-  const int r = blockIdx.x;
+  int r = blockIdx.x;
+  bool table = true;
+  if (DIRECT && a.num_routes > kDirectRoutes) {
+    __shared__ int s_route;
+    if (threadIdx.x == 0) s_route = -1;
+    __syncthreads();
+    bool bad = false;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < a.num_routes; i += 1024) {
+      const int x = a.entry_begin[i], y = a.entry_begin[i + 1];
+      bad |= x < 0 || y < x || y > a.num_entries;
+      if (x == (int)blockIdx.x && y > x) s_route = i;  // (one, in a table that does not decrease)
+    }
+    bad = __syncthreads_or(bad);
+    if (bad && threadIdx.x == 0) atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
+    r = bad ? -1 : s_route;
+    if (r < 0) return;
+    table = false;
+  } else if (!DIRECT && a.num_routes > kPlanRoutes) {
+    if (a.plan[4 * r] < 0) return;
+    table = false;
+  }
   int flag = 0;
-  const int j0 = append_check<!DIRECT>(a, r, flag);
+  const int j0 = append_check<!DIRECT>(a, r, table, flag);
   if (threadIdx.x == 0 && flag) atomicOr(a.err_flags, flag);
   if (!DIRECT && threadIdx.x == 0) a.plan[4 * r] = j0;
   if (j0 < 0) return;
@@ -358,9 +396,13 @@ __global__ __launch_bounds__(1024) void append_plan_kernel(AppendRowsArgs a) {
   if (threadIdx.x == 0) a.routes[r].tok_end += n;
 }
 
-// One wave per (page tile, KV head, K or V).  Route r has the tiles
-// floor(entry_begin[r] / 16) + 2 r and on: at least its n / 16 + 2 pages fit
-// before the next route's.
+// First page tile of route r, whose first entry is `entry`: its n / 16 + 2 pages fit
+// before the next route's, as at most min(r, entry) routes before it have entries.
+__host__ __device__ __forceinline__ int64_t append_first_tile(int entry, int r) {
+  return (int64_t)(entry / kPage) + 2 * (int64_t)(r < entry ? r : entry);
+}
+
+// One wave per (page tile, KV head, K or V).
 template <bool FP8>
 __global__ __launch_bounds__(256) void append_tile_kernel(AppendRowsArgs a) {
   __shared__ uint16_t lds[FP8 ? 4 * kPage * 64 : 1];
@@ -373,7 +415,7 @@ __global__ __launch_bounds__(256) void append_tile_kernel(AppendRowsArgs a) {
   int lo = 0, hi = a.num_routes;  // first(lo) <= tile < first(hi)
   while (hi - lo > 1) {
     const int step = (hi - lo + 63) / 64, at = lo + lane * step;
-    const bool in = at < hi && (int64_t)(a.entry_begin[at] / kPage) + 2 * (int64_t)at <= tile;
+    const bool in = at < hi && append_first_tile(a.entry_begin[at], at) <= tile;
     const uint64_t v = __ballot(in);
     // a table that decreases can answer anything; a plan is then never made
     const int last = v ? 63 - __builtin_clzll(v) : 0;
@@ -384,7 +426,7 @@ __global__ __launch_bounds__(256) void append_tile_kernel(AppendRowsArgs a) {
   if (j0 < 0) return;
   const int e0 = a.plan[4 * lo + 1], n = a.plan[4 * lo + 2], base = a.plan[4 * lo + 3];
   const int p0 = j0 / kPage;
-  const int64_t p = p0 + tile - (e0 / kPage + 2 * (int64_t)lo);
+  const int64_t p = p0 + tile - append_first_tile(e0, lo);
   if (p < p0 || p > (j0 + n - 1) / kPage) return;
   const int s0 = p == p0 ? j0 % kPage : 0;
   const int s1 = (int)min((int64_t)kPage, j0 + n - p * kPage);
@@ -1793,16 +1835,22 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
 
 hipError_t launch_append_rows(const AppendRowsArgs& a, bool fp8, hipStream_t stream) {
   if (a.num_entries <= kDirectEntries && a.num_entries <= kDirectMean * a.num_routes) {
+    const int wgs = a.num_routes > kDirectRoutes ? a.num_entries : a.num_routes;
     if (fp8)
-      append_plan_kernel<true, true><<<a.num_routes, 1024, 0, stream>>>(a);
+      append_plan_kernel<true, true><<<wgs, 1024, 0, stream>>>(a);
     else
-      append_plan_kernel<false, true><<<a.num_routes, 1024, 0, stream>>>(a);
+      append_plan_kernel<false, true><<<wgs, 1024, 0, stream>>>(a);
     return hipGetLastError();
   }
-  append_plan_kernel<false, false><<<a.num_routes, 512, 0, stream>>>(a);
-  const hipError_t st = hipGetLastError();
-  if (st != hipSuccess) return st;
-  const int64_t tiles = (int64_t)a.num_entries / kPage + 2 * (int64_t)a.num_routes;
+  hipError_t st;
+  const bool many = a.num_routes > kPlanRoutes;
+  if (many) {
+    append_table_kernel<<<1, 1024, 0, stream>>>(a);
+    if ((st = hipGetLastError()) != hipSuccess) return st;
+  }
+  append_plan_kernel<false, false><<<a.num_routes, many ? 64 : 512, 0, stream>>>(a);
+  if ((st = hipGetLastError()) != hipSuccess) return st;
+  const int64_t tiles = append_first_tile(a.num_entries, a.num_routes);
   const int64_t grid = (tiles * 2 * a.num_kv_heads + 3) / 4;
   if (fp8)
     append_tile_kernel<true><<<(uint32_t)grid, 256, 0, stream>>>(a);

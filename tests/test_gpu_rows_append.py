@@ -358,3 +358,49 @@ def test_a_prompt_over_several_routes_of_a_sequence(gpu, counts, fp8):
     k, v = _rows(int(begin[-1]), 2, 6, spread=30.0)
     ref = _check(c, k, v, begin)
     assert list(ref[-2][:, 3]) == [40 + counts[0], 96 + counts[1], 192 + counts[2], 10 + counts[3]]
+
+
+# Calls of more than 128 routes (one launch) and of more than 2048 (planned) read the
+# table of entries in other ways.
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("R", [128, 129, 2048, 2049, 5000])
+def test_many_routes_of_which_few_take_rows(gpu, R, fp8):
+    for n, seed in ((1, 0), (64, 1), (65, 2), (400, 3), (3 * min(R, 1000), 4)):
+        rng = np.random.default_rng(R + seed)
+        counts = rng.multinomial(n, np.ones(R) / R)
+        if seed in (1, 2):                                   # the first, the last, one of many
+            counts[:] = 0
+            counts[[0, R // 2, R - 1]] = 1, n - 3, 2
+        c = Cache(rng.integers(0, 40, R), H=2, fp8=fp8, spare=5 + n // 16 * (seed in (1, 2)), seed=seed)
+        begin = np.concatenate([[0], np.cumsum(counts)]) + (2 if n == 65 else 0)
+        k, v = _rows(n + 2, 2, seed)
+        _check(c, k, v, begin, rng.permutation(n + 2) if n != 400 else None)
+
+
+@pytest.mark.parametrize("n", [40, 3000])
+def test_all_or_none_among_many_routes(gpu, n):
+    R = 2500
+    k, v = _rows(n, 2, 1)
+    for what, flags in (("full", 1), ("page", 4), ("row", 2), ("base", 2), ("csr", 2), ("csr_end", 2)):
+        counts = np.full(R, n // R)
+        counts[[0, 700, R - 1]] += 4
+        counts[20] = 0
+        counts = np.minimum(counts, n)
+        begin = np.concatenate([[0], np.cumsum(counts)])
+        lst = np.arange(max(n, int(begin[-1]))) % n
+        c = Cache(np.arange(R) % 20, H=2, spare=2, seed=4)
+        if what == "full":
+            c.routes[700][5] = 0
+        elif what == "page":
+            c.page_ids[c.routes[700][4]] = -1
+            c.routes[700][2:4] = 0, 3
+        elif what == "row":
+            lst[begin[700] + 3] = n
+        elif what == "base":
+            c.routes[700][4] = len(c.page_ids)
+        elif what == "csr":
+            begin[1000] = begin[700]
+        else:
+            begin[-1] = len(lst) + 1
+        ref = _check(c, k, v, begin, lst, flags=flags)
+        assert ref[2][0][3] == (0 if "csr" in what else begin[1]), what
