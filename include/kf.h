@@ -416,6 +416,8 @@ size_t kf_rows_attn_workspace_bytes(const kf_shape* shape, int32_t num_rows);
  * rows NaN; a page id outside the pool sets KF_EFLAG_BAD_PAGE and makes the
  * rows NaN that see a token of that page.  Sequences without rows are not
  * looked at.
+ * max_pages_per_route bounds the pages that hold a route's tokens, not those it
+ * reserves; launches of few sequences run faster the closer it is.
  * Alignment: q, pools and out 16 bytes, workspace 256, the rest 4.
  */
 int kf_prompt_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64_t q_stride,

@@ -120,7 +120,7 @@ struct RowsArgs {
   int32_t max_recs;     // records per KV head
   int32_t rec_rows;     // rows of a record
   int32_t slots;        // resident workgroups
-  int32_t parts;        // > 0: no plan; every row tile in so many parts
+  int32_t parts;        // > 0: no plan; every row tile in so many parts at most
   int32_t may_split;    // a plan may split row tiles: a combine follows
 };
 
@@ -132,7 +132,7 @@ struct RowsLayout {
 RowsLayout rows_layout(int32_t num_rows, int32_t num_seqs, int32_t num_kv_heads, int32_t group,
                        int64_t cus);
 
-// Parts per row tile of a launch that runs without a plan, 0 with one.
+// Parts per row tile, at most, of a launch that runs without a plan, 0 with one.
 int32_t unplanned_parts(const RowsLayout& l, int32_t num_seqs, int32_t num_kv_heads,
                         int32_t num_routes, int32_t num_page_ids, int32_t max_pages_per_route,
                         int64_t slots);

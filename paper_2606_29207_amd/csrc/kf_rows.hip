@@ -833,6 +833,13 @@ __device__ __forceinline__ int find_tile(const RowsArgs& a, int tile, int lane, 
   return 1;
 }
 
+// Parts of a row tile of `all` key tiles, of `most` for which the launch has
+// workgroups: its page table may reserve many times what it holds.
+__device__ __forceinline__ int tile_parts(int most, int64_t all) {
+  const float by_turns = 2.0f * __builtin_sqrtf((float)all);
+  return max(1, min(most, min((int)((all + kMinPart - 1) / kMinPart), (int)by_turns)));
+}
+
 // ---------------------------------------------------------------- attention
 __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
@@ -1571,8 +1578,9 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     } else {
       const int64_t all = k + (TREE ? (n_rows + kKeyTile - 1) / kKeyTile : 0);
       const int part = item / a.max_tiles;
-      it.key0 = uniform((int)(all * part / a.parts));
-      it.key1 = part + 1 < a.parts ? uniform((int)(all * (part + 1) / a.parts)) : INT32_MAX;
+      const int parts = uniform(tile_parts(a.parts, all));  // those behind them are empty
+      it.key0 = uniform((int)(all * part / parts));
+      it.key1 = part + 1 != parts ? uniform((int)(all * (part + 1) / parts)) : INT32_MAX;
     }
   }
   if (it.seq < 0) {
@@ -1734,6 +1742,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   if (it.rec >= 0) {
     const size_t rec = ((size_t)it.rec * H + g) * a.rec_rows + (m - m0);
     if (half == 0) *reinterpret_cast<f32x2*>(a.rec_ml + 2 * rec) = f32x2{st.m, l};
+    if (l == 0.0f) return;  // the combine does not read it
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -1756,6 +1765,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
 
 // The parts of a split row tile into its outputs: a wave per (row, head), a lane
 // per part's maximum and sum, then the parts' outputs, eight on their way at a time.
+// A part whose sum is 0 has written none.
 // Bound by its chain of loads: 4 us for one tile, 8 us for 48 trees in 2 to 4 parts,
 // 14 .. 18 us for 128 and 256 full tiles in 4 and 2.
 __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
@@ -1801,6 +1811,7 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
       load(0);
       f32x2 x = {neg_inf(), 0.0f};  // of part p + lane
       if (lane < n) x = *reinterpret_cast<const f32x2*>(ml + (size_t)(p + lane) * stride * 2);
+      const uint64_t some = __ballot(x.y != 0.0f);  // parts with outputs
       const float top = fmaxf(ref, wave_max(x.x));
       const float base = top == neg_inf() ? 0.0f : top;
       const float f = exp2_fast(ref - base), e = exp2_fast(x.x - base);
@@ -1814,13 +1825,13 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
       for (int i0 = 0;;) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          if (i0 + i >= n) continue;
+          if (!(some >> (i0 + i) & 1)) continue;
           const float w = __builtin_bit_cast(
               float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, e), i0 + i));
           o.x = __builtin_fmaf(w, y[i].x, o.x);
           o.y = __builtin_fmaf(w, y[i].y, o.y);
         }
-        if ((i0 += 8) >= n) break;
+        if ((i0 += 8) >= n || !(some >> i0)) break;
         load(i0);
       }
     }

@@ -63,8 +63,14 @@ int32_t unplanned_parts(const RowsLayout& l, int32_t num_seqs, int32_t num_kv_he
                         int64_t slots) {
   const int64_t items = (int64_t)l.max_tiles * num_kv_heads;
   if (num_seqs > 64 || num_seqs < 1 || items > slots) return 0;
-  // mean key tiles of a sequence, as the page table tells it
-  const int64_t keys = ((int64_t)num_page_ids * KF_PAGE_SIZE / kKeyTile + num_routes) / num_seqs + 1;
+  // mean key tiles of a sequence at most, as the page table tells it: pages that are
+  // reserved count too.  The parts of a row tile follow its own tokens (tile_parts): 64
+  // rows with 8K tokens reserved 14.4 us (24.2 in parts of the reserved pages), 8.9 with
+  // none, 8 drafted tokens over 300 14.5 for any reservation.  But launches that take a
+  // plan because of it pay for it: 48 trees of 8 over 300 tokens 20 us with a table of
+  // their own length, 51 with 8K reserved each and as much in max_pages_per_route.
+  const int64_t pages = std::min((int64_t)num_page_ids, (int64_t)num_routes * max_pages_per_route);
+  const int64_t keys = (pages * KF_PAGE_SIZE / kKeyTile + num_routes) / num_seqs + 1;
   int64_t parts = std::min(slots / items, (keys + kMinPart - 1) / kMinPart);
   // steps go down with the parts, the combine's turns up: 8 drafted tokens over 8K
   // tokens, 8 KV heads, 24.7 us in parts of kMinPart, 21.9 in 2 sqrt(keys) parts,

@@ -599,3 +599,24 @@ def test_splits_among_more_sequences_than_the_plan_keeps_in_lds(gpu, tree, B, fp
     ref = r.oracle()
     assert ref[2] == 6
     assert_rows(r.gpu(), ref)
+
+
+# ------------------------------------------------- pages reserved, but not held
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("tree", [False, True])
+def test_few_tokens_in_large_reservations(gpu, tree, fp8):
+    """Launches cut for reserved pages, most of whose parts see no token; as many
+    parts as one sequence gets, and bad tables among them."""
+    for lens, counts, spare in (([40], [8], 2000), ([700, 1, 0], [5, 1, 2], 700), ([64], [64], 500),
+                                ([9, 400, 3, 33], [9, 20, 3, 1], 100), ([5000], [3], 1)):
+        c = Cache(lens, H=2, fp8=fp8, part=2048, spare=spare, seed=spare)
+        if not tree:
+            counts = np.minimum(counts, np.maximum(lens, 1))
+        r = Rows(c, counts, 4, tree=tree, seed=spare)
+        assert_rows(r.gpu(), r.oracle(), f"{lens}")
+        if lens[0] == 9:
+            c.page_ids[c.routes[1][4] + 3] = -1
+            c.routes[2][5] = 0
+            ref = r.oracle()
+            assert ref[2] == 6
+            assert_rows(r.gpu(), ref)
