@@ -111,7 +111,7 @@ struct RowsArgs {
   int32_t* head;        // [0] items (-1: every row becomes NaN), [1] split tiles,
                         // [2] (row, head) pairs of the largest
   int32_t* seq_tiles;   // [num_seqs + 1] first row tile of each sequence
-  int32_t* seq_info;    // [num_seqs][4] tokens, smallest tok_begin, bad
+  int32_t* seq_info;    // [num_seqs][4] key tiles, smallest tok_begin, bad, largest tok_end
   RowsItem* items;
   RowsSplit* splits;
   float* rec_ml;        // [records][Hkv][rec_rows][2] (max, sum), base 2

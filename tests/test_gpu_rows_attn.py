@@ -620,3 +620,16 @@ def test_few_tokens_in_large_reservations(gpu, tree, fp8):
             ref = r.oracle()
             assert ref[2] == 6
             assert_rows(r.gpu(), ref)
+
+
+@pytest.mark.parametrize("part", [16, 20])
+@pytest.mark.parametrize("tree", [False, True])
+def test_planned_splits_of_short_routes(gpu, tree, part):
+    """A tile or two a route, in plans of LDS and of memory; empty routes between."""
+    for B in (70, 1030):
+        lens = [2000, 1, 700, 0, 1500] + [3] * (B - 5)
+        counts = [9, 1, 40, 2 * tree, 3] + [0, 1] * ((B - 5) // 2) + [0] * ((B - 5) % 2)
+        c = Cache(lens, H=2, part=part, seed=B)
+        c.routes[9][3] = c.routes[9][2]            # sequence 0 holds a gap
+        r = Rows(c, counts, 4, tree=tree, seed=B)
+        assert_rows(r.gpu(), r.oracle(), f"B {B}")
