@@ -64,10 +64,10 @@ __device__ __forceinline__ float wave_max(float x) {
 // else: memory bounds them.  A wave takes one page of one KV head, K or V, so that the
 // whole page is written at once (V's rows of sixteen slots turn around in registers)
 // and its fp8 scale is one wave's decision.  16K rows of 8 KV heads (134 MB): 28 us,
-// 4.9 TB/s, a copy's rate; prompts into fp8 pages (260 MB) 58 us, 4.5 TB/s; the plan
-// before them 5 us.  Appends of a few rows are one launch, bound by its chain of
-// loads (7.3 us a pass).
-//
+// 4.9 TB/s, a copy's rate; prompts into fp8 pages (260 MB) 48 .. 58 us, 4.5 .. 5.4
+// TB/s; the plan before them 5 us.  Appends of a few rows are one launch, bound by its
+// chain of loads (7.3 us a pass).
+
 // Whether row i of the table of entries decreases or leaves [0, num_entries].
 __device__ __forceinline__ bool bad_entries(const AppendRowsArgs& a, int i) {
   const int x = a.entry_begin[i], y = a.entry_begin[i + 1];
@@ -897,7 +897,7 @@ struct Walk {
   int base, n;    // its first page id's index, its tokens that the row tile sees
   int tb;         // its first token
   int j, tiles;   // next tile of the route, its tiles
-  int pid[2];     // page ids of that tile, on their way
+  int pid[2];     // page ids of that tile (sent for a step ahead, awaited at its barrier)
 };
 
 // One tile: its first token's position (of drafted tokens: its first row) and how
@@ -1225,10 +1225,15 @@ __device__ __forceinline__ void fill_nan(const RowsArgs& a, int row0, int64_t m0
 // tiles the same.  16K-token prompt, 32 / 8 heads: 2150 .. 2330 us on different
 // cards, 0.95 .. 1.02 PFLOP/s of its causal work, where the largest plain product
 // reaches 1.28 .. 1.40.  A wave's step issues 106 vector, 85 scalar, 16 LDS and 16
-// matrix instructions; the matrix cores are busy 48 % of the time, LDS, the vector
-// units and the waits for each other share the rest.  fp8 chunks over 32K tokens, 64 /
-// 8 heads: 2690 .. 2800 us, 0.80 PFLOP/s; widening adds the difference.  Trees of few
-// rows wait for memory: 48 over 2K .. 64K tokens, 4.1 GB, 671 us, 6.1 TB/s.
+// matrix instructions; the matrix cores are busy 49 % of the time.  In every step the
+// wave waits for the page ids that it has just sent for (scalar loads count with LDS,
+// whose counter the barrier waits for) and for all sixteen operands before its first
+// product.  fp8 chunks over 32K tokens, 64 / 8 heads: 2690 .. 2800 us, 0.80 PFLOP/s: 155
+// vector, 89 scalar and 23 LDS instructions a step with the widening, whose stores
+// conflict (0.7 cycles per LDS instruction), and V's operands are read in pairs behind
+// the softmax.  fp8 trees have scalar registers spilled in the loop as well (some 140;
+// 120 scalar instructions a step).  bf16 trees of few rows wait for memory: 48 over 2K ..
+// 64K tokens, 4.1 GB, 678 us, 6.0 TB/s.
 template <bool FP8, bool TREE>
 struct Work {
   const RowsArgs& a;
@@ -1399,7 +1404,7 @@ struct Work {
     }
     u32x4 k[8], v[8];
     load_k(lk, ka, k);
-    if constexpr (!FP8) load_v(lv, lane, v);  // (fp8 has no registers for it)
+    if constexpr (!FP8) load_v(lv, lane, v);  // (fp8: no registers for it beside K's)
     float top = neg_inf(), top1 = neg_inf();
     if constexpr (FP8) {
 #pragma unroll

@@ -6,8 +6,13 @@ one decode step as the paper orders it (Section 3.2, steps 3-4; Section 5.1):
 the tail routes append the step's K/V token, every route computes its partial,
 and the partials of each sequence are merged.  Prompts, drafted trees and
 accepted rows go over the same buffers (append_rows, prompt_attn, tree_attn).
-Marshalling only: the calls are the library's HIP kernels, enqueued on the current stream.  Their
-arguments are checked and marshalled once, when the state is built.
+Marshalling only: the calls are the library's HIP kernels, enqueued on the current
+stream.  The arguments of a decode step are checked and marshalled once, when the
+state is built.  Those of the calls on whole rows, whose tensors differ from call to
+call, are checked in every call, which also allocates its outputs and workspace (24 to
+35 us of host time, more than the kernels of a small tree); a loop that keeps its
+buffers binds them with kf.bind_prompt_attn, kf.bind_tree_attn and
+kf.bind_kv_append_rows (8 us a call).
 """
 from __future__ import annotations
 
