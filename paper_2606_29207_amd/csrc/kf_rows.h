@@ -42,6 +42,11 @@ constexpr int kDirectRoutes = 128;
 // there on a launch before it does: 200 entries in 1024 routes 15.2 and 17.5, in 2048
 // 18.0 and 17.7, in 4096 25 and 18, in 65535 1820 and 53.
 constexpr int kPlanRoutes = 2048;
+// Most of so many routes take few rows or none, and their workgroups are a wave each; of
+// four waves above kWaveEntries entries, where one route may take thousands: 16K listed
+// rows of one route among 4096 63 us (113 with one wave, 62 with eight), spread over all
+// of them 91 (87, 98); 1000 of one route 21 with one wave and with four.
+constexpr int kWaveEntries = 1024;
 
 // ------------------------------------------------------------------- append
 struct AppendRowsArgs {

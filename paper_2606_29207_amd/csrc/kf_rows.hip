@@ -100,9 +100,11 @@ __device__ int append_check(const AppendRowsArgs& a, int r, bool table, int& fla
     flag = KF_EFLAG_BAD_ROUTE;
   if (flag) return -1;
   bool page = false, row = false;
+#pragma unroll 4
   for (int64_t p = j0 / kPage + lane; p <= last; p += step)
     page |= (uint32_t)a.page_ids[base + p] >= (uint32_t)a.num_pages;
   if (a.row_list)
+#pragma unroll 4
     for (int i = lane; i < n; i += step) row |= (uint32_t)a.row_list[e0 + i] >= (uint32_t)a.num_rows;
   flag = any(page) ? KF_EFLAG_BAD_PAGE : any(row) ? KF_EFLAG_BAD_ROUTE : 0;
   return flag ? -1 : (int)j0;
@@ -1887,7 +1889,8 @@ hipError_t launch_append_rows(const AppendRowsArgs& a, bool fp8, hipStream_t str
     append_table_kernel<<<1, 1024, 0, stream>>>(a);
     if ((st = hipGetLastError()) != hipSuccess) return st;
   }
-  append_plan_kernel<false, false><<<a.num_routes, many ? 64 : 512, 0, stream>>>(a);
+  const int threads = !many ? 512 : a.num_entries > kWaveEntries ? 256 : 64;
+  append_plan_kernel<false, false><<<a.num_routes, threads, 0, stream>>>(a);
   if ((st = hipGetLastError()) != hipSuccess) return st;
   const int64_t tiles = append_first_tile(a.num_entries, a.num_routes);
   const int64_t grid = (tiles * 2 * a.num_kv_heads + 3) / 4;

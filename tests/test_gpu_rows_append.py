@@ -404,3 +404,31 @@ def test_all_or_none_among_many_routes(gpu, n):
             begin[-1] = len(lst) + 1
         ref = _check(c, k, v, begin, lst, flags=flags)
         assert ref[2][0][3] == (0 if "csr" in what else begin[1]), what
+
+
+@pytest.mark.parametrize("listed", [False, True])
+@pytest.mark.parametrize("n", [1000, 1024, 1025, 5000])
+def test_one_route_among_many_takes_thousands(gpu, n, listed):
+    """Checks of one route by a wave and by four; its last page and last row are looked at."""
+    R, at = 2100, 1234
+    c = Cache(np.arange(R) % 18, H=1, spare=1, seed=n)
+    c.routes[at, 4], c.routes[at, 5] = len(c.page_ids), -(-n // 16) + 2
+    pool = c.k_pool.shape[0]
+    c.page_ids = np.concatenate([c.page_ids, np.arange(c.routes[at, 5]) + pool]).astype(np.int32)
+    more = len(c.page_ids) - pool + 10
+    c.k_pool = np.concatenate([c.k_pool, np.zeros((more, *c.k_pool.shape[1:]), np.uint16)])
+    c.v_pool = np.concatenate([c.v_pool, np.zeros((more, *c.v_pool.shape[1:]), np.uint16)])
+    counts = np.zeros(R, int)
+    counts[[3, at]] = 2, n - 2
+    begin = np.concatenate([[0], np.cumsum(counts)])
+    k, v = _rows(n, 1, 1)
+    lst = np.random.default_rng(n).permutation(n) if listed else None
+    _check(c, k, v, begin, lst)
+    end = int(c.routes[at][3] - c.routes[at][2]) + n - 2
+    if listed:
+        lst[-1] = n
+        ref = _check(c, k, v, begin, lst, flags=2)
+    else:
+        c.page_ids[c.routes[at][4] + (end - 1) // 16] = -1
+        ref = _check(c, k, v, begin, lst, flags=4)
+    assert ref[2][3][3] == 3 + 2 and ref[2][at][3] == c.routes[at][3]
