@@ -76,16 +76,18 @@ __device__ __forceinline__ bool bad_entries(const AppendRowsArgs& a, int i) {
 
 // One route's check: its tokens before the append, or -1 if it takes no rows (flag
 // says why).  WHOLE: by the workgroup together; else by every wave for itself, for
-// calls of a few rows, which are a chain of loads.  table: the table of entries too.
-template <bool WHOLE>
-__device__ int append_check(const AppendRowsArgs& a, int r, bool table, int& flag) {
+// calls of a few rows, which are a chain of loads.  TABLE: the table of entries too.
+template <bool WHOLE, bool TABLE>
+__device__ int append_check(const AppendRowsArgs& a, int r, int& flag) {
   const int lane = WHOLE ? threadIdx.x : threadIdx.x & 63, step = WHOLE ? blockDim.x : 64;
+  // page ids and listed rows read at a time (a few waves: more; 1 row 7.1 us, 7.4 with 4)
+  constexpr int kAtOnce = WHOLE && !TABLE ? 4 : 1;
   auto any = [](bool x) -> bool { return WHOLE ? __syncthreads_or(x) : __ballot(x) != 0; };
   const int e0 = a.entry_begin[r], n = a.entry_begin[r + 1] - e0;
   const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + r);
   const int seq = rp[0], tb = rp[2], te = rp[3], base = rp[4], cap = rp[5];
   flag = 0;
-  if (table) {
+  if (TABLE) {
     bool bad = false;
     for (int i = lane; i < a.num_routes; i += step) bad |= bad_entries(a, i);
     flag = any(bad) ? KF_EFLAG_BAD_ROUTE : 0;
@@ -100,11 +102,11 @@ __device__ int append_check(const AppendRowsArgs& a, int r, bool table, int& fla
     flag = KF_EFLAG_BAD_ROUTE;
   if (flag) return -1;
   bool page = false, row = false;
-#pragma unroll 4
+#pragma unroll kAtOnce
   for (int64_t p = j0 / kPage + lane; p <= last; p += step)
     page |= (uint32_t)a.page_ids[base + p] >= (uint32_t)a.num_pages;
   if (a.row_list)
-#pragma unroll 4
+#pragma unroll kAtOnce
     for (int i = lane; i < n; i += step) row |= (uint32_t)a.row_list[e0 + i] >= (uint32_t)a.num_rows;
   flag = any(page) ? KF_EFLAG_BAD_PAGE : any(row) ? KF_EFLAG_BAD_ROUTE : 0;
   return flag ? -1 : (int)j0;
@@ -345,14 +347,14 @@ __global__ __launch_bounds__(1024) void append_table_kernel(AppendRowsArgs a) {
 }
 
 // One workgroup per route: the check; the plan of its pages, or with DIRECT the
-// pages themselves; the route's new end.  With DIRECT and many routes a workgroup
-// per entry: the first one of a route works on it.
-template <bool FP8, bool DIRECT>
+// pages themselves; the route's new end.  MANY routes: the table of entries has been
+// read before, or with DIRECT there is a workgroup per entry, which reads it once, and
+// the first one of a route works on it.
+template <bool FP8, bool DIRECT, bool MANY>
 __global__ __launch_bounds__(1024) void append_plan_kernel(AppendRowsArgs a) {
   __shared__ uint16_t lds[FP8 && DIRECT ? 16 * kPage * 64 : 1];
   int r = blockIdx.x;
-  bool table = true;
-  if (DIRECT && a.num_routes > kDirectRoutes) {
+  if constexpr (DIRECT && MANY) {
     __shared__ int s_route;
     if (threadIdx.x == 0) s_route = -1;
     __syncthreads();
@@ -367,13 +369,11 @@ __global__ __launch_bounds__(1024) void append_plan_kernel(AppendRowsArgs a) {
     if (bad && threadIdx.x == 0) atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
     r = bad ? -1 : s_route;
     if (r < 0) return;
-    table = false;
-  } else if (!DIRECT && a.num_routes > kPlanRoutes) {
+  } else if (MANY) {
     if (a.plan[4 * r] < 0) return;
-    table = false;
   }
   int flag = 0;
-  const int j0 = append_check<!DIRECT>(a, r, table, flag);
+  const int j0 = append_check<!DIRECT, !MANY>(a, r, flag);
   if (threadIdx.x == 0 && flag) atomicOr(a.err_flags, flag);
   if (!DIRECT && threadIdx.x == 0) a.plan[4 * r] = j0;
   if (j0 < 0) return;
@@ -1608,7 +1608,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     } else {
       const int64_t all = k + (TREE ? (n_rows + kKeyTile - 1) / kKeyTile : 0);
       const int part = item / a.max_tiles;
-      const int parts = uniform(tile_parts(a.parts, all));  // those behind them are empty
+      const int parts = tile_parts(a.parts, all);  // those behind them are empty
       it.key0 = uniform((int)(all * part / parts));
       it.key1 = part + 1 != parts ? uniform((int)(all * (part + 1) / parts)) : INT32_MAX;
     }
@@ -1876,21 +1876,26 @@ __global__ __launch_bounds__(256) void rows_combine_kernel(RowsArgs a) {
 
 hipError_t launch_append_rows(const AppendRowsArgs& a, bool fp8, hipStream_t stream) {
   if (a.num_entries <= kDirectEntries && a.num_entries <= kDirectMean * a.num_routes) {
-    const int wgs = a.num_routes > kDirectRoutes ? a.num_entries : a.num_routes;
-    if (fp8)
-      append_plan_kernel<true, true><<<wgs, 1024, 0, stream>>>(a);
+    const bool many = a.num_routes > kDirectRoutes;
+    if (fp8 && many)
+      append_plan_kernel<true, true, true><<<a.num_entries, 1024, 0, stream>>>(a);
+    else if (fp8)
+      append_plan_kernel<true, true, false><<<a.num_routes, 1024, 0, stream>>>(a);
+    else if (many)
+      append_plan_kernel<false, true, true><<<a.num_entries, 1024, 0, stream>>>(a);
     else
-      append_plan_kernel<false, true><<<wgs, 1024, 0, stream>>>(a);
+      append_plan_kernel<false, true, false><<<a.num_routes, 1024, 0, stream>>>(a);
     return hipGetLastError();
   }
   hipError_t st;
-  const bool many = a.num_routes > kPlanRoutes;
-  if (many) {
+  if (a.num_routes > kPlanRoutes) {
     append_table_kernel<<<1, 1024, 0, stream>>>(a);
     if ((st = hipGetLastError()) != hipSuccess) return st;
+    append_plan_kernel<false, false, true>
+        <<<a.num_routes, a.num_entries > kWaveEntries ? 256 : 64, 0, stream>>>(a);
+  } else {
+    append_plan_kernel<false, false, false><<<a.num_routes, 512, 0, stream>>>(a);
   }
-  const int threads = !many ? 512 : a.num_entries > kWaveEntries ? 256 : 64;
-  append_plan_kernel<false, false><<<a.num_routes, threads, 0, stream>>>(a);
   if ((st = hipGetLastError()) != hipSuccess) return st;
   const int64_t tiles = append_first_tile(a.num_entries, a.num_routes);
   const int64_t grid = (tiles * 2 * a.num_kv_heads + 3) / 4;
