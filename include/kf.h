@@ -381,8 +381,8 @@ int kf_kv_append_rows(const kf_shape* shape, void* k_pool, void* v_pool, float* 
                       int32_t* err_flags, void* stream);
 
 /*
- * kf_rows_attn_workspace_bytes -- device scratch that kf_prompt_attn and
- * kf_tree_attn need for num_rows query rows of shape->num_seqs sequences on
+ * kf_rows_attn_workspace_bytes -- device scratch that kf_prompt_attn,
+ * kf_window_attn and kf_tree_attn need for num_rows query rows of shape->num_seqs sequences on
  * the current device: the launch's list of work items, and the partials of
  * rows whose keys are split over several workgroups.  It does not depend on
  * the routes, the pages or the lengths.  No initialisation is needed; contents
@@ -431,6 +431,25 @@ int kf_prompt_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64
                    void* workspace, size_t workspace_bytes, int32_t* err_flags, void* stream);
 
 /*
+ * kf_window_attn -- kf_prompt_attn with a sliding window and attention sinks: the
+ * row at position p sees the resident tokens t <= p with t < sinks or
+ * t > p - window, and no others (window = 0: the sinks alone; a window that holds
+ * every position, or as many sinks: kf_prompt_attn).  Prompts, chunks of them, and
+ * decode steps (one row per sequence, its token appended before).  Tokens that no
+ * row sees are not read, but every route of the sequence is checked and t, p are
+ * logical positions, so that a launch costs what its rows see, whatever the cache
+ * holds.  sinks, window >= 0.  Arguments, outputs, checks, alignment and workspace
+ * (kf_rows_attn_workspace_bytes) otherwise as for kf_prompt_attn.
+ */
+int kf_window_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64_t q_stride,
+                   const int32_t* seq_row_begin, const int32_t* first_pos, int32_t sinks,
+                   int32_t window, const void* k_pool, const void* v_pool, const float* k_scale,
+                   const float* v_scale, const kf_route* routes, int32_t num_routes,
+                   int32_t max_pages_per_route, const int32_t* page_ids,
+                   const int32_t* seq_route_begin, void* out, float* lse, void* workspace,
+                   size_t workspace_bytes, int32_t* err_flags, void* stream);
+
+/*
  * kf_tree_attn -- attention of drafted tokens over the cache and over their own
  * tree.  Rows as for kf_prompt_attn, at most KF_MAX_DRAFT per sequence; row i
  * of sequence b sees every resident token of the sequence's routes and the
@@ -450,6 +469,82 @@ int kf_tree_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64_t
                  const kf_route* routes, int32_t num_routes, int32_t max_pages_per_route,
                  const int32_t* page_ids, const int32_t* seq_route_begin, void* out, float* lse,
                  void* workspace, size_t workspace_bytes, int32_t* err_flags, void* stream);
+
+/*
+ * Operators that keep a cache within a budget: what each cached token has meant to
+ * the queries so far, and the removal of those that meant least.  (kf_window_attn
+ * above bounds what is read instead.)  Token weights are float32
+ * [num_pages][num_kv_heads][16 slots] in either pool layout, beside the pools and
+ * indexed as they are.
+ */
+
+/*
+ * kf_attn_weights -- the attention weight that each resident token received from
+ * rows of queries, added to what it had: for every route of a sequence with rows,
+ * token t of it and KV head g,
+ *   weights[t][g] = old + sum over the rows i that see t (t <= p, as for
+ *     kf_prompt_attn) and the query heads h of g's group of
+ *     exp(scale * (q[i][h] . k_t) - lse[i][h]),
+ *   old = decay * weights[t][g] for t < first_pos[b], else 0,
+ * where lse [num_rows][num_q_heads] is what the rows' attention returned.  A token
+ * whose own row is in the call is new and starts from 0, so that a decode step's
+ * call (one row per sequence, first_pos its position), a prompt's and a chunk's
+ * need no clearing; with decay = 0 weights are not read.  A row whose lse is -inf
+ * or NaN gives nothing.  Sums are float32; the same arguments give the same bits.
+ * q and lse as for kf_prompt_attn (q_stride elements between rows of q).
+ * Routes are taken one by one, as kf_partial_attn takes them, and weights of
+ * sequences without rows, and of slots that hold no token, are left as they were.
+ * max_pages_per_route as for kf_prompt_attn.
+ * Device checks: a route whose sequence is outside [0, num_seqs), or whose
+ * sequence's row of seq_row_begin decreases or leaves [0, num_rows], or that fails
+ * kf_partial_attn's checks sets KF_EFLAG_BAD_ROUTE and is left as it was; tokens of
+ * a page whose id lies outside the pool set KF_EFLAG_BAD_PAGE and have no weight.
+ * At most 65535 routes in a call.
+ * Alignment: q and k_pool 16 bytes, the rest 4.
+ */
+int kf_attn_weights(const kf_shape* shape, const void* q, int32_t num_rows, int64_t q_stride,
+                    const float* lse, const int32_t* seq_row_begin, const int32_t* first_pos,
+                    const void* k_pool, const float* k_scale, const kf_route* routes,
+                    int32_t num_routes, int32_t max_pages_per_route, const int32_t* page_ids,
+                    float decay, float* weights, int32_t* err_flags, void* stream);
+
+/*
+ * kf_kv_evict -- eviction by weight: of the L tokens of sequence b, in the order of
+ * its routes, K = min(L, keep[b]) stay, for each KV head by itself: the first
+ * F = min(K, keep_first), the last R = min(K - F, keep_last), and of those between
+ * them the K - F - R of the largest weights (the earlier of equal ones; NaN below
+ * all others; -0 equals 0).  They move, in their order, into the pages of route
+ * into[b] -- one of the sequence's own rows of the table, without tokens, page_cap
+ * pages reserved -- with their weights, and the routes' rows follow:
+ * routes[into[b]].tok_end = tok_begin + K, and every other route of the sequence is
+ * empty, its pages the caller's again.  Nothing else of the pools changes: not the
+ * pages that the tokens came from, not the slots behind the last one.  into[b] = -1
+ * leaves sequence b alone.  max_keep bounds keep[b].
+ * The table, the CSR rows and a later kf_decode_step agree without the host: give
+ * into as the tail_route that follows, and the emptied route as the next call's.
+ * Positions (kf_prompt_attn, kf_window_attn, kf_attn_weights) are those of the
+ * routes: the kept tokens sit at tok_begin .. tok_begin + K - 1.
+ * bf16 pools: bits are copied.  fp8 pools, per page and KV head, K and V apart: a
+ * page whose tokens all had one scale takes it and their codes; another takes the
+ * largest of their scales s' (by size), and a code of scale s becomes the E4M3 code
+ * nearest to decode(code) * s / s' (float32, ties to even, clamped to +-448, a NaN's
+ * stays): kf_kv_append goes on from either.
+ * A sequence is evicted whole or not at all.  Device checks (flag, that sequence
+ * unchanged): its CSR row, at most 1024 routes, each sound (kf_partial_attn's checks)
+ * and its own, into[b] among them and empty, 0 <= keep[b] <= max_keep, L below 2^31 -
+ * 1024 (KF_EFLAG_BAD_ROUTE); pages reserved for K tokens (KF_EFLAG_TAIL_FULL); page
+ * ids of the tokens and of the pages that they go to (KF_EFLAG_BAD_PAGE).
+ * workspace: kf_kv_evict_workspace_bytes(shape, max_keep), 16-byte aligned; dead
+ * between calls, and calls that may overlap need their own.  0 for invalid
+ * arguments and for more than 65535 sequences or KV heads, which no launch takes.
+ * Alignment: pools 16 bytes, the rest 4.
+ */
+size_t kf_kv_evict_workspace_bytes(const kf_shape* shape, int32_t max_keep);
+int kf_kv_evict(const kf_shape* shape, void* k_pool, void* v_pool, float* k_scale, float* v_scale,
+                float* weights, kf_route* routes, int32_t num_routes, int32_t max_pages_per_route,
+                const int32_t* page_ids, const int32_t* seq_route_begin, const int32_t* into,
+                const int32_t* keep, int32_t max_keep, int32_t keep_first, int32_t keep_last,
+                void* workspace, size_t workspace_bytes, int32_t* err_flags, void* stream);
 
 /*
  * kf_debug_gather -- test export: the resident tokens of route `route`

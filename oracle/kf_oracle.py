@@ -383,10 +383,11 @@ def kv_append_rows(k_pool, v_pool, routes, page_ids, k_rows, v_rows, route_entry
 
 def rows_attn(q, row_begin, k_pool, v_pool, routes, page_ids, seq_route_begin, *, num_kv_heads,
               scale, max_pages_per_route, first_pos=None, tree_mask=None, k_draft=None,
-              v_draft=None, k_scale=None, v_scale=None, max_draft=64):
+              v_draft=None, k_scale=None, v_scale=None, max_draft=64, sinks=0, window=None):
     """Attention of packed query rows (bf16 bits [N, Hq, d]) over the cache of
     their sequences.  Prompts (first_pos): row i of sequence b sits at position
-    first_pos[b] + i - row_begin[b] and sees the resident tokens up to it.  Trees
+    first_pos[b] + i - row_begin[b] and sees the resident tokens up to it; with a
+    window, of those only t < sinks and t > position - window.  Trees
     (tree_mask): it sees every resident token, and the drafted rows
     row_begin[b] + j (bf16 bits [N, Hkv, d]) of its mask's bits j.
 
@@ -421,7 +422,10 @@ def rows_attn(q, row_begin, k_pool, v_pool, routes, page_ids, seq_route_begin, *
                         np.asarray(page_ids))
         n = i1 - i0
         if tree_mask is None:
-            sees = tok[None, :] <= (int(first_pos[b]) + np.arange(n))[:, None]
+            at = (int(first_pos[b]) + np.arange(n))[:, None]
+            sees = tok[None, :] <= at
+            if window is not None:
+                sees &= (tok[None, :] < sinks) | (tok[None, :] > at - window)
         else:
             bits = np.asarray(tree_mask[i0:i1]).astype(np.int64).view(np.uint64)
             drafted = (bits[:, None] >> np.arange(n, dtype=np.uint64)[None, :]) & np.uint64(1)
@@ -445,6 +449,133 @@ def rows_attn(q, row_begin, k_pool, v_pool, routes, page_ids, seq_route_begin, *
                     rows, K[at], V[at], scale)
                 spread[i0 + i, g * G:(g + 1) * G] = attend(rows, K[at], np.abs(V[at]), scale)[0]
     return out, lse, flags, spread
+
+
+def attn_weights(q, lse, row_begin, first_pos, k_pool, routes, page_ids, weights, *,
+                 num_kv_heads, scale, decay, max_pages_per_route, k_scale=None):
+    """The attention weight that every resident token and KV head received from the
+    rows (bf16 bits [N, Hq, d]; lse [N, Hq]), after decay * what it had; a token at
+    or behind its sequence's first_pos had nothing.  weights [P, Hkv, 16].
+
+    Returns the new weights (float64), flags, and the number of terms that each sum
+    has at most."""
+    N, Hq, d = q.shape
+    G = Hq // num_kv_heads
+    B = len(row_begin) - 1
+    out = np.array(weights, np.float64)
+    flags = terms = 0
+    safe = np.clip(np.asarray(page_ids, np.int64), 0, k_pool.shape[0] - 1)
+    for r in range(len(routes)):
+        b = int(routes[r][0])
+        if not 0 <= b < B:
+            flags |= EFLAG_BAD_ROUTE
+            continue
+        i0, i1 = int(row_begin[b]), int(row_begin[b + 1])
+        if i0 == i1 and 0 <= i0 <= N:
+            continue
+        if not 0 <= i0 <= i1 <= N or not _route_ok(routes[r], B, len(page_ids),
+                                                   max_pages_per_route):
+            flags |= EFLAG_BAD_ROUTE
+            continue
+        tok = np.arange(routes[r][2], routes[r][3], dtype=np.int64)
+        at = int(routes[r][4]) + np.arange(len(tok)) // PAGE
+        pid = np.asarray(page_ids)[at]
+        good = (pid >= 0) & (pid < k_pool.shape[0])
+        flags |= 0 if good.all() else EFLAG_BAD_PAGE
+        terms = max(terms, (i1 - i0) * G)
+        sees = tok[None, :] <= (int(first_pos[b]) + np.arange(i1 - i0))[:, None]
+        slot = np.arange(len(tok)) % PAGE
+        for g in range(num_kv_heads):
+            K, _ = gather_kv(routes[r], safe, k_pool, np.swapaxes(k_pool, 2, 3), g, k_scale, k_scale)
+            total = np.zeros(len(tok))
+            for i in range(i0, i1):
+                for h in range(g * G, (g + 1) * G):
+                    z = float(lse[i, h])
+                    if not z > -np.inf:
+                        continue
+                    e = np.exp(scale * (K @ bf16_to_f64(q[i, h])) - z)
+                    total += np.where(sees[i - i0], e, 0.0)
+            old = out[pid[good], g, slot[good]] if decay != 0 else np.zeros(int(good.sum()))
+            old = np.where(tok[good] < int(first_pos[b]), decay * old, 0.0)
+            out[pid[good], g, slot[good]] = old + total[good]
+    return out, flags, terms
+
+
+def kv_evict(k_pool, v_pool, weights, routes, page_ids, seq_route_begin, into, keep, *, max_keep,
+             keep_first, keep_last, max_pages_per_route, k_scale=None, v_scale=None):
+    """Eviction by weight: of each sequence's tokens at most keep[b] stay per KV head
+    (the first keep_first, the last keep_last, the heaviest others, the earlier of
+    equal ones), moved in order into the pages of the empty route into[b].  Pools
+    [P, Hkv, 16, d] and [P, Hkv, d, 16].  Returns copies of everything that changes:
+    k_pool, v_pool, weights, routes, k_scale, v_scale, flags."""
+    k_pool, v_pool, weights, routes = (np.array(x) for x in (k_pool, v_pool, weights, routes))
+    fp8 = k_scale is not None
+    k_scale, v_scale = (np.array(x) if fp8 else None for x in (k_scale, v_scale))
+    P, H = k_pool.shape[:2]
+    flags = 0
+    for b in range(len(seq_route_begin) - 1):
+        r0, r1, to = int(seq_route_begin[b]), int(seq_route_begin[b + 1]), int(into[b])
+        if to == -1:
+            continue
+        rows = range(r0, r1)
+        if (not 0 <= r0 <= r1 <= len(routes) or r1 - r0 > 1024 or not r0 <= to < r1
+                or not 0 <= int(keep[b]) <= max_keep
+                or any(not _route_ok(routes[r], len(seq_route_begin) - 1, len(page_ids),
+                                     max_pages_per_route) or int(routes[r][0]) != b for r in rows)
+                or routes[to][3] != routes[to][2]):
+            flags |= EFLAG_BAD_ROUTE
+            continue
+        src = [(int(routes[r][4]) + j // PAGE, j % PAGE) for r in rows
+               for j in range(int(routes[r][3]) - int(routes[r][2]))]
+        L = len(src)
+        K = min(L, int(keep[b]))
+        pages = -(-K // PAGE)
+        if pages > routes[to][5]:
+            flags |= EFLAG_TAIL_FULL
+            continue
+        if int(routes[to][2]) + K > 2 ** 31 - 1 or int(routes[to][4]) + pages > len(page_ids):
+            flags |= EFLAG_BAD_ROUTE
+            continue
+        spid = np.array([page_ids[p] for p, _ in src], np.int64).reshape(-1)
+        sslot = np.array([s for _, s in src], np.int64).reshape(-1)
+        dpid = np.asarray(page_ids, np.int64)[int(routes[to][4]):int(routes[to][4]) + pages]
+        if any(np.any((x < 0) | (x >= P)) for x in (spid, dpid)):
+            flags |= EFLAG_BAD_PAGE
+            continue
+        first = min(K, keep_first)
+        last = min(K - first, keep_last)
+        mid = np.arange(first, L - last)
+        for g in range(H):
+            w = np.array(weights[spid[mid], g, sslot[mid]], np.float64) + 0.0
+            heavy = mid[np.lexsort((mid, -np.where(np.isnan(w), 0.0, w), np.isnan(w)))]
+            stay = np.sort(np.concatenate([np.arange(first), heavy[:K - first - last],
+                                           np.arange(L - last, L)])).astype(int)
+            for p in range(pages):
+                idx = stay[p * PAGE:(p + 1) * PAGE]
+                sp, ss, n = spid[idx], sslot[idx], len(idx)
+                k, v = k_pool[sp, g, ss], v_pool[sp, g, :, ss]
+                if fp8:
+                    k, k_scale[dpid[p], g] = _one_scale(k, k_scale[sp, g])
+                    v, v_scale[dpid[p], g] = _one_scale(v, v_scale[sp, g])
+                k_pool[dpid[p], g, :n] = k
+                v_pool[dpid[p], g, :, :n] = v.T
+                weights[dpid[p], g, :n] = weights[sp, g, ss]
+        for r in rows:
+            routes[r][3] = routes[r][2] + (K if r == to else 0)
+    return k_pool, v_pool, weights, routes, k_scale, v_scale, flags
+
+
+def _one_scale(codes, was):
+    """E4M3 codes [n, d] of the scales was [n] under one scale: theirs if it is one,
+    else the largest by size."""
+    if np.all(was.view(np.uint32) == was.view(np.uint32)[0]):
+        return codes, was[0]
+    now = np.float32(np.max(np.abs(was)))
+    x = e4m3_to_f64(codes).astype(np.float32) * was[:, None].astype(np.float32) / now
+    new = e4m3_encode_rne(np.where(np.isnan(x), np.float32(448), np.clip(x, -448, 448)))
+    new = np.where((codes & 0x7F) == 0x7F, codes, new)
+    same = was.view(np.uint32) == now.view(np.uint32)
+    return np.where(same[:, None], codes, new), now
 
 
 # --------------------------------------------------------------------- bytes

@@ -1,0 +1,63 @@
+// Internal interface between the C-ABI layer of the cache-budget operators
+// (kf_budget_api.cpp) and their gfx950 kernels (kf_budget.hip).
+#pragma once
+
+#include "kf_internal.h"
+
+namespace kf {
+
+constexpr int64_t kMaxBudgetWgs = 0xFFFFFF;  // workgroups of a launch: 32 bits of threads
+
+// ------------------------------------------------------------- attn_weights
+constexpr int kFewColumns = 64;  // (row, head) pairs of a sequence that stay in registers
+
+struct AttnWeightsArgs {
+  const uint16_t* q;
+  int64_t q_stride;
+  const float* lse;
+  const int32_t* seq_row_begin;
+  const int32_t* first_pos;
+  const void* k_pool;
+  const float* k_scale;
+  const kf_route* routes;
+  const int32_t* page_ids;
+  float* weights;  // [num_pages][Hkv][kPage]
+  int32_t* err_flags;
+  float decay, scale_log2;
+  int32_t num_rows, num_seqs, num_q_heads, num_kv_heads, group;
+  int32_t num_routes, max_pages_per_route, num_pages, num_page_ids;
+  int32_t head_major;
+  int32_t chunk_pages, chunks;  // pages of a workgroup, workgroups of a route and KV head
+  int32_t key_waves;            // waves beside each other along the keys: 1, 2 or 4 of 4
+};
+
+// Fills chunk_pages, chunks and key_waves for `slots` resident workgroups.
+void plan_attn_weights(AttnWeightsArgs& a, int64_t slots);
+
+hipError_t launch_attn_weights(const AttnWeightsArgs& a, bool fp8, hipStream_t stream);
+
+// -------------------------------------------------------------------- evict
+struct EvictArgs {
+  void* k_pool;
+  void* v_pool;
+  float* k_scale;
+  float* v_scale;
+  float* weights;
+  kf_route* routes;
+  const int32_t* page_ids;
+  const int32_t* seq_route_begin;
+  const int32_t* into;
+  const int32_t* keep;
+  int32_t* err_flags;
+  int32_t num_seqs, num_kv_heads, num_routes, max_pages_per_route, num_pages, num_page_ids;
+  int32_t head_major;
+  int32_t max_keep, keep_first, keep_last;
+  // workspace
+  int32_t* plan;  // [num_seqs][2]: tokens kept (-1: the sequence is left alone), index of the
+                  // first page id that they go to
+  int32_t* list;  // [num_seqs][Hkv][max_keep]: page * kPage + slot of each, in order
+};
+
+hipError_t launch_evict(const EvictArgs& a, bool fp8, hipStream_t stream);
+
+}  // namespace kf

@@ -1,0 +1,171 @@
+// C-ABI layer of the operators that keep a cache within a budget: host-side
+// argument checks, workspace sizing and launches on the caller's stream.
+// Declarations and the contract of every entry point are in include/kf.h.
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "kf.h"
+#include "kf_budget.h"
+
+namespace {
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+bool fp8_pool(const kf_shape* s) { return s->kv_dtype == KF_KV_FP8_E4M3; }
+
+hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
+
+int64_t div_up(int64_t x, int64_t y) { return (x + y - 1) / y; }
+
+size_t evict_list_offset(int32_t num_seqs) {
+  return ((size_t)num_seqs * 2 * sizeof(int32_t) + 255) / 256 * 256;
+}
+
+// A page and a slot of it share 31 bits of the list of what stays.
+bool pages_fit(const kf_shape* s) { return s->num_pages <= INT32_MAX / KF_PAGE_SIZE; }
+
+}  // namespace
+
+extern "C" {
+
+int kf_attn_weights(const kf_shape* shape, const void* q, int32_t num_rows, int64_t q_stride,
+                    const float* lse, const int32_t* seq_row_begin, const int32_t* first_pos,
+                    const void* k_pool, const float* k_scale, const kf_route* routes,
+                    int32_t num_routes, int32_t max_pages_per_route, const int32_t* page_ids,
+                    float decay, float* weights, int32_t* err_flags, void* stream) {
+  const int st = kf::check_shape(shape);
+  if (st != KF_OK) return st;
+  if (num_rows < 0 || num_routes < 0 || max_pages_per_route < 0 || !isfinite(decay))
+    return KF_ERR_INVALID_ARG;
+  if (num_rows == 0 || num_routes == 0 || shape->num_seqs == 0) return KF_OK;
+  if (!q || !lse || !seq_row_begin || !first_pos || !k_pool || !routes || !weights || !err_flags ||
+      (shape->num_page_ids > 0 && !page_ids) || (fp8_pool(shape) && !k_scale))
+    return KF_ERR_INVALID_ARG;
+  if (q_stride < (int64_t)shape->num_q_heads * KF_HEAD_DIM || q_stride % 8 != 0)
+    return KF_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(k_pool, 16)) return KF_ERR_INVALID_ARG;
+  const void* p4[] = {lse, seq_row_begin, first_pos, k_scale, routes, page_ids, weights, err_flags};
+  for (const void* p : p4)
+    if (p && !aligned(p, 4)) return KF_ERR_INVALID_ARG;
+  const int32_t H = shape->num_kv_heads, group = shape->num_q_heads / H;
+  if (num_routes > kf::kMaxLaunchRoutes || (int64_t)num_rows * group > INT32_MAX - 256 ||
+      (int64_t)num_routes * H > kf::kMaxBudgetWgs)
+    return KF_ERR_UNSUPPORTED;
+
+  kf::AttnWeightsArgs a{};
+  a.q = static_cast<const uint16_t*>(q);
+  a.q_stride = q_stride;
+  a.lse = lse;
+  a.seq_row_begin = seq_row_begin;
+  a.first_pos = first_pos;
+  a.k_pool = k_pool;
+  a.k_scale = k_scale;
+  a.routes = routes;
+  a.page_ids = page_ids;
+  a.weights = weights;
+  a.err_flags = err_flags;
+  a.decay = decay;
+  a.scale_log2 = (float)((double)shape->scale * 1.4426950408889634074);
+  a.num_rows = num_rows;
+  a.num_seqs = shape->num_seqs;
+  a.num_q_heads = shape->num_q_heads;
+  a.num_kv_heads = H;
+  a.group = group;
+  a.num_routes = num_routes;
+  a.max_pages_per_route = max_pages_per_route;
+  a.num_pages = shape->num_pages;
+  a.num_page_ids = shape->num_page_ids;
+  a.head_major = shape->kv_layout == KF_KV_HEAD_MAJOR;
+  kf::plan_attn_weights(a, 2 * (int64_t)kf::cu_count());
+  return kf::launch_attn_weights(a, fp8_pool(shape), as_stream(stream)) == hipSuccess ? KF_OK
+                                                                                     : KF_ERR_HIP;
+}
+
+size_t kf_kv_evict_workspace_bytes(const kf_shape* shape, int32_t max_keep) {
+  if (kf::check_shape(shape) != KF_OK || max_keep < 0) return 0;
+  if (shape->num_seqs > kf::kMaxLaunchRoutes || shape->num_kv_heads > kf::kMaxLaunchRoutes) return 0;
+  return evict_list_offset(shape->num_seqs) + 256 +
+         (size_t)shape->num_seqs * shape->num_kv_heads * max_keep * sizeof(int32_t);
+}
+
+int kf_kv_evict(const kf_shape* shape, void* k_pool, void* v_pool, float* k_scale, float* v_scale,
+                float* weights, kf_route* routes, int32_t num_routes, int32_t max_pages_per_route,
+                const int32_t* page_ids, const int32_t* seq_route_begin, const int32_t* into,
+                const int32_t* keep, int32_t max_keep, int32_t keep_first, int32_t keep_last,
+                void* workspace, size_t workspace_bytes, int32_t* err_flags, void* stream) {
+  const int st = kf::check_shape(shape);
+  if (st != KF_OK) return st;
+  if (num_routes < 0 || max_pages_per_route < 0 || max_keep < 0 || keep_first < 0 || keep_last < 0)
+    return KF_ERR_INVALID_ARG;
+  if (shape->num_seqs == 0 || num_routes == 0) return KF_OK;
+  if (!k_pool || !v_pool || !weights || !routes || !seq_route_begin || !into || !keep ||
+      !err_flags || (shape->num_page_ids > 0 && !page_ids))
+    return KF_ERR_INVALID_ARG;
+  if (fp8_pool(shape) && (!k_scale || !v_scale)) return KF_ERR_INVALID_ARG;
+  if (!aligned(k_pool, 16) || !aligned(v_pool, 16)) return KF_ERR_INVALID_ARG;
+  const void* p4[] = {k_scale, v_scale, weights, routes, page_ids, seq_route_begin, into, keep,
+                      err_flags};
+  for (const void* p : p4)
+    if (p && !aligned(p, 4)) return KF_ERR_INVALID_ARG;
+  const int64_t pages = div_up(max_keep, KF_PAGE_SIZE);
+  const size_t need = kf_kv_evict_workspace_bytes(shape, max_keep);
+  if (need == 0 || !pages_fit(shape) ||
+      (div_up(pages * 2 * shape->num_kv_heads, 4) + 1) * shape->num_seqs > kf::kMaxBudgetWgs ||
+      (int64_t)shape->num_kv_heads * shape->num_seqs * 4 > kf::kMaxBudgetWgs)
+    return KF_ERR_UNSUPPORTED;
+  if (!workspace || !aligned(workspace, 16) || workspace_bytes < need) return KF_ERR_WORKSPACE;
+
+  kf::EvictArgs a{};
+  a.k_pool = k_pool;
+  a.v_pool = v_pool;
+  a.k_scale = k_scale;
+  a.v_scale = v_scale;
+  a.weights = weights;
+  a.routes = routes;
+  a.page_ids = page_ids;
+  a.seq_route_begin = seq_route_begin;
+  a.into = into;
+  a.keep = keep;
+  a.err_flags = err_flags;
+  a.num_seqs = shape->num_seqs;
+  a.num_kv_heads = shape->num_kv_heads;
+  a.num_routes = num_routes;
+  a.max_pages_per_route = max_pages_per_route;
+  a.num_pages = shape->num_pages;
+  a.num_page_ids = shape->num_page_ids;
+  a.head_major = shape->kv_layout == KF_KV_HEAD_MAJOR;
+  a.max_keep = max_keep;
+  a.keep_first = keep_first;
+  a.keep_last = keep_last;
+  a.plan = static_cast<int32_t*>(workspace);
+  a.list = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) +
+                                      evict_list_offset(shape->num_seqs));
+  return kf::launch_evict(a, fp8_pool(shape), as_stream(stream)) == hipSuccess ? KF_OK : KF_ERR_HIP;
+}
+
+}  // extern "C"
+
+namespace kf {
+
+// How a launch's keys are dealt out, by what the host knows: the pages that the table
+// reserves, and the (row, head) pairs of a sequence on the mean.
+void plan_attn_weights(AttnWeightsArgs& a, int64_t slots) {
+  const int64_t most = std::max(1, a.max_pages_per_route);
+  const int64_t pages = std::max<int64_t>(1, std::min((int64_t)a.num_page_ids, a.num_routes * most)) *
+                        a.num_kv_heads;
+  int64_t chunk;
+  if ((int64_t)a.num_rows * a.group <= (int64_t)kFewColumns * a.num_seqs) {
+    a.key_waves = 4;
+    chunk = std::min<int64_t>(128, std::max<int64_t>(16, pages / (4 * slots) / 16 * 16));
+  } else {
+    a.key_waves = pages >= 32 * slots ? 4 : pages >= 16 * slots ? 2 : 1;
+    chunk = 4 * a.key_waves;
+  }
+  while (div_up(most, chunk) * a.num_kv_heads * a.num_routes > kMaxBudgetWgs) chunk *= 2;
+  a.chunk_pages = (int32_t)std::min<int64_t>(chunk, INT32_MAX / 2);
+  a.chunks = (int32_t)div_up(most, a.chunk_pages);
+}
+
+}  // namespace kf

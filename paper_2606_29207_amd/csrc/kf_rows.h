@@ -93,7 +93,7 @@ struct RowsArgs {
   const uint16_t* q;
   int64_t q_stride;
   const int32_t* seq_row_begin;
-  const int32_t* first_pos;    // prompts
+  const int32_t* first_pos;    // prompts, rows with a window
   const uint16_t* k_draft;     // trees
   const uint16_t* v_draft;
   int64_t kv_stride;
@@ -127,6 +127,8 @@ struct RowsArgs {
   int32_t slots;        // resident workgroups
   int32_t parts;        // > 0: no plan; every row tile in so many parts at most
   int32_t may_split;    // a plan may split row tiles: a combine follows
+  int32_t sinks, window;  // window < 0: none (last: the kernels' arguments before them keep
+                          // their places, and with those the scalar registers of their loads)
 };
 
 struct RowsLayout {
@@ -138,9 +140,10 @@ RowsLayout rows_layout(int32_t num_rows, int32_t num_seqs, int32_t num_kv_heads,
                        int64_t cus);
 
 // Parts per row tile, at most, of a launch that runs without a plan, 0 with one.
+// most_keys: key tiles that a row tile sees at most, whatever the cache holds.
 int32_t unplanned_parts(const RowsLayout& l, int32_t num_seqs, int32_t num_kv_heads,
                         int32_t num_routes, int32_t num_page_ids, int32_t max_pages_per_route,
-                        int64_t slots);
+                        int64_t most_keys, int64_t slots);
 
 hipError_t launch_rows_attn(const RowsArgs& a, bool fp8, bool tree, hipStream_t stream);
 

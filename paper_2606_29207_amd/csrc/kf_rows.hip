@@ -1,65 +1,18 @@
 // gfx950 kernels of the operators on whole rows of tokens:
 //   append_plan_kernel, append_tile_kernel -- rows of K/V into the paged cache
 //   rows_plan_kernel     -- work items of an attention launch
-//   rows_kernel          -- attention of prompt rows or drafted trees over it
+//   rows_kernel          -- attention of prompt rows, of rows with a window, or of
+//                           drafted trees over it
 //   rows_combine_kernel  -- reduction of the row tiles whose keys were split
+#include "kf_device.h"
 #include "kf_rows.h"
 
 namespace kf {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
 constexpr float kLn2 = 0.69314718055994530942f;
 
-__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
-__device__ __forceinline__ float qnan() { return __builtin_nanf(""); }
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  bf16x2 v = {(__bf16)lo, (__bf16)hi};
-  return __builtin_bit_cast(uint32_t, v);
-}
-
-// Slice index of (page, KV head) in a pool of either layout.
-__device__ __forceinline__ size_t slice_of(int page, int g, int H, int P, int32_t head_major) {
-  return head_major ? (size_t)g * P + page : (size_t)page * H + g;
-}
-
-template <class T>
-__device__ __forceinline__ u32x4 ld16(const T* p) {
-  return *reinterpret_cast<const u32x4*>(p);
-}
-
 // ------------------------------------------------------------------- append
-// E4M3FN codes of two floats, round to nearest even, clamped to +-448, the
-// sign bit the input's (a NaN becomes 448), in the low half.
-__device__ __forceinline__ uint32_t e4m3_pair(float x, float y) {
-  x = __builtin_copysignf(fminf(fabsf(x), 448.0f), x);
-  y = __builtin_copysignf(fminf(fabsf(y), 448.0f), y);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false) & 0xFFFFu;
-}
-
-// Values of the two codes in the low half (exact).
-__device__ __forceinline__ f32x2 e4m3_values(uint32_t codes) {
-  const uint32_t b = __builtin_bit_cast(
-      uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, false));
-  return f32x2{__builtin_bit_cast(float, b << 16), __builtin_bit_cast(float, b & 0xFFFF0000u)};
-}
-
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) x = fmaxf(x, __shfl_xor(x, m));
-  return x;
-}
-
 // Appends move 512 bytes in and 512 (fp8 256) out per token and KV head, and nothing
 // else: memory bounds them.  A wave takes one page of one KV head, K or V, so that the
 // whole page is written at once (V's rows of sixteen slots turn around in registers)
@@ -461,13 +414,24 @@ __device__ __forceinline__ int64_t wave_sum(int64_t x) {
 // estimate where the routes leave gaps or part-filled tiles).  Tokens / 32 would leave
 // the tiles of short routes to the last part: 16 trees of 8 over 8K tokens in routes of
 // 16 tokens 278 us, 599 that way, of 48 tokens 145 and 223, of 256 the same.
-template <bool TREE>
+// (With a window: the tokens of the sinks and from the first row's window on, in the
+// same proportion, and two tiles at their ends.)
+template <bool TREE, bool WINDOW>
 __device__ __forceinline__ int key_tiles(const RowsArgs& a, int pos, int t, int n, int tiles,
                                          int first, int last) {
   if (TREE) return tiles + (n + kKeyTile - 1) / kKeyTile;
   const int64_t rows = ((int64_t)(t + 1) * kRowTile - 1) / a.group;
   const int64_t end = pos + (rows < n ? rows : n - 1) + 1 - first, span = (int64_t)last - first;
   if (end <= 0 || span <= 0) return 0;
+  if (WINDOW) {
+    const int64_t e = end < span ? end : span;
+    const int64_t row0 = (int64_t)t * kRowTile / a.group;
+    int64_t lo = pos + row0 - a.window + 1 - first, si = (int64_t)a.sinks - first;
+    lo = lo < 0 ? 0 : lo < e ? lo : e;
+    si = si < 0 ? 0 : si < lo ? si : lo;
+    const int64_t k = ((e - lo + si) * tiles + span - 1) / span + 2;
+    return (int)(k < tiles ? k : tiles);
+  }
   if (end >= span) return tiles;
   const int64_t plain = (span + kKeyTile - 1) / kKeyTile;
   return (int)(tiles == plain ? (end + kKeyTile - 1) / kKeyTile : (end * tiles + span - 1) / span);
@@ -481,7 +445,7 @@ __device__ __forceinline__ int key_tiles(const RowsArgs& a, int pos, int t, int 
 // route, of 64 267 and 262.
 constexpr int kPlanSeqs = 1024;
 
-template <bool TREE>
+template <bool TREE, bool WINDOW>
 __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
   __shared__ unsigned long long s_work;
   __shared__ int s_most, s_least, s_recs, s_parts, s_splits, s_pairs;
@@ -627,7 +591,7 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
     b = lo;
     wrong = info[4 * b + 2] != 0;
     if (wrong) return 1;
-    const int k = key_tiles<TREE>(a, TREE ? 0 : pos[b], t - tiles_of[b], begin[b + 1] - begin[b],
+    const int k = key_tiles<TREE, WINDOW>(a, TREE ? 0 : pos[b], t - tiles_of[b], begin[b + 1] - begin[b],
                                   info[4 * b], info[4 * b + 1], info[4 * b + 3]);
     return k > 0 ? k : 1;
   };
@@ -866,11 +830,6 @@ __device__ __forceinline__ int tile_parts(int most, int64_t all) {
 }
 
 // ---------------------------------------------------------------- attention
-__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
 // The x of the lower and of the upper of this lane and the one 32 away.  (The
 // compiler's builtin for this instruction returns its first result twice.)
 __device__ __forceinline__ f32x2 both_halves(float x) {
@@ -887,18 +846,14 @@ __device__ __forceinline__ float sum_halves(float x) {
   return u.x + u.y;
 }
 
-// Tables that no kernel of the launch writes, read through the scalar cache.
-template <class T>
-__device__ __forceinline__ const __attribute__((address_space(4))) T* fixed(const T* p) {
-  return (const __attribute__((address_space(4))) T*)(uintptr_t)p;
-}
-
 // The visible tokens of a sequence as tiles of 32, route after route.
 struct Walk {
   int r, r_end;   // current route, the sequence's last + 1
-  int base, n;    // its first page id's index, its tokens that the row tile sees
+  int base, n;    // its first page id's index, its tokens that the row tile sees (with a
+                  // window: those before the tile's last row, in its window or not)
   int tb;         // its first token
   int j, tiles;   // next tile of the route, its tiles
+  int from, to;   // with a window: the tile behind the sinks, where the window begins
   int pid[2];     // page ids of that tile (sent for a step ahead, awaited at its barrier)
 };
 
@@ -928,27 +883,78 @@ __device__ __forceinline__ void walk_ids(const RowsArgs& a, Walk& w) {
   for (int i = 0; i < 2; ++i) w.pid[i] = fixed(a.page_ids)[w.base + min(2 * w.j + i, last)];
 }
 
-// Enters route w.r at tile j.
-__device__ __forceinline__ void walk_enter(const RowsArgs& a, Walk& w, int last_pos, int j) {
-  const auto* rp = fixed(reinterpret_cast<const int32_t*>(a.routes)) + 6 * (int64_t)w.r;
-  w.n = visible(rp[2], rp[3], last_pos);
-  w.tb = rp[2];
-  w.base = rp[4];
-  w.tiles = (w.n + kKeyTile - 1) / kKeyTile;
-  w.j = j;
+// The tokens that a row tile sees: those up to its last row's position; with a window
+// those before low (where its first row's window begins) only if they are sinks.
+struct Sight {
+  int last_pos, low, sinks;
+};
+
+// The first token of the window of a row at first_pos + i.
+__device__ __forceinline__ int window_begin(const RowsArgs& a, int first_pos, int i) {
+  const int64_t x = (int64_t)first_pos + i - a.window + 1;
+  return (int)max((int64_t)INT32_MIN, min((int64_t)INT32_MAX, x));
+}
+
+// A route's tokens begin .. end - 1 in that sight: n, and its tiles [0, from) and
+// [to, tiles).
+template <bool WINDOW>
+__device__ __forceinline__ void route_sight(const Sight& s, int begin, int end, int& n, int& from,
+                                            int& to, int& tiles) {
+  n = visible(begin, end, s.last_pos);
+  tiles = (n + kKeyTile - 1) / kKeyTile;
+  from = to = 0;
+  if (WINDOW) {
+    const int64_t before = (int64_t)s.low - begin;  // tokens before the window
+    if (before >= n)
+      to = tiles;
+    else
+      to = before <= 0 ? 0 : (int)before / kKeyTile;
+    from = (visible(begin, end, min(s.last_pos, s.sinks - 1)) + kKeyTile - 1) / kKeyTile;
+    to = max(to, from);
+    if (to == tiles) to = tiles = from;
+  }
+}
+template <bool WINDOW>
+__device__ __forceinline__ int sight_tiles(const Sight& s, int begin, int end) {
+  int n, from, to, tiles;
+  route_sight<WINDOW>(s, begin, end, n, from, to, tiles);
+  return tiles - to + from;
+}
+
+// Enters the route begin .. end - 1 at the k-th of its visible tiles.
+template <bool WINDOW>
+__device__ __forceinline__ void walk_route(Walk& w, const Sight& s, int begin, int end, int base,
+                                           int k) {
+  route_sight<WINDOW>(s, begin, end, w.n, w.from, w.to, w.tiles);
+  w.tb = begin;
+  w.base = base;
+  w.j = WINDOW && k >= w.from ? k - w.from + w.to : k;
 }
 
 // Behind a route's last tile: the next route that has any.
-__device__ __forceinline__ void walk_on(const RowsArgs& a, Walk& w, int last_pos) {
+template <bool WINDOW>
+__device__ __forceinline__ void walk_on(const RowsArgs& a, Walk& w, const Sight& s) {
   while (w.j >= w.tiles && w.r < w.r_end) {
-    if (++w.r < w.r_end) walk_enter(a, w, last_pos, 0);
+    if (++w.r < w.r_end) {
+      const auto* rp = fixed(reinterpret_cast<const int32_t*>(a.routes)) + 6 * (int64_t)w.r;
+      if (WINDOW) {
+        walk_route<WINDOW>(w, s, rp[2], rp[3], rp[4], 0);
+      } else {
+        w.n = visible(rp[2], rp[3], s.last_pos);
+        w.tb = rp[2];
+        w.base = rp[4];
+        w.tiles = (w.n + kKeyTile - 1) / kKeyTile;
+        w.j = 0;
+      }
+    }
   }
   if (w.r < w.r_end) walk_ids(a, w);
 }
 
 // The visible tiles of a sequence's routes; -1 if one of them is bad.  The first
 // route of a sequence goes into its item.
-__device__ __forceinline__ int count_tiles(const RowsArgs& a, int b, int r0, int r1, int last_pos,
+template <bool WINDOW>
+__device__ __forceinline__ int count_tiles(const RowsArgs& a, int b, int r0, int r1, const Sight& s,
                                            int lane, RowsItem& it) {
   it.tok_begin = it.tok_end = it.page_base = 0;
   int64_t tiles = 0;
@@ -961,33 +967,35 @@ __device__ __forceinline__ int count_tiles(const RowsArgs& a, int b, int r0, int
     it.tok_end = row[3];
     it.page_base = row[4];
     if (r1 - r0 == 1)
-      return route_ok(a, b, row)
-                 ? (visible(row[2], row[3], last_pos) + kKeyTile - 1) / kKeyTile : -1;
+      return route_ok(a, b, row) ? sight_tiles<WINDOW>(s, row[2], row[3]) : -1;
   }
   for (int r = r0 + lane; r < r1; r += 64) {
     const int32_t* rp = reinterpret_cast<const int32_t*>(a.routes + r);
     bad |= !route_ok(a, b, rp);
-    tiles += (visible(rp[2], rp[3], last_pos) + kKeyTile - 1) / kKeyTile;
+    tiles += sight_tiles<WINDOW>(s, rp[2], rp[3]);
   }
   return __ballot(bad) ? -1 : uniform((int)min(wave_sum(tiles), (int64_t)1 << 30));
 }
 
 // Positions the walk at key tile k of the sequence; tiles of a route: its
 // visible tokens / 32, rounded up.  Sixty-four routes at a time.
-__device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int r1, int last_pos,
+template <bool WINDOW>
+__device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int r1, const Sight& s,
                                         int64_t k, int lane) {
   w.r = w.r_end = r1;
   w.j = w.tiles = 0;
+  w.from = w.to = 0;
   w.base = w.n = w.tb = w.pid[0] = w.pid[1] = 0;
   for (int r = r0; r < r1; r += 64) {
-    int n = 0, tb = 0, base = 0;
+    int n = 0, tb = 0, te = 0, base = 0;
     if (r + lane < r1) {
       const kf_route& row = a.routes[r + lane];
       tb = row.tok_begin;
+      te = row.tok_end;
       base = row.page_base;
-      n = visible(tb, row.tok_end, last_pos);
+      if (!WINDOW) n = visible(tb, te, s.last_pos);
     }
-    const int tiles = (n + kKeyTile - 1) / kKeyTile;
+    const int tiles = WINDOW ? sight_tiles<WINDOW>(s, tb, te) : (n + kKeyTile - 1) / kKeyTile;
     int64_t x = tiles;
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) {
@@ -998,11 +1006,18 @@ __device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int 
     if (found) {
       const int at = uniform(__builtin_ctzll(found));
       w.r = r + at;
-      w.n = __builtin_amdgcn_readlane(n, at);
-      w.tb = __builtin_amdgcn_readlane(tb, at);
-      w.base = __builtin_amdgcn_readlane(base, at);
-      w.tiles = __builtin_amdgcn_readlane(tiles, at);
-      w.j = uniform((int)(k - __shfl((long long)(x - tiles), at)));
+      if (WINDOW) {
+        const int j = uniform((int)(k - __shfl((long long)(x - tiles), at)));
+        walk_route<WINDOW>(w, s, __builtin_amdgcn_readlane(tb, at),
+                           __builtin_amdgcn_readlane(te, at), __builtin_amdgcn_readlane(base, at),
+                           j);
+      } else {
+        w.n = __builtin_amdgcn_readlane(n, at);
+        w.tb = __builtin_amdgcn_readlane(tb, at);
+        w.base = __builtin_amdgcn_readlane(base, at);
+        w.tiles = __builtin_amdgcn_readlane(tiles, at);
+        w.j = uniform((int)(k - __shfl((long long)(x - tiles), at)));
+      }
       walk_ids(a, w);
       return;
     }
@@ -1031,20 +1046,6 @@ __device__ __forceinline__ void to_lds(const char* g, char* l) {
       (const __attribute__((address_space(1))) uint32_t*)g,
       (__attribute__((address_space(3))) uint32_t*)(__attribute__((address_space(3))) void*)l, 16,
       0, ONCE ? 2 : 0);
-}
-
-// 16 E4M3 codes -> two times 8 bf16, exactly.
-__device__ __forceinline__ void widen(u32x4 codes, u32x4& lo, u32x4& hi) {
-  uint32_t o[8];
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    o[2 * w] = __builtin_bit_cast(
-        uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[w], 1.0f, false));
-    o[2 * w + 1] = __builtin_bit_cast(
-        uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[w], 1.0f, true));
-  }
-  lo = u32x4{o[0], o[1], o[2], o[3]};
-  hi = u32x4{o[4], o[5], o[6], o[7]};
 }
 
 // 4 bytes each of four lanes into LDS.
@@ -1236,7 +1237,7 @@ __device__ __forceinline__ void fill_nan(const RowsArgs& a, int row0, int64_t m0
 // the softmax.  fp8 trees have scalar registers spilled in the loop as well (some 140;
 // 120 scalar instructions a step).  bf16 trees of few rows wait for memory: 48 over 2K ..
 // 64K tokens, 4.1 GB, 678 us, 6.0 TB/s.
-template <bool FP8, bool TREE>
+template <bool FP8, bool TREE, bool WINDOW>
 struct Work {
   const RowsArgs& a;
   int tid, lane, wave, g;
@@ -1246,6 +1247,9 @@ struct Work {
   u32x4 q[8];
   // positions: the lane's row, the wave's and the workgroup's first, the workgroup's last
   int pos, pos_min, tile_min, last_pos;
+  // with a window, where it begins: of the lane's row, of the wave's and workgroup's
+  // last, of the workgroup's first
+  int low, low_max, tile_low, first_low;
   uint64_t draft;            // drafted rows that the lane's row sees
   Walk walk;
   int left;                  // tiles of this part still to come
@@ -1280,10 +1284,12 @@ struct Work {
         pg.at[i] = head_at + (uint64_t)(uint32_t)pid * page_bytes;
         pg.pid[i] = pid;
       }
-      if (__builtin_expect(++walk.j < walk.tiles, 1))
+      ++walk.j;
+      if (WINDOW && walk.j == walk.from) walk.j = walk.to;
+      if (__builtin_expect(walk.j < walk.tiles, 1))
         walk_ids(a, walk);
       else
-        walk_on(a, walk, last_pos);
+        walk_on<WINDOW>(a, walk, Sight{last_pos, first_low, a.sinks});
     } else if (TREE && drafts > 0) {
       t.pos0 = n_rows - drafts;
       t.left = drafts;
@@ -1291,6 +1297,12 @@ struct Work {
       drafts -= kKeyTile;
     }
     return t;
+  }
+
+  // Whether some token of the tile lies before a window that begins at `begin`, and is
+  // no sink.
+  __device__ __forceinline__ bool cut_before(const Tile& t, int begin) const {
+    return t.pos0 < begin && __builtin_elementwise_sub_sat(a.sinks, t.pos0) < kKeyTile;
   }
 
   __device__ __forceinline__ static bool paged(const Tile& t) {
@@ -1361,8 +1373,11 @@ struct Work {
                                        char* __restrict__ lv, f32x4 scales) {
     ++steps;
     bool odd = false;
-    if (__builtin_expect(
-            t.kind || __builtin_elementwise_sub_sat(tile_min, t.pos0) < kKeyTile - 1, 0)) {
+    // (what a window adds stands in statements of its own: as terms of these two
+    // conditions, false at compile time, it cost the tree kernels 217 scalar registers)
+    bool partly = t.kind || __builtin_elementwise_sub_sat(tile_min, t.pos0) < kKeyTile - 1;
+    if constexpr (WINDOW) partly |= cut_before(t, tile_low);
+    if (__builtin_expect(partly, 0)) {
       // some row of the workgroup does not see all of it
       if (cut_tile(t.left, tid, lv)) *odd_step = steps;
       lds_barrier();
@@ -1392,11 +1407,17 @@ struct Work {
     }
     const int half = lane >> 5;
     uint32_t sees = ~0u;
-    const bool mask = t.kind || __builtin_elementwise_sub_sat(pos_min, t.pos0) < kKeyTile - 1;
+    bool mask = t.kind || __builtin_elementwise_sub_sat(pos_min, t.pos0) < kKeyTile - 1;
+    if constexpr (WINDOW) mask |= cut_before(t, low_max);
     if (__builtin_expect(mask, 0)) {
       const int e = min(__builtin_elementwise_sub_sat(pos, t.pos0), t.left - 1);
       sees = e < 0 ? 0 : e >= 31 ? ~0u : (2u << e) - 1;
       if (TREE && (t.kind & kDraft)) sees = (uint32_t)(draft >> t.pos0);
+      if (WINDOW) {
+        auto below = [](int n) -> uint32_t { return n <= 0 ? 0 : n >= 32 ? ~0u : (1u << n) - 1; };
+        sees &= ~below(__builtin_elementwise_sub_sat(low, t.pos0)) |
+                below(__builtin_elementwise_sub_sat(a.sinks, t.pos0));
+      }
       const uint32_t mine = sees >> (8 * half);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -1539,7 +1560,7 @@ struct Work {
   }
 };
 
-template <bool FP8, bool TREE>
+template <bool FP8, bool TREE, bool WINDOW>
 __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   // K and V: four tiles each (bf16), or two tiles and a ring of four (fp8)
   constexpr int kTile = kKeyTile * kDim * 2, kRing = FP8 ? kKeyTile * kDim : 16;
@@ -1597,11 +1618,15 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     return TREE ? INT32_MAX
                 : __builtin_elementwise_add_sat(p0, (int)((uint32_t)min(pair, m1 - 1) / (uint32_t)G));
   };
-  const int last_pos = uniform(position(m1 - 1));
+  Sight sight{uniform(position(m1 - 1)), INT32_MIN, 0};
+  if (WINDOW) {
+    sight.low = uniform(window_begin(a, p0, (int)((uint32_t)m0 / (uint32_t)G)));
+    sight.sinks = a.sinks;
+  }
   const int route0 = it.route0, route1 = it.route1;
   if (a.parts > 0) {
     const int k = TREE && n_rows > KF_MAX_DRAFT
-                      ? -1 : count_tiles(a, b, route0, route1, last_pos, lane, it);
+                      ? -1 : count_tiles<WINDOW>(a, b, route0, route1, sight, lane, it);
     if (k < 0) {
       it.seq = -1 - b;
       if (tid == 0) atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
@@ -1627,7 +1652,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   const uint32_t mc = mine ? m : m1 - 1;
   const int row = mc / (uint32_t)G, h = g * G + mc % (uint32_t)G;
   const float c0 = a.scale_log2;
-  Work<FP8, TREE> w{a};
+  Work<FP8, TREE, WINDOW> w{a};
   w.tid = tid;
   w.lane = lane;
   w.wave = wave;
@@ -1641,7 +1666,8 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     w.q[ks] = ld16(a.q + (row0 + row) * a.q_stride + (size_t)h * kDim + 16 * ks + 8 * half);
   }
   w.pos = w.pos_min = w.tile_min = INT32_MAX;
-  w.last_pos = last_pos;
+  w.last_pos = sight.last_pos;
+  w.low = w.low_max = w.tile_low = w.first_low = sight.low;
   w.draft = 0;
   if constexpr (TREE) {
     w.draft = mine ? a.tree_mask[row0 + row] : 0;
@@ -1650,6 +1676,14 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     w.pos = position(m);
     w.pos_min = uniform(position(m0 + 32 * wave));
     w.tile_min = uniform(position(m0));
+    if (WINDOW) {
+      auto begins = [&](int pair) {
+        return window_begin(a, p0, (int)((uint32_t)min(pair, m1 - 1) / (uint32_t)G));
+      };
+      w.low = begins(m);
+      w.low_max = uniform(begins(m0 + 32 * wave + 31));
+      w.tile_low = uniform(begins(m1 - 1));
+    }
   }
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
@@ -1676,18 +1710,25 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   // A part that begins in its sequence's first route has that in its item (packed
   // prompts 183 -> 180 us, one short one 8.9 -> 8.0; fp8's kernel has no registers for
   // it, chunks 2704 -> 2779).
-  const int see = route0 < route1 ? visible(it.tok_begin, it.tok_end, last_pos) : 0;
-  if (!FP8 && it.key0 < (see + kKeyTile - 1) / kKeyTile) {
+  const int see = route0 < route1 ? visible(it.tok_begin, it.tok_end, sight.last_pos) : 0;
+  const int first_tiles = !WINDOW          ? (see + kKeyTile - 1) / kKeyTile
+                          : route0 < route1 ? sight_tiles<WINDOW>(sight, it.tok_begin, it.tok_end)
+                                            : 0;
+  if (!FP8 && it.key0 < first_tiles) {
     w.walk.r = route0;
     w.walk.r_end = route1;
-    w.walk.n = see;
-    w.walk.tb = it.tok_begin;
-    w.walk.base = it.page_base;
-    w.walk.tiles = (see + kKeyTile - 1) / kKeyTile;
-    w.walk.j = it.key0;
+    if (WINDOW) {
+      walk_route<WINDOW>(w.walk, sight, it.tok_begin, it.tok_end, it.page_base, it.key0);
+    } else {
+      w.walk.n = see;
+      w.walk.tb = it.tok_begin;
+      w.walk.base = it.page_base;
+      w.walk.tiles = (see + kKeyTile - 1) / kKeyTile;
+      w.walk.j = it.key0;
+    }
     walk_ids(a, w.walk);
   } else {
-    walk_to(a, w.walk, route0, route1, last_pos, it.key0, lane);
+    walk_to<WINDOW>(a, w.walk, route0, route1, sight, it.key0, lane);
   }
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) {
@@ -1906,26 +1947,20 @@ hipError_t launch_append_rows(const AppendRowsArgs& a, bool fp8, hipStream_t str
   return hipGetLastError();
 }
 
-hipError_t launch_rows_attn(const RowsArgs& a, bool fp8, bool tree, hipStream_t stream) {
+template <bool TREE, bool WINDOW>
+hipError_t launch_rows(const RowsArgs& a, bool fp8, hipStream_t stream) {
   hipError_t st;
   if (a.parts == 0) {
-    if (tree)
-      rows_plan_kernel<true><<<1, 1024, 0, stream>>>(a);
-    else
-      rows_plan_kernel<false><<<1, 1024, 0, stream>>>(a);
+    rows_plan_kernel<TREE, WINDOW><<<1, 1024, 0, stream>>>(a);
     if ((st = hipGetLastError()) != hipSuccess) return st;
   }
   // (a workgroup without an item still takes its place on a compute unit)
   const int items = a.parts > 0 ? a.max_tiles * a.parts : a.max_tiles + (a.may_split ? a.max_recs : 0);
   const uint32_t grid = (uint32_t)items * a.num_kv_heads;
-  if (fp8 && tree)
-    rows_kernel<true, true><<<grid, 256, 0, stream>>>(a);
-  else if (fp8)
-    rows_kernel<true, false><<<grid, 256, 0, stream>>>(a);
-  else if (tree)
-    rows_kernel<false, true><<<grid, 256, 0, stream>>>(a);
+  if (fp8)
+    rows_kernel<true, TREE, WINDOW><<<grid, 256, 0, stream>>>(a);
   else
-    rows_kernel<false, false><<<grid, 256, 0, stream>>>(a);
+    rows_kernel<false, TREE, WINDOW><<<grid, 256, 0, stream>>>(a);
   st = hipGetLastError();
   if (st != hipSuccess || a.parts == 1 || (a.parts == 0 && !a.may_split)) return st;
   // a wave per (row, head) and turn; most splits at most
@@ -1934,6 +1969,12 @@ hipError_t launch_rows_attn(const RowsArgs& a, bool fp8, bool tree, hipStream_t 
   const uint32_t wgs = (uint32_t)min((waves + 3) / 4, (int64_t)kCombineWgsPerSlot * a.slots);
   rows_combine_kernel<<<wgs, 256, 0, stream>>>(a);
   return hipGetLastError();
+}
+
+hipError_t launch_rows_attn(const RowsArgs& a, bool fp8, bool tree, hipStream_t stream) {
+  if (tree) return launch_rows<true, false>(a, fp8, stream);
+  return a.window < 0 ? launch_rows<false, false>(a, fp8, stream)
+                      : launch_rows<false, true>(a, fp8, stream);
 }
 
 }  // namespace kf

@@ -60,7 +60,7 @@ RowsLayout rows_layout(int32_t num_rows, int32_t num_seqs, int32_t num_kv_heads,
 // over 300 .. 1500 tokens 69 and 49, over 800 .. 2500 95 and 76 (up to kMostSteps).
 int32_t unplanned_parts(const RowsLayout& l, int32_t num_seqs, int32_t num_kv_heads,
                         int32_t num_routes, int32_t num_page_ids, int32_t max_pages_per_route,
-                        int64_t slots) {
+                        int64_t most_keys, int64_t slots) {
   const int64_t items = (int64_t)l.max_tiles * num_kv_heads;
   if (num_seqs > 64 || num_seqs < 1 || items > slots) return 0;
   // mean key tiles of a sequence at most, as the page table tells it: pages that are
@@ -70,7 +70,8 @@ int32_t unplanned_parts(const RowsLayout& l, int32_t num_seqs, int32_t num_kv_he
   // plan because of it pay for it: 48 trees of 8 over 300 tokens 20 us with a table of
   // their own length, 51 with 8K reserved each and as much in max_pages_per_route.
   const int64_t pages = std::min((int64_t)num_page_ids, (int64_t)num_routes * max_pages_per_route);
-  const int64_t keys = (pages * KF_PAGE_SIZE / kKeyTile + num_routes) / num_seqs + 1;
+  const int64_t keys =
+      std::min((pages * KF_PAGE_SIZE / kKeyTile + num_routes) / num_seqs + 1, most_keys);
   int64_t parts = std::min(slots / items, (keys + kMinPart - 1) / kMinPart);
   // steps go down with the parts, the combine's turns up: 8 drafted tokens over 8K
   // tokens, 8 KV heads, 24.7 us in parts of kMinPart, 21.9 in 2 sqrt(keys) parts,
@@ -78,8 +79,9 @@ int32_t unplanned_parts(const RowsLayout& l, int32_t num_seqs, int32_t num_kv_he
   parts = std::min(parts, (int64_t)(2.0 * sqrt((double)keys)));
   parts = std::max<int64_t>(1, std::min<int64_t>(parts, l.max_recs / l.max_tiles));
   // the longest sequence's at most, where every sequence has a route
-  const int64_t most = ((int64_t)max_pages_per_route * KF_PAGE_SIZE / kKeyTile + 1) *
-                       std::max(1, num_routes - num_seqs + 1);
+  const int64_t most = std::min(((int64_t)max_pages_per_route * KF_PAGE_SIZE / kKeyTile + 1) *
+                                    std::max(1, num_routes - num_seqs + 1),
+                                most_keys);
   return keys <= kMeanSteps * parts || most <= kMostSteps * parts ? (int32_t)parts : 0;
 }
 
@@ -87,14 +89,15 @@ int32_t unplanned_parts(const RowsLayout& l, int32_t num_seqs, int32_t num_kv_he
 
 namespace {
 
-// Host checks that the two attention operators share; fills the kernel
-// arguments (a.num_rows == 0: nothing to launch).
+// Host checks that the attention operators share; fills the kernel arguments
+// (a.num_rows == 0: nothing to launch).  window < 0: none.
 int prepare_rows(const kf_shape* shape, const void* q, int32_t num_rows, int64_t q_stride,
                  const int32_t* seq_row_begin, const void* k_pool, const void* v_pool,
                  const float* k_scale, const float* v_scale, const kf_route* routes,
                  int32_t num_routes, int32_t max_pages_per_route, const int32_t* page_ids,
                  const int32_t* seq_route_begin, void* out, float* lse, void* workspace,
-                 size_t workspace_bytes, int32_t* err_flags, kf::RowsArgs& a) {
+                 size_t workspace_bytes, int32_t* err_flags, kf::RowsArgs& a, int32_t sinks = 0,
+                 int32_t window = -1) {
   const int st = kf::check_shape(shape);
   if (st != KF_OK) return st;
   if (num_rows < 0 || num_routes < 0 || max_pages_per_route < 0) return KF_ERR_INVALID_ARG;
@@ -153,8 +156,14 @@ int prepare_rows(const kf_shape* shape, const void* q, int32_t num_rows, int64_t
   a.max_recs = l.max_recs;
   a.rec_rows = l.rec_rows;
   a.slots = (int32_t)(2 * cus);
+  a.sinks = sinks;
+  a.window = window;
+  // the sinks, a window and the row tile's own rows, part-filled tiles at their ends
+  const int64_t most_keys =
+      window < 0 ? INT64_MAX
+                 : ((int64_t)sinks + window + kf::kRowTile / group) / kf::kKeyTile + 4;
   a.parts = kf::unplanned_parts(l, shape->num_seqs, shape->num_kv_heads, num_routes,
-                                shape->num_page_ids, max_pages_per_route, a.slots);
+                                shape->num_page_ids, max_pages_per_route, most_keys, a.slots);
   // the row tiles that num_rows comes to if every row belongs to a sequence
   const int64_t tiles = ((int64_t)num_rows * group + kf::kRowTile - 1) / kf::kRowTile;
   a.may_split = l.max_recs > 1 && tiles * shape->num_kv_heads < kf::kSplitSlots * (int64_t)a.slots;
@@ -244,6 +253,28 @@ int kf_prompt_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64
   const int st = prepare_rows(shape, q, num_rows, q_stride, seq_row_begin, k_pool, v_pool, k_scale,
                               v_scale, routes, num_routes, max_pages_per_route, page_ids,
                               seq_route_begin, out, lse, workspace, workspace_bytes, err_flags, a);
+  if (st != KF_OK || num_rows == 0) return st;
+  a.first_pos = first_pos;
+  return kf::launch_rows_attn(a, fp8_pool(shape), false, as_stream(stream)) == hipSuccess
+             ? KF_OK
+             : KF_ERR_HIP;
+}
+
+int kf_window_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64_t q_stride,
+                   const int32_t* seq_row_begin, const int32_t* first_pos, int32_t sinks,
+                   int32_t window, const void* k_pool, const void* v_pool, const float* k_scale,
+                   const float* v_scale, const kf_route* routes, int32_t num_routes,
+                   int32_t max_pages_per_route, const int32_t* page_ids,
+                   const int32_t* seq_route_begin, void* out, float* lse, void* workspace,
+                   size_t workspace_bytes, int32_t* err_flags, void* stream) {
+  kf::RowsArgs a{};
+  if (sinks < 0 || window < 0) return KF_ERR_INVALID_ARG;
+  if (num_rows > 0 && ((shape && shape->num_seqs > 0 && !first_pos) || !aligned(first_pos, 4)))
+    return KF_ERR_INVALID_ARG;
+  const int st = prepare_rows(shape, q, num_rows, q_stride, seq_row_begin, k_pool, v_pool, k_scale,
+                              v_scale, routes, num_routes, max_pages_per_route, page_ids,
+                              seq_route_begin, out, lse, workspace, workspace_bytes, err_flags, a,
+                              sinks, window);
   if (st != KF_OK || num_rows == 0) return st;
   a.first_pos = first_pos;
   return kf::launch_rows_attn(a, fp8_pool(shape), false, as_stream(stream)) == hipSuccess

@@ -42,7 +42,8 @@ EXPORTS = ("kf_kv_append", "kf_partial_attn_workspace_bytes", "kf_partial_attn_p
            "kf_partial_attn_spans", "kf_partial_attn", "kf_partial_attn_subset",
            "kf_merge_partials", "kf_decode_step", "kf_decode_step_no_alloc",
            "kf_kv_append_rows_workspace_bytes", "kf_kv_append_rows",
-           "kf_rows_attn_workspace_bytes", "kf_prompt_attn", "kf_tree_attn", "kf_debug_gather",
+           "kf_rows_attn_workspace_bytes", "kf_prompt_attn", "kf_window_attn", "kf_tree_attn",
+           "kf_attn_weights", "kf_kv_evict_workspace_bytes", "kf_kv_evict", "kf_debug_gather",
            "kf_status_str", "kf_version")
 
 
@@ -109,9 +110,20 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.kf_prompt_attn.argtypes = [sp, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp,
                                    vp, vp, sz, vp, vp]
     lib.kf_prompt_attn.restype = ctypes.c_int
+    lib.kf_window_attn.argtypes = [sp, vp, i32, i64, vp, vp, i32, i32, vp, vp, vp, vp, vp, i32, i32,
+                                   vp, vp, vp, vp, vp, sz, vp, vp]
+    lib.kf_window_attn.restype = ctypes.c_int
     lib.kf_tree_attn.argtypes = [sp, vp, i32, i64, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, i32, i32,
                                  vp, vp, vp, vp, vp, sz, vp, vp]
     lib.kf_tree_attn.restype = ctypes.c_int
+    lib.kf_attn_weights.argtypes = [sp, vp, i32, i64, vp, vp, vp, vp, vp, vp, i32, i32, vp,
+                                    ctypes.c_float, vp, vp, vp]
+    lib.kf_attn_weights.restype = ctypes.c_int
+    lib.kf_kv_evict_workspace_bytes.argtypes = [sp, i32]
+    lib.kf_kv_evict_workspace_bytes.restype = sz
+    lib.kf_kv_evict.argtypes = [sp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, i32, i32, i32,
+                                vp, sz, vp, vp]
+    lib.kf_kv_evict.restype = ctypes.c_int
     lib.kf_debug_gather.argtypes = [sp, vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, vp, vp]
     lib.kf_debug_gather.restype = ctypes.c_int
     lib.kf_status_str.argtypes = [ctypes.c_int]
@@ -566,7 +578,7 @@ def rows_attn_workspace_bytes(shape: Shape, num_rows: int) -> int:
 
 
 def alloc_rows_workspace(shape: Shape, num_rows: int, device="cuda"):
-    """Workspace of prompt_attn and tree_attn for num_rows rows."""
+    """Workspace of prompt_attn, window_attn and tree_attn for num_rows rows."""
     n = rows_attn_workspace_bytes(shape, num_rows)
     if n == 0:
         raise KFError("invalid workspace request")
@@ -576,8 +588,8 @@ def alloc_rows_workspace(shape: Shape, num_rows: int, device="cuda"):
 def _bind_rows(fn, what: str, shape: Shape, q, mid, mid_keep, k_pool, v_pool, routes,
                max_pages_per_route, page_ids, seq_route_begin, seq_row_begin, out, lse, workspace,
                err_flags, k_scale, v_scale) -> BoundCall:
-    """prompt_attn and tree_attn: the arguments that they share.  mid: the C
-    arguments around seq_row_begin, which is given as a marker."""
+    """prompt_attn, window_attn and tree_attn: the arguments that they share.  mid:
+    the C arguments around seq_row_begin, which is given as a marker."""
     B, Hq = shape.num_seqs, shape.num_q_heads
     stride = _rows(q, "q", Hq)
     N = q.shape[0]
@@ -633,6 +645,32 @@ def prompt_attn(shape: Shape, q, first_pos, k_pool, v_pool, routes, max_pages_pe
                      v_scale)(stream)
 
 
+def bind_window_attn(shape: Shape, q, first_pos, sinks, window, k_pool, v_pool, routes,
+                     max_pages_per_route, page_ids, seq_route_begin, seq_row_begin, out, lse,
+                     workspace, err_flags, k_scale=None, v_scale=None) -> BoundCall:
+    """kf_window_attn bound to its buffers; call it as (stream).  A row at position p
+    sees the tokens t <= p with t < sinks or t > p - window; the rest as for
+    bind_prompt_attn (a decode step: one row per sequence)."""
+    _dev(first_pos, "first_pos", torch.int32)
+    _need(first_pos.numel() >= shape.num_seqs, "first_pos must be int32 [num_seqs]")
+    sinks, window = int(sinks), int(window)
+    _need(0 <= sinks < 2 ** 31 and 0 <= window < 2 ** 31, "sinks and window must be int32 >= 0")
+    return _bind_rows(load().kf_window_attn, "kf_window_attn", shape, q,
+                      lambda begin: (begin, _ptr(first_pos), sinks, window),
+                      ((first_pos, "first_pos"),), k_pool, v_pool, routes, max_pages_per_route,
+                      page_ids, seq_route_begin, seq_row_begin, out, lse, workspace, err_flags,
+                      k_scale, v_scale)
+
+
+def window_attn(shape: Shape, q, first_pos, sinks, window, k_pool, v_pool, routes,
+                max_pages_per_route, page_ids, seq_route_begin, seq_row_begin, out, lse, workspace,
+                err_flags, k_scale=None, v_scale=None, stream=None):
+    """kf_window_attn: causal attention with a sliding window and attention sinks."""
+    bind_window_attn(shape, q, first_pos, sinks, window, k_pool, v_pool, routes,
+                     max_pages_per_route, page_ids, seq_route_begin, seq_row_begin, out, lse,
+                     workspace, err_flags, k_scale, v_scale)(stream)
+
+
 def bind_tree_attn(shape: Shape, q, k_draft, v_draft, tree_mask, k_pool, v_pool, routes,
                    max_pages_per_route, page_ids, seq_route_begin, seq_row_begin, out, lse,
                    workspace, err_flags, k_scale=None, v_scale=None) -> BoundCall:
@@ -660,6 +698,117 @@ def tree_attn(shape: Shape, q, k_draft, v_draft, tree_mask, k_pool, v_pool, rout
     bind_tree_attn(shape, q, k_draft, v_draft, tree_mask, k_pool, v_pool, routes,
                    max_pages_per_route, page_ids, seq_route_begin, seq_row_begin, out, lse,
                    workspace, err_flags, k_scale, v_scale)(stream)
+
+
+# ---------------------------------------------------- operators of a budget
+def _check_weights(shape: Shape, weights):
+    _dev(weights, "weights", torch.float32)
+    _need(weights.numel() == shape.num_pages * shape.num_kv_heads * PAGE_SIZE,
+          "weights must be float32 [num_pages, num_kv_heads, 16]")
+
+
+def alloc_weights(shape: Shape, device="cuda") -> torch.Tensor:
+    """Token weights of a pool (attn_weights, kv_evict), all zero."""
+    return torch.zeros((shape.num_pages, shape.num_kv_heads, PAGE_SIZE), device=device)
+
+
+def bind_attn_weights(shape: Shape, q, lse, first_pos, k_pool, routes, max_pages_per_route,
+                      page_ids, seq_row_begin, decay, weights, err_flags,
+                      k_scale=None) -> BoundCall:
+    """kf_attn_weights bound to its buffers; call it as (stream).  q bf16 [N, Hq, 128],
+    lse float32 [N, Hq]: packed rows and what their attention returned; first_pos
+    int32 [B], seq_row_begin int32 [B + 1]; weights float32 [P, Hkv, 16] (updated)."""
+    H = shape.num_kv_heads
+    stride = _rows(q, "q", shape.num_q_heads)
+    N = q.shape[0]
+    for t, n in ((lse, "lse"), (k_pool, "k_pool"), (routes, "routes"), (page_ids, "page_ids"),
+                 (err_flags, "err_flags")):
+        _dev(t, n)
+    _dev(first_pos, "first_pos", torch.int32)
+    _need(first_pos.numel() >= shape.num_seqs, "first_pos must be int32 [num_seqs]")
+    _csr(seq_row_begin, "seq_row_begin", shape.num_seqs)
+    _need(tuple(lse.shape) == (N, shape.num_q_heads) and lse.dtype == torch.float32,
+          "lse must be float32 [num_rows, Hq]")
+    _need(err_flags.dtype == torch.int32 and err_flags.numel() >= 1, "err_flags must be int32 [1]")
+    _check_weights(shape, weights)
+    _check_tables(shape, k_pool, k_pool, routes, page_ids)
+    if shape.kv_dtype == KV_FP8_E4M3:
+        _check_scales(shape, k_scale, k_scale)
+    _same_device(k_pool, ((q, "q"), (lse, "lse"), (first_pos, "first_pos"), (routes, "routes"),
+                          (page_ids, "page_ids"), (seq_row_begin, "seq_row_begin"),
+                          (weights, "weights"), (err_flags, "err_flags"), (k_scale, "k_scale")))
+    sh = _copy_shape(shape)
+    args = (ctypes.byref(sh), _ptr(q), N, stride, _ptr(lse), _ptr(seq_row_begin), _ptr(first_pos),
+            _ptr(k_pool), _ptr(k_scale), _ptr(routes), routes.shape[0], int(max_pages_per_route),
+            _ptr(page_ids), float(decay), _ptr(weights), _ptr(err_flags))
+    keep = (sh, q, lse, seq_row_begin, first_pos, k_pool, k_scale, routes, page_ids, weights,
+            err_flags)
+    return BoundCall(load().kf_attn_weights, "kf_attn_weights", args, keep, k_pool.device.index)
+
+
+def attn_weights(shape: Shape, q, lse, first_pos, k_pool, routes, max_pages_per_route, page_ids,
+                 seq_row_begin, decay, weights, err_flags, k_scale=None, stream=None):
+    """kf_attn_weights: the attention weight of every token, accumulated."""
+    bind_attn_weights(shape, q, lse, first_pos, k_pool, routes, max_pages_per_route, page_ids,
+                      seq_row_begin, decay, weights, err_flags, k_scale)(stream)
+
+
+def kv_evict_workspace_bytes(shape: Shape, max_keep: int) -> int:
+    return int(load().kf_kv_evict_workspace_bytes(ctypes.byref(shape), int(max_keep)))
+
+
+def bind_kv_evict(shape: Shape, k_pool, v_pool, weights, routes, max_pages_per_route, page_ids,
+                  seq_route_begin, into, keep, max_keep, keep_first, keep_last, err_flags,
+                  k_scale=None, v_scale=None, workspace=None) -> BoundCall:
+    """kf_kv_evict bound to its buffers; call it as (stream).  into int32 [B]: the
+    sequence's empty route that takes what stays (-1: leave it alone); keep int32 [B],
+    at most max_keep: tokens that stay, the first keep_first and the last keep_last
+    among them; pools, scales, weights float32 [P, Hkv, 16] and routes are updated.
+    workspace=None allocates what the call needs (4 bytes a kept token and KV head)."""
+    B = shape.num_seqs
+    for t, n in ((k_pool, "k_pool"), (v_pool, "v_pool"), (routes, "routes"),
+                 (page_ids, "page_ids"), (err_flags, "err_flags")):
+        _dev(t, n)
+    _csr(seq_route_begin, "seq_route_begin", B)
+    for t, n in ((into, "into"), (keep, "keep")):
+        _dev(t, n, torch.int32)
+        _need(t.numel() >= B, f"{n} must be int32 [num_seqs]")
+    _need(err_flags.dtype == torch.int32 and err_flags.numel() >= 1, "err_flags must be int32 [1]")
+    _check_weights(shape, weights)
+    _check_tables(shape, k_pool, v_pool, routes, page_ids)
+    _check_scales(shape, k_scale, v_scale)
+    max_keep, keep_first, keep_last = int(max_keep), int(keep_first), int(keep_last)
+    _need(all(0 <= x < 2 ** 31 for x in (max_keep, keep_first, keep_last)),
+          "max_keep, keep_first and keep_last must be int32 >= 0")
+    if workspace is None:
+        n = kv_evict_workspace_bytes(shape, max_keep)
+        if n == 0:
+            raise KFError("invalid workspace request")
+        workspace = torch.empty(n, dtype=torch.uint8, device=k_pool.device)
+    _dev(workspace, "workspace")
+    _same_device(k_pool, ((v_pool, "v_pool"), (weights, "weights"), (routes, "routes"),
+                          (page_ids, "page_ids"), (seq_route_begin, "seq_route_begin"),
+                          (into, "into"), (keep, "keep"), (err_flags, "err_flags"),
+                          (k_scale, "k_scale"), (v_scale, "v_scale"), (workspace, "workspace")))
+    sh = _copy_shape(shape)
+    args = (ctypes.byref(sh), _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale),
+            _ptr(weights), _ptr(routes), routes.shape[0], int(max_pages_per_route), _ptr(page_ids),
+            _ptr(seq_route_begin), _ptr(into), _ptr(keep), max_keep, keep_first, keep_last,
+            _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(err_flags))
+    keep_alive = (sh, k_pool, v_pool, k_scale, v_scale, weights, routes, page_ids,
+                  seq_route_begin, into, keep, workspace, err_flags)
+    return BoundCall(load().kf_kv_evict, "kf_kv_evict", args, keep_alive, k_pool.device.index)
+
+
+def kv_evict(shape: Shape, k_pool, v_pool, weights, routes, max_pages_per_route, page_ids,
+             seq_route_begin, into, keep, max_keep, keep_first, keep_last, err_flags, k_scale=None,
+             v_scale=None, workspace=None, stream=None):
+    """kf_kv_evict.  On another stream than the current one give a workspace of your
+    own."""
+    _need(workspace is not None or stream is None, "a workspace is needed with a stream")
+    bind_kv_evict(shape, k_pool, v_pool, weights, routes, max_pages_per_route, page_ids,
+                  seq_route_begin, into, keep, max_keep, keep_first, keep_last, err_flags, k_scale,
+                  v_scale, workspace)(stream)
 
 
 def debug_gather(shape: Shape, k_pool, v_pool, routes, route, max_pages_per_route, page_ids,
