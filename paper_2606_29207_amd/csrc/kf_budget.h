@@ -37,6 +37,11 @@ void plan_attn_weights(AttnWeightsArgs& a, int64_t slots);
 hipError_t launch_attn_weights(const AttnWeightsArgs& a, bool fp8, hipStream_t stream);
 
 // -------------------------------------------------------------------- evict
+constexpr int kPartTokens = 8192;  // of a part of a sequence whose tokens are told apart by several
+                                   // workgroups, and the most parts
+constexpr int kMaxParts = 32;
+constexpr size_t kMostParts = 4096;  // of a launch: 100 MB of bins
+
 struct EvictArgs {
   void* k_pool;
   void* v_pool;
@@ -56,7 +61,19 @@ struct EvictArgs {
   int32_t* plan;  // [num_seqs][2]: tokens kept (-1: the sequence is left alone), index of the
                   // first page id that they go to
   int32_t* list;  // [num_seqs][Hkv][max_keep]: page * kPage + slot of each, in order
+  // several workgroups for a sequence and KV head
+  int32_t parts;   // 1: one does
+  uint32_t* rows;  // [num_seqs][Hkv][parts][3 passes][2048 bins]
+  int32_t* state;  // [num_seqs][Hkv][parts][4]: the threshold's bits, how many equal ones are
+                   // wanted, larger keys of the part, a bad page among its own
 };
+
+// The workspace of an eviction.
+struct EvictLayout {
+  size_t list_off, state_off, rows_off, total;
+  int32_t parts;
+};
+EvictLayout evict_layout(const kf_shape& s, int32_t max_keep);
 
 hipError_t launch_evict(const EvictArgs& a, bool fp8, hipStream_t stream);
 

@@ -1,6 +1,7 @@
 // gfx950 kernels of the operators that keep a cache within a budget:
 //   attn_weights_kernel -- the attention weight that every token receives
-//   evict_select_kernel -- which tokens of a sequence and KV head stay
+//   evict_select_kernel -- which tokens of a sequence and KV head stay, by one workgroup
+//   evict_count_kernel, evict_list_kernel -- the same by several, a launch for each pass
 //   evict_move_kernel   -- those tokens into the pages of another route
 #include "kf_budget.h"
 #include "kf_device.h"
@@ -376,8 +377,9 @@ __global__ __launch_bounds__(256, 2) void attn_weights_kernel(AttnWeightsArgs a)
 }
 
 // -------------------------------------------------------------------- evict
-constexpr int kKeysInLds = 34 * 1024;   // tokens of a sequence whose keys stay in LDS
-constexpr int kEvictRoutes = 1024;      // routes of a sequence at most
+constexpr int kKeysInLds = 34 * 1024;  // tokens of a sequence whose keys stay in LDS
+constexpr int kEvictRoutes = 1024;     // routes of a sequence at most
+constexpr int kBins = 2048;            // of a pass of 11 bits
 
 // Orders as the weights do; NaN before all others, zeros equal.
 __device__ __forceinline__ uint32_t order_key(float w) {
@@ -386,231 +388,487 @@ __device__ __forceinline__ uint32_t order_key(float w) {
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// The tokens of a sequence and KV head that stay: of its L tokens, in the order of its
-// routes, the first and the last ones, and of the others those of the largest keys, the
-// earlier of equal ones.  A threshold by radix, 11, 11 and 10 bits a pass over the keys.
-// Each wave has a stretch of the tokens of its own, so that a place's rank is its
-// wave's first rank and a count of ballots.
-__global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
-  __shared__ uint32_t keys[kKeysInLds];
-  __shared__ uint32_t hist[2048];
-  __shared__ int pre[kEvictRoutes + 1], pbase[kEvictRoutes];
-  __shared__ int s_scan[2][16], s_bin, s_want;
-  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
-  const int g = blockIdx.x, b = blockIdx.y, H = a.num_kv_heads;
-  int32_t* plan = a.plan + 2 * b;
-  const int into = a.into[b];
-  if (into == -1) {
-    if (g == 0 && tid == 0) plan[0] = -1;
-    return;
+// The bits of a key that a pass counts: 11, 11 and 10 from the top.
+__device__ __forceinline__ int pass_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ __forceinline__ int pass_bins(int pass) { return pass == 2 ? kBins / 2 : kBins; }
+// Whether a key has the threshold's bits above those.
+__device__ __forceinline__ bool pass_takes(int pass, uint32_t key, uint32_t top) {
+  return pass == 0 || ((key ^ top) >> (pass == 1 ? 21 : 10)) == 0;
+}
+
+// Sum over the waves before this one of x[0 .. 15], and over all.
+template <class T>
+__device__ __forceinline__ T waves_before(const T* x, int w, T& all) {
+  T before = 0;
+  all = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    if (i < w) before += x[i];
+    all += x[i];
   }
-  const int r0 = a.seq_route_begin[b], r1 = a.seq_route_begin[b + 1], keep = a.keep[b];
-  auto fail = [&](int flag) {
-    if (tid == 0) {
-      if (g == 0) {
-        plan[0] = -1;
-        atomicOr(a.err_flags, flag);
-      }
-    }
-  };
+  return before;
+}
+template <class T>
+__device__ __forceinline__ T wave_scan(T x, int lane) {  // inclusive
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const T y = (T)__shfl_up((long long)x, m);
+    if (lane >= m) x += y;
+  }
+  return x;
+}
+template <>
+__device__ __forceinline__ int wave_scan(int x, int lane) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int y = __shfl_up(x, m);
+    if (lane >= m) x += y;
+  }
+  return x;
+}
+
+// A sequence's tokens, route after route, and what stays of them.
+struct EvictSeq {
+  int status;      // 0, -1: left alone, or the error's flag
+  int routes;      // its routes
+  int L, K;        // its tokens, and those that stay
+  int c0, c1;      // the places that compete; those before and behind stay
+  int base;        // index of the first page id that they go to
+};
+struct EvictShared {
+  int pre[kEvictRoutes + 1], base[kEvictRoutes];  // of its routes: first place, first page id's
+                                                  // index
+  int64_t sum[16];
+  int scan[2][16];
+  int bin, want;
+};
+
+// Checked by every workgroup (1024 threads) for itself, but for the page ids.
+__device__ __forceinline__ EvictSeq evict_sequence(const EvictArgs& a, int b, EvictShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
+  EvictSeq s{};
+  const int into = a.into[b], keep = a.keep[b];
+  const int r0 = a.seq_route_begin[b], r1 = a.seq_route_begin[b + 1];
+  s.status = -1;
+  if (into == -1) return s;
+  s.status = KF_EFLAG_BAD_ROUTE;
   if (r0 < 0 || r1 < r0 || r1 > a.num_routes || r1 - r0 > kEvictRoutes || into < r0 || into >= r1 ||
       keep < 0 || keep > a.max_keep)
-    return fail(KF_EFLAG_BAD_ROUTE);
-  // the routes' tokens, and where each one's begin among the sequence's
-  const int R = r1 - r0;
+    return s;
+  s.routes = r1 - r0;
+  const kf_route to = a.routes[into];
   int n = 0;
   bool bad = false;
-  if (tid < R) {
+  if (tid < s.routes) {
     const kf_route row = a.routes[r0 + tid];
     bad = row.seq != b || !route_row_ok(row.tok_begin, row.tok_end, row.page_base, row.page_cap,
                                         a.max_pages_per_route, a.num_page_ids);
     n = bad ? 0 : row.tok_end - row.tok_begin;
-    if (r0 + tid == into) bad = bad || n != 0;
-    pbase[tid] = row.page_base;
+    bad = bad || (r0 + tid == into && n != 0);
+    sh.base[tid] = row.page_base;
   }
-  int64_t x = n;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int64_t y = __shfl_up((long long)x, m);
-    if (lane >= m) x += y;
-  }
-  // (sums beyond 32 bits are refused: each wave's is below 2^37)
-  __shared__ int64_t s_sum[16];
-  if (lane == 63) s_sum[w] = x;
-  if (__syncthreads_or(bad)) return fail(KF_EFLAG_BAD_ROUTE);
-  int64_t before = 0, all = 0;
-  for (int i = 0; i < 16; ++i) {
-    if (i < w) before += s_sum[i];
-    all += s_sum[i];
-  }
-  if (all > INT32_MAX - 1024) return fail(KF_EFLAG_BAD_ROUTE);
-  if (tid < R) pre[tid] = (int)(before + x) - n;
-  if (tid == 0) pre[R] = (int)all;
+  // (64 bits: a route has up to 2^31 - 1 tokens)
+  const int64_t x = wave_scan((int64_t)n, lane);
+  if (lane == 63) sh.sum[w] = x;
+  if (__syncthreads_or(bad)) return s;
+  int64_t all;
+  const int64_t before = waves_before(sh.sum, w, all);
+  if (all > INT32_MAX - 1024) return s;
+  if (tid < s.routes) sh.pre[tid] = (int)(before + x) - n;
+  if (tid == 0) sh.pre[s.routes] = (int)all;
+  s.L = (int)all;
+  s.K = min(s.L, keep);
+  s.base = to.page_base;
+  const int64_t pages = ((int64_t)s.K + kPage - 1) / kPage;
+  if ((int64_t)to.tok_begin + s.K > INT32_MAX || to.page_base + pages > a.num_page_ids) return s;
+  s.status = pages > to.page_cap ? KF_EFLAG_TAIL_FULL : 0;
+  const int first = min(s.K, a.keep_first), last = min(s.K - first, a.keep_last);
+  s.c0 = first;
+  s.c1 = s.L - last;
   __syncthreads();
-  const int L = (int)all, K = min(L, keep);
-  const int first = min(K, a.keep_first), last = min(K - first, a.keep_last);
-  // where they go
-  const kf_route to = a.routes[into];
-  const int64_t pages = ((int64_t)K + kPage - 1) / kPage;
-  if (pages > to.page_cap) return fail(KF_EFLAG_TAIL_FULL);
-  if ((int64_t)to.tok_begin + K > INT32_MAX || to.page_base + pages > a.num_page_ids)
-    return fail(KF_EFLAG_BAD_ROUTE);
-  for (int64_t p = tid; p < pages; p += 1024)
-    bad |= (uint32_t)a.page_ids[to.page_base + p] >= (uint32_t)a.num_pages;
+  return s;
+}
 
-  // this wave's stretch, and a walk over the places lo .. hi - 1 of it, eight at a time a
-  // lane: f(place, token, its weight) with the token's page * 16 + slot
-  const int per = ((L + 1023) / 1024) * 64, lo = min(L, w * per), hi = min(L, lo + per);
-  auto walk = [&](bool want_weights, auto f) __attribute__((always_inline)) {
-    int r = 0;
-    {  // the route of place lo + lane
-      const int e = min(lo + lane, L - 1);
-      int top = R;
-      while (top - r > 1) {
-        const int mid = (r + top) >> 1;
-        (pre[mid] <= e ? r : top) = mid;
+// Whether an id of the pages that they go to is bad (this thread's share).
+__device__ __forceinline__ bool evict_bad_target(const EvictArgs& a, const EvictSeq& s) {
+  bool bad = false;
+  for (int p = threadIdx.x; p < (s.K + kPage - 1) / kPage; p += 1024)
+    bad |= (uint32_t)a.page_ids[s.base + p] >= (uint32_t)a.num_pages;
+  return bad;
+}
+
+// The places lo .. hi - 1, eight at a time a lane, 64 beside each other: f(place, at,
+// weight) with at = the token's page * 16 + slot, -1 for a page outside the pool.
+// Lanes beyond hi call f too.
+template <class F>
+__device__ __forceinline__ void evict_walk(const EvictArgs& a, const EvictSeq& s,
+                                           const EvictShared& sh, int g, int lo, int hi,
+                                           bool want_weights, F f) {
+  const int lane = threadIdx.x & 63;
+  int r = 0;
+  {  // the route of place lo + lane
+    const int e = min(lo + lane, s.L - 1);
+    int top = s.routes;
+    while (top - r > 1) {
+      const int mid = (r + top) >> 1;
+      (sh.pre[mid] <= e ? r : top) = mid;
+    }
+  }
+  int begin = sh.pre[r], end = sh.pre[r + 1], base = sh.base[r];
+  for (int e0 = lo; e0 < hi; e0 += 512) {
+    int at[8];
+    float wt[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int e = e0 + 64 * i + lane;
+      at[i] = 0;
+      if (e < hi) {
+        if (e >= end) {
+          do ++r;
+          while (e >= sh.pre[r + 1]);
+          begin = sh.pre[r];
+          end = sh.pre[r + 1];
+          base = sh.base[r];
+        }
+        at[i] = a.page_ids[base + (e - begin) / kPage];
       }
+      wt[i] = __builtin_bit_cast(float, begin);  // (the slot follows from it)
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int e = e0 + 64 * i + lane, slot = (e - __builtin_bit_cast(int, wt[i])) & (kPage - 1);
+      wt[i] = 0.0f;
+      if (e < hi) {
+        at[i] = (uint32_t)at[i] < (uint32_t)a.num_pages ? at[i] * kPage + slot : -1;
+        if (want_weights && at[i] >= 0)
+          wt[i] = a.weights[((size_t)(at[i] >> 4) * a.num_kv_heads + g) * kPage + slot];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f(e0 + 64 * i + lane, at[i], wt[i]);
+  }
+}
+
+// One more of a bin, for the lanes that say so.  Many weights are alike: one lane
+// counts for all of one bin.
+__device__ __forceinline__ void evict_count(uint32_t* hist, bool mine, uint32_t bin) {
+  const uint64_t who = __ballot(mine);
+  if (!who) return;
+  const int lane = threadIdx.x & 63, lead = __builtin_ctzll(who);
+  const uint32_t one = __builtin_amdgcn_readlane(bin, lead);
+  if (__ballot(mine && bin == one) == who) {
+    if (lane == lead) atomicAdd(&hist[one], (uint32_t)__builtin_popcountll(who));
+  } else if (mine) {
+    atomicAdd(&hist[bin], 1u);
+  }
+}
+
+// The bin in which the want-th largest lies, and how many of that bin are wanted.
+// Thread t has h0 of bin bins - 1 - 2 t and h1 of the one below.
+__device__ __forceinline__ void evict_find(EvictShared& sh, int bins, int h0, int h1, int& bin,
+                                           int& want) {
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
+  const int y = wave_scan(h0 + h1, lane);
+  if (lane == 63) sh.scan[0][w] = y;
+  __syncthreads();
+  int all;
+  const int above = waves_before(sh.scan[0], w, all) + y - h0 - h1;
+  if (above < want && above + h0 + h1 >= want) {
+    const bool upper = above + h0 >= want;
+    sh.bin = bins - 1 - 2 * tid - (upper ? 0 : 1);
+    sh.want = want - above - (upper ? 0 : h0);
+  }
+  __syncthreads();
+  bin = sh.bin;
+  want = sh.want;
+}
+
+// What a place is: it stays for sure (one of the first or last ones, or its key is
+// larger than the threshold), or its key equals it, and it stays if it is one of the
+// first of these that are wanted.
+struct EvictRule {
+  int c0, c1;
+  bool none, every;  // none or all of those that compete stay
+  uint32_t top;
+  __device__ __forceinline__ bool sure(int e, uint32_t key) const {
+    return e < c0 || e >= c1 || every || (!none && key > top);
+  }
+  __device__ __forceinline__ bool equal(int e, uint32_t key) const {
+    return e >= c0 && e < c1 && !none && !every && key == top;
+  }
+};
+
+// Which tokens of a sequence and KV head stay, by one workgroup: a threshold by radix
+// over their keys, which stay in LDS, up to 34K of them.  Each wave has a stretch of the
+// places of its own, so that a place's rank is its wave's first rank and a count of
+// ballots.
+__global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
+  __shared__ uint32_t keys[kKeysInLds];
+  __shared__ uint32_t hist[kBins];
+  __shared__ EvictShared sh;
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
+  const int g = blockIdx.x, b = blockIdx.y;
+  int32_t* plan = a.plan + 2 * b;
+  EvictSeq s = evict_sequence(a, b, sh);
+  const int per = (s.L + 1023) / 1024 * 64;
+  const int lo = min(s.L, w * per), hi = min(s.L, lo + per);
+  const bool in_lds = s.L <= kKeysInLds;
+  if (s.status == 0) {
+    bool bad = evict_bad_target(a, s);
+    evict_walk(a, s, sh, g, lo, hi, in_lds, [&](int e, int at, float wt) {
+      if (e >= hi) return;
+      bad |= at < 0;
+      if (in_lds) keys[e] = order_key(wt);
+    });
+    if (__syncthreads_or(bad)) s.status = KF_EFLAG_BAD_PAGE;
+  }
+  if (g == 0 && tid == 0) {
+    plan[0] = s.status ? -1 : s.K;
+    plan[1] = s.base;
+    if (s.status > 0) atomicOr(a.err_flags, s.status);
+  }
+  if (s.status) return;
+
+  // the keys of this wave's places, eight at a time a lane
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    if (!in_lds) {
+      evict_walk(a, s, sh, g, lo, hi, true, [&](int e, int at, float wt) { f(e, order_key(wt)); });
+      return;
     }
     for (int e0 = lo; e0 < hi; e0 += 512) {
-      int at[8];
-      float wt[8];
+      uint32_t k[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int e = e0 + 64 * i + lane;
-        at[i] = 0;
-        if (e < hi) {
-          while (e >= pre[r + 1]) ++r;
-          const int j = e - pre[r], pid = a.page_ids[pbase[r] + j / kPage];
-          if ((uint32_t)pid < (uint32_t)a.num_pages)
-            at[i] = pid * kPage + j % kPage;
-          else
-            at[i] = -1;
-        }
-      }
+      for (int i = 0; i < 8; ++i) k[i] = keys[min(e0 + 64 * i + lane, s.L - 1)];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        wt[i] = 0.0f;
-        if (want_weights && e0 + 64 * i + lane < hi && at[i] >= 0)
-          wt[i] = a.weights[((size_t)(at[i] >> 4) * H + g) * kPage + (at[i] & 15)];
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f(e0 + 64 * i + lane, at[i], wt[i]);
+      for (int i = 0; i < 8; ++i) f(e0 + 64 * i + lane, k[i]);
     }
   };
-  const bool in_lds = L <= kKeysInLds;
-  walk(in_lds, [&](int e, int at, float wt) {
-    if (e >= hi) return;
-    bad |= at < 0;
-    if (in_lds) keys[e] = order_key(wt);
-  });
-  if (__syncthreads_or(bad)) return fail(KF_EFLAG_BAD_PAGE);
-
-  const int c0 = first, c1 = L - last;  // the places that compete
-  int want = K - first - last;          // and how many of them stay
-  uint32_t top = 0;                     // the threshold's bits so far
-  const bool none = want == 0, every = want == c1 - c0;
-  if (!none && !every) {
+  int want = s.K - s.c0 - (s.L - s.c1);  // of those that compete
+  EvictRule rule{s.c0, s.c1, want == 0, want == s.c1 - s.c0, 0};
+  if (!rule.none && !rule.every) {
+    const int from = max(lo, s.c0), till = min(hi, s.c1);
     for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-      const int above = pass == 0 ? 32 : pass == 1 ? 21 : 10;
+      const int bins = pass_bins(pass);
       hist[tid] = hist[tid + 1024] = 0;
       __syncthreads();
-      auto count = [&](int e, uint32_t key) __attribute__((always_inline)) {
-        const bool mine = e >= max(lo, c0) && e < min(hi, c1) &&
-                          (pass == 0 || key >> above == top >> above);
-        const uint64_t who = __ballot(mine);
-        if (!who) return;
-        const uint32_t bin = (key >> shift) & (bins - 1);
-        const int lead = __builtin_ctzll(who);
-        const uint32_t one = __builtin_amdgcn_readlane(bin, lead);
-        if (__ballot(mine && bin == one) == who) {  // many weights are alike
-          if (lane == lead) atomicAdd(&hist[one], (uint32_t)__builtin_popcountll(who));
-        } else if (mine) {
-          atomicAdd(&hist[bin], 1u);
-        }
-      };
-      if (in_lds) {
-        for (int e = lo + lane; e < lo + per; e += 64) count(e, e < hi ? keys[e] : 0);
-      } else {
-        walk(true, [&](int e, int, float wt) { count(e, order_key(wt)); });
-      }
+      each([&](int e, uint32_t key) {
+        evict_count(hist, e >= from && e < till && pass_takes(pass, key, rule.top),
+                    key >> pass_shift(pass) & (bins - 1));
+      });
       __syncthreads();
-      // the bin in which the want-th largest lies: thread t has bins 2 t and 2 t + 1 from
-      // the top
-      const int bin = bins - 1 - 2 * tid;
-      const int h0 = bin > 0 ? (int)hist[bin] : 0, h1 = bin > 0 ? (int)hist[bin - 1] : 0;
-      int y = h0 + h1;
-#pragma unroll
-      for (int m = 1; m < 64; m <<= 1) {
-        const int z = __shfl_up(y, m);
-        if (lane >= m) y += z;
-      }
-      if (lane == 63) s_scan[0][w] = y;
-      __syncthreads();
-      int under = y - h0 - h1;
-      for (int i = 0; i < w; ++i) under += s_scan[0][i];
-      if (under < want && under + h0 + h1 >= want) {
-        const bool upper = under + h0 >= want;
-        s_bin = upper ? bin : bin - 1;
-        s_want = want - under - (upper ? 0 : h0);
-      }
-      __syncthreads();
-      top |= (uint32_t)s_bin << shift;
-      want = s_want;
-      __syncthreads();
+      const int at = bins - 1 - 2 * tid;
+      int bin;
+      evict_find(sh, bins, at > 0 ? hist[at] : 0, at > 0 ? hist[at - 1] : 0, bin, want);
+      rule.top |= (uint32_t)bin << pass_shift(pass);
     }
-  }
-  // A place stays if it is one of the first or last ones, if its key is larger than
-  // top, or if it is one of the first `want` equal ones.
-  auto kind = [&](int e, uint32_t key, bool& equal) -> bool {
-    equal = false;
-    if (e >= hi) return false;
-    if (e < c0 || e >= c1) return true;
-    if (none) return false;
-    if (every) return true;
-    equal = key == top;
-    return key > top;
-  };
-  int sure = 0, equals = 0;
-  auto tally = [&](int e, uint32_t key) {
-    bool eq;
-    const bool yes = kind(e, key, eq);
-    sure += __builtin_popcountll(__ballot(yes));
-    equals += __builtin_popcountll(__ballot(eq));
-  };
-  if (in_lds) {
-    for (int e = lo + lane; e < lo + per; e += 64) tally(e, e < hi ? keys[e] : 0);
   } else {
-    walk(true, [&](int e, int, float wt) { tally(e, order_key(wt)); });
+    want = 0;
   }
+  int sure = 0, equals = 0;
+  each([&](int e, uint32_t key) {
+    sure += __builtin_popcountll(__ballot(e < hi && rule.sure(e, key)));
+    equals += __builtin_popcountll(__ballot(e < hi && rule.equal(e, key)));
+  });
+  __syncthreads();
   if (lane == 0) {
-    s_scan[0][w] = sure;
-    s_scan[1][w] = equals;
+    sh.scan[0][w] = sure;
+    sh.scan[1][w] = equals;
   }
   __syncthreads();
-  sure = equals = 0;
-  for (int i = 0; i < w; ++i) {
-    sure += s_scan[0][i];
-    equals += s_scan[1][i];
-  }
-  if (none || every) want = 0;
-  int32_t* list = a.list + ((size_t)b * H + g) * a.max_keep;
+  int all;
+  sure = waves_before(sh.scan[0], w, all);
+  equals = waves_before(sh.scan[1], w, all);
+  int32_t* list = a.list + ((size_t)b * a.num_kv_heads + g) * a.max_keep;
   const uint64_t lower = ((uint64_t)1 << lane) - 1;
-  walk(!in_lds, [&](int e, int at, float wt) {
-    bool eq;
-    const uint32_t key = in_lds ? (e < hi ? keys[e] : 0) : order_key(wt);
-    const bool yes = kind(e, key, eq);
+  evict_walk(a, s, sh, g, lo, hi, !in_lds, [&](int e, int at, float wt) {
+    const uint32_t key = in_lds ? keys[min(e, s.L - 1)] : order_key(wt);
+    const bool yes = e < hi && rule.sure(e, key), eq = e < hi && rule.equal(e, key);
     const uint64_t ys = __ballot(yes), es = __ballot(eq);
     const int eq_rank = equals + __builtin_popcountll(es & lower);
-    const int rank = sure + __builtin_popcountll(ys & lower) + min(eq_rank, want);
-    if (yes || (eq && eq_rank < want)) list[rank] = at;
+    if (yes || (eq && eq_rank < want))
+      list[sure + __builtin_popcountll(ys & lower) + min(eq_rank, want)] = at;
     sure += __builtin_popcountll(ys);
     equals += __builtin_popcountll(es);
   });
-  if (g == 0 && tid == 0) {
-    plan[0] = K;
-    plan[1] = to.page_base;
+}
+
+// The same by several workgroups of a sequence and KV head, a launch for each pass:
+// each has a part of the places and counts it into a row of bins of its own, and the
+// launch behind adds up the rows.
+struct EvictPart {
+  int parts, lo, hi;  // parts that the sequence has, this one's places
+};
+__device__ __forceinline__ EvictPart evict_part(const EvictArgs& a, const EvictSeq& s, int p) {
+  EvictPart x;
+  x.parts = max(1, min(a.parts, (s.L + kPartTokens - 1) / kPartTokens));
+  const int per = ((s.L + x.parts - 1) / x.parts + 1023) / 1024 * 1024;
+  x.lo = (int)min((int64_t)s.L, (int64_t)p * per);
+  x.hi = (int)min((int64_t)s.L, (int64_t)x.lo + per);
+  return x;
+}
+// Row of bins of part p in a pass.
+__device__ __forceinline__ uint32_t* evict_row(const EvictArgs& a, int b, int g, int p, int pass) {
+  return a.rows + ((((size_t)b * a.num_kv_heads + g) * a.parts + p) * 3 + pass) * kBins;
+}
+__device__ __forceinline__ int32_t* evict_state(const EvictArgs& a, int b, int g, int p) {
+  return a.state + (((size_t)b * a.num_kv_heads + g) * a.parts + p) * 4;
+}
+
+// Adds up the rows of a pass, finds the bin, and returns the keys above it in part p
+// (MINE), or in the parts before it, with those in the bin in `same`.
+template <bool MINE>
+__device__ __forceinline__ int evict_next(const EvictArgs& a, EvictShared& sh, int b, int g, int p,
+                                          int parts, int pass, uint32_t& top, int& want,
+                                          int& same) {
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
+  const int bins = pass_bins(pass), at = bins - 1 - 2 * tid;
+  int h0 = 0, h1 = 0, x0 = 0, x1 = 0;
+  if (at > 0) {
+#pragma unroll 4
+    for (int i = 0; i < parts; ++i) {
+      const u32x2 h = *reinterpret_cast<const u32x2*>(evict_row(a, b, g, i, pass) + at - 1);
+      h0 += h.y;
+      h1 += h.x;
+      if (MINE ? i == p : i < p) {
+        x0 += h.y;
+        x1 += h.x;
+      }
+    }
   }
+  int bin;
+  evict_find(sh, bins, h0, h1, bin, want);
+  top |= (uint32_t)bin << pass_shift(pass);
+  int above = (at > bin ? x0 : 0) + (at - 1 > bin ? x1 : 0);
+  int in_bin = at == bin ? x0 : at - 1 == bin ? x1 : 0;
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) {
+    above += __shfl_xor(above, m);
+    in_bin += __shfl_xor(in_bin, m);
+  }
+  __syncthreads();
+  if (lane == 0) {
+    sh.scan[0][w] = above;
+    sh.scan[1][w] = in_bin;
+  }
+  __syncthreads();
+  waves_before(sh.scan[1], w, same);
+  waves_before(sh.scan[0], w, above);
+  return above;
+}
+
+template <int PASS>
+__global__ __launch_bounds__(1024) void evict_count_kernel(EvictArgs a) {
+  __shared__ uint32_t hist[kBins];
+  __shared__ EvictShared sh;
+  const int tid = threadIdx.x, w = uniform(tid >> 6);
+  const int p = blockIdx.x % a.parts, g = blockIdx.x / a.parts, b = blockIdx.y;
+  const EvictSeq s = evict_sequence(a, b, sh);
+  if (s.status) return;
+  const EvictPart part = evict_part(a, s, p);
+  if (p >= part.parts) return;
+  int want = s.K - s.c0 - (s.L - s.c1);
+  const bool counts = want != 0 && want != s.c1 - s.c0;
+  if (PASS > 0 && !counts) return;
+  int32_t* state = evict_state(a, b, g, p);
+  uint32_t top = 0;
+  if constexpr (PASS > 0) {
+    int same;
+    if (PASS > 1) {  // (the first part's: the launch before wrote the same to all)
+      top = state[0];
+      want = state[1];
+    }
+    const int above = evict_next<true>(a, sh, b, g, p, part.parts, PASS - 1, top, want, same);
+    if (tid == 0) {
+      state[0] = top;
+      state[1] = want;
+      state[2] = above + (PASS > 1 ? state[2] : 0);
+    }
+  }
+  hist[tid] = hist[tid + 1024] = 0;
+  __syncthreads();
+  const int per = (part.hi - part.lo + 1023) / 1024 * 64;
+  const int lo = min(part.hi, part.lo + w * per), hi = min(part.hi, lo + per);
+  const int from = max(lo, s.c0), till = min(hi, s.c1);
+  bool bad = false;
+  evict_walk(a, s, sh, g, lo, hi, counts, [&](int e, int at, float wt) {
+    if (e < hi) bad |= at < 0;
+    const uint32_t key = order_key(wt);
+    evict_count(hist, counts && e >= from && e < till && pass_takes(PASS, key, top),
+                key >> pass_shift(PASS) & (pass_bins(PASS) - 1));
+  });
+  if constexpr (PASS == 0) {
+    if (p == 0) bad |= evict_bad_target(a, s);
+    bad = __syncthreads_or(bad);
+    if (tid == 0) state[3] = bad;
+  } else {
+    __syncthreads();
+  }
+  reinterpret_cast<u32x2*>(evict_row(a, b, g, p, PASS))[tid] =
+      *reinterpret_cast<const u32x2*>(hist + 2 * tid);
+}
+
+__global__ __launch_bounds__(1024) void evict_list_kernel(EvictArgs a) {
+  __shared__ EvictShared sh;
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
+  const int p = blockIdx.x % a.parts, g = blockIdx.x / a.parts, b = blockIdx.y;
+  EvictSeq s = evict_sequence(a, b, sh);
+  const EvictPart part = evict_part(a, s, p);
+  if (s.status == 0) {
+    bool bad = false;
+    for (int i = lane; i < part.parts; i += 64) bad |= evict_state(a, b, g, i)[3] != 0;
+    if (__ballot(bad)) s.status = KF_EFLAG_BAD_PAGE;
+  }
+  if (blockIdx.x == 0 && tid == 0) {
+    int32_t* plan = a.plan + 2 * b;
+    plan[0] = s.status ? -1 : s.K;
+    plan[1] = s.base;
+    if (s.status > 0) atomicOr(a.err_flags, s.status);
+  }
+  if (s.status || p >= part.parts) return;
+  int want = s.K - s.c0 - (s.L - s.c1);
+  EvictRule rule{s.c0, s.c1, want == 0, want == s.c1 - s.c0, 0};
+  // those that stay before this part: first and last ones, larger keys, equal ones
+  int sure = min(part.lo, s.c0) + max(0, part.lo - s.c1), equals = 0;
+  const bool counts = !rule.none && !rule.every;
+  if (counts) {
+    int32_t* state = evict_state(a, b, g, 0);
+    rule.top = state[0];
+    want = state[1];
+    sure += evict_next<false>(a, sh, b, g, p, part.parts, 2, rule.top, want, equals);
+    for (int i = 0; i < p; ++i) sure += evict_state(a, b, g, i)[2];
+  } else {
+    if (rule.every) sure += max(0, min(part.lo, s.c1) - s.c0);
+    want = 0;
+  }
+  const int per = (part.hi - part.lo + 1023) / 1024 * 64;
+  const int lo = min(part.hi, part.lo + w * per), hi = min(part.hi, lo + per);
+  int mine = 0, alike = 0;
+  evict_walk(a, s, sh, g, lo, hi, counts, [&](int e, int at, float wt) {
+    const uint32_t key = order_key(wt);
+    mine += __builtin_popcountll(__ballot(e < hi && rule.sure(e, key)));
+    alike += __builtin_popcountll(__ballot(e < hi && rule.equal(e, key)));
+  });
+  __syncthreads();
+  if (lane == 0) {
+    sh.scan[0][w] = mine;
+    sh.scan[1][w] = alike;
+  }
+  __syncthreads();
+  int all;
+  sure += waves_before(sh.scan[0], w, all);
+  equals += waves_before(sh.scan[1], w, all);
+  int32_t* list = a.list + ((size_t)b * a.num_kv_heads + g) * a.max_keep;
+  const uint64_t lower = ((uint64_t)1 << lane) - 1;
+  evict_walk(a, s, sh, g, lo, hi, counts, [&](int e, int at, float wt) {
+    const uint32_t key = order_key(wt);
+    const bool yes = e < hi && rule.sure(e, key), eq = e < hi && rule.equal(e, key);
+    const uint64_t ys = __ballot(yes), es = __ballot(eq);
+    const int eq_rank = equals + __builtin_popcountll(es & lower);
+    if (yes || (eq && eq_rank < want))
+      list[sure + __builtin_popcountll(ys & lower) + min(eq_rank, want)] = at;
+    sure += __builtin_popcountll(ys);
+    equals += __builtin_popcountll(es);
+  });
 }
 
 // A code of a page of scale was as one of a page of scale now: the nearest to
@@ -764,7 +1022,15 @@ hipError_t launch_attn_weights(const AttnWeightsArgs& a, bool fp8, hipStream_t s
 }
 
 hipError_t launch_evict(const EvictArgs& a, bool fp8, hipStream_t stream) {
-  evict_select_kernel<<<dim3(a.num_kv_heads, a.num_seqs), 1024, 0, stream>>>(a);
+  if (a.parts > 1) {
+    const dim3 grid((uint32_t)a.num_kv_heads * a.parts, a.num_seqs);
+    evict_count_kernel<0><<<grid, 1024, 0, stream>>>(a);
+    evict_count_kernel<1><<<grid, 1024, 0, stream>>>(a);
+    evict_count_kernel<2><<<grid, 1024, 0, stream>>>(a);
+    evict_list_kernel<<<grid, 1024, 0, stream>>>(a);
+  } else {
+    evict_select_kernel<<<dim3(a.num_kv_heads, a.num_seqs), 1024, 0, stream>>>(a);
+  }
   const hipError_t st = hipGetLastError();
   if (st != hipSuccess) return st;
   const int64_t pages = ((int64_t)a.max_keep + kPage - 1) / kPage;

@@ -19,10 +19,6 @@ hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
 
 int64_t div_up(int64_t x, int64_t y) { return (x + y - 1) / y; }
 
-size_t evict_list_offset(int32_t num_seqs) {
-  return ((size_t)num_seqs * 2 * sizeof(int32_t) + 255) / 256 * 256;
-}
-
 // A page and a slot of it share 31 bits of the list of what stays.
 bool pages_fit(const kf_shape* s) { return s->num_pages <= INT32_MAX / KF_PAGE_SIZE; }
 
@@ -86,8 +82,7 @@ int kf_attn_weights(const kf_shape* shape, const void* q, int32_t num_rows, int6
 size_t kf_kv_evict_workspace_bytes(const kf_shape* shape, int32_t max_keep) {
   if (kf::check_shape(shape) != KF_OK || max_keep < 0) return 0;
   if (shape->num_seqs > kf::kMaxLaunchRoutes || shape->num_kv_heads > kf::kMaxLaunchRoutes) return 0;
-  return evict_list_offset(shape->num_seqs) + 256 +
-         (size_t)shape->num_seqs * shape->num_kv_heads * max_keep * sizeof(int32_t);
+  return kf::evict_layout(*shape, max_keep).total;
 }
 
 int kf_kv_evict(const kf_shape* shape, void* k_pool, void* v_pool, float* k_scale, float* v_scale,
@@ -111,9 +106,10 @@ int kf_kv_evict(const kf_shape* shape, void* k_pool, void* v_pool, float* k_scal
     if (p && !aligned(p, 4)) return KF_ERR_INVALID_ARG;
   const int64_t pages = div_up(max_keep, KF_PAGE_SIZE);
   const size_t need = kf_kv_evict_workspace_bytes(shape, max_keep);
+  const kf::EvictLayout l = kf::evict_layout(*shape, max_keep);
   if (need == 0 || !pages_fit(shape) ||
       (div_up(pages * 2 * shape->num_kv_heads, 4) + 1) * shape->num_seqs > kf::kMaxBudgetWgs ||
-      (int64_t)shape->num_kv_heads * shape->num_seqs * 4 > kf::kMaxBudgetWgs)
+      (int64_t)shape->num_kv_heads * shape->num_seqs * 4 * l.parts > kf::kMaxBudgetWgs)
     return KF_ERR_UNSUPPORTED;
   if (!workspace || !aligned(workspace, 16) || workspace_bytes < need) return KF_ERR_WORKSPACE;
 
@@ -139,15 +135,35 @@ int kf_kv_evict(const kf_shape* shape, void* k_pool, void* v_pool, float* k_scal
   a.max_keep = max_keep;
   a.keep_first = keep_first;
   a.keep_last = keep_last;
-  a.plan = static_cast<int32_t*>(workspace);
-  a.list = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) +
-                                      evict_list_offset(shape->num_seqs));
+  char* ws = static_cast<char*>(workspace);
+  a.plan = reinterpret_cast<int32_t*>(ws);
+  a.list = reinterpret_cast<int32_t*>(ws + l.list_off);
+  a.parts = l.parts;
+  a.state = reinterpret_cast<int32_t*>(ws + l.state_off);
+  a.rows = reinterpret_cast<uint32_t*>(ws + l.rows_off);
   return kf::launch_evict(a, fp8_pool(shape), as_stream(stream)) == hipSuccess ? KF_OK : KF_ERR_HIP;
 }
 
 }  // extern "C"
 
 namespace kf {
+
+// Sequences of more tokens than one part has, on the mean of what the table reserves,
+// are told apart by several workgroups each.
+EvictLayout evict_layout(const kf_shape& s, int32_t max_keep) {
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  EvictLayout l{};
+  const int64_t tokens = (int64_t)s.num_page_ids * KF_PAGE_SIZE / std::max(1, s.num_seqs);
+  l.parts = (int32_t)std::min<int64_t>(kMaxParts, std::max<int64_t>(1, tokens / kPartTokens));
+  const size_t units = (size_t)s.num_seqs * s.num_kv_heads;
+  while (l.parts > 1 && units * l.parts > kMostParts) --l.parts;
+  l.list_off = up((size_t)s.num_seqs * 2 * sizeof(int32_t)) + 256;
+  l.state_off = l.list_off + up(units * max_keep * sizeof(int32_t));
+  const size_t parts = l.parts > 1 ? units * l.parts : 0;
+  l.rows_off = l.state_off + up(parts * 4 * sizeof(int32_t));
+  l.total = l.rows_off + parts * 3 * 2048 * sizeof(uint32_t);
+  return l;
+}
 
 // How a launch's keys are dealt out, by what the host knows: the pages that the table
 // reserves, and the (row, head) pairs of a sequence on the mean.

@@ -210,3 +210,43 @@ def test_graph_replays_and_streams(gpu):
         g.replay()
         torch.cuda.synchronize()
         assert_evicted(evict_result(c, d, w), want, f"replay {i}")
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_one_long_sequence_among_short_ones(gpu, fp8):
+    # more tokens than a workgroup keeps in LDS, where the launch has one per sequence
+    lens = [40000] + [20] * 9
+    c = Evictable(lens, [7000] + [15] * 9, H=1, fp8=fp8, part=9000, seed=12)
+    check(c, 4, 500)
+
+
+@pytest.mark.parametrize("keep,first,last", [(1, 0, 0), (9000, 0, 9000), (20000, 20000, 0),
+                                             (30000, 10, 10), (25000, 0, 1), (70000, 5, 5),
+                                             (0, 0, 0)])
+def test_parts_of_a_long_sequence(gpu, keep, first, last):
+    c = Evictable([30000, 9000], [keep, keep], H=2, part=7000, seed=13)
+    c.weights[np.random.default_rng(3).random(c.weights.shape) < 0.4] = 0.5
+    check(c, first, last)
+
+
+@pytest.mark.parametrize("what", ["page", "first_page", "dst_page", "cap", "row"])
+def test_refusals_of_a_long_sequence(gpu, what):
+    c = Evictable([30000, 20000], [900, 1000], H=2, part=7000, seed=14)
+    row, to = int(c.seq_route_begin[1]), int(c.into[1])
+    bad = 1
+    if what == "page":
+        c.page_ids[c.routes[row + 2, 4] + 300] = -1
+    elif what == "first_page":           # behind them: the first one that takes what stays
+        c.page_ids[c.routes[row + 2, 4] + 400] = -1
+        bad = 0
+    elif what == "dst_page":
+        c.page_ids[c.routes[to, 4] + 60] = c.k_pool.shape[0]
+    elif what == "cap":
+        c.routes[to, 5] = 3
+    else:
+        c.routes[row, 0] = 0
+    got = check(c, 4, 10)
+    assert got[6] == {"page": 4, "first_page": 4, "dst_page": 4, "cap": 1, "row": 2}[what]
+    lo, hi = c.seq_route_begin[bad], c.seq_route_begin[bad + 1]
+    assert np.array_equal(got[3][lo:hi], c.routes[lo:hi])
+    assert got[3][c.into[1 - bad], 3] == (900, 1000)[1 - bad]
