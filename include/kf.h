@@ -499,14 +499,20 @@ int kf_tree_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64_t
  * sequence's row of seq_row_begin decreases or leaves [0, num_rows], or that fails
  * kf_partial_attn's checks sets KF_EFLAG_BAD_ROUTE and is left as it was; tokens of
  * a page whose id lies outside the pool set KF_EFLAG_BAD_PAGE and have no weight.
- * At most 65535 routes in a call.
+ * At most 65535 routes, and 2^28 - 256 (row, query head of a group) pairs, in a call.
+ * workspace: kf_attn_weights_workspace_bytes of the same arguments (launches of many
+ * rows over few pages split the rows' sum and use it: 4 MB at most), 16-byte aligned;
+ * dead between calls, and calls that may overlap need their own.
  * Alignment: q and k_pool 16 bytes, the rest 4.
  */
+size_t kf_attn_weights_workspace_bytes(const kf_shape* shape, int32_t num_rows, int32_t num_routes,
+                                       int32_t max_pages_per_route);
 int kf_attn_weights(const kf_shape* shape, const void* q, int32_t num_rows, int64_t q_stride,
                     const float* lse, const int32_t* seq_row_begin, const int32_t* first_pos,
                     const void* k_pool, const float* k_scale, const kf_route* routes,
                     int32_t num_routes, int32_t max_pages_per_route, const int32_t* page_ids,
-                    float decay, float* weights, int32_t* err_flags, void* stream);
+                    float decay, float* weights, void* workspace, size_t workspace_bytes,
+                    int32_t* err_flags, void* stream);
 
 /*
  * kf_kv_evict -- eviction by weight: of the L tokens of sequence b, in the order of

@@ -9,7 +9,14 @@ namespace kf {
 constexpr int64_t kMaxBudgetWgs = 0xFFFFFF;  // workgroups of a launch: 32 bits of threads
 
 // ------------------------------------------------------------- attn_weights
-constexpr int kFewColumns = 64;  // (row, head) pairs of a sequence that stay in registers
+constexpr int kFewColumns = 64;    // (row, head) pairs of a sequence that stay in registers
+constexpr int kHeldColumns = 256;  // ... in LDS
+// Workgroups that share more columns than that, and 32 columns steps of each at least.
+// With 1, 4, 8 and 16, us: prompts of 500 rows 60, 27, 20 and 17, of 2000 183, 65, 54 and
+// 66, of 10K 949, 556, 518 and 521, 16 of 300 .. 1500 190, 165, 181 and 239 (5 by the rule).
+constexpr int kMaxSegments = 8;
+constexpr int64_t kSegmentSteps = 4;
+constexpr int64_t kSegmentWgs = 8;  // workgroups of a launch at most, per resident one
 
 struct AttnWeightsArgs {
   const uint16_t* q;
@@ -28,11 +35,17 @@ struct AttnWeightsArgs {
   int32_t num_routes, max_pages_per_route, num_pages, num_page_ids;
   int32_t head_major;
   int32_t chunk_pages, chunks;  // pages of a workgroup, workgroups of a route and KV head
-  int32_t key_waves;            // waves beside each other along the keys: 1, 2 or 4 of 4
+  int32_t segments;  // workgroups that share the columns of the same keys
+  float* sums;       // workspace: [segments][num_routes][chunks * Hkv][256 tokens], if they are
+                     // several
 };
 
-// Fills chunk_pages, chunks and key_waves for `slots` resident workgroups.
+// How a launch is dealt out, by what the host knows; and its workspace (0: none).
 void plan_attn_weights(AttnWeightsArgs& a, int64_t slots);
+inline size_t attn_weights_bytes(const AttnWeightsArgs& a) {
+  return a.segments == 1 ? 0 : (size_t)a.segments * a.num_routes * a.chunks * a.num_kv_heads *
+                                   256 * sizeof(float);
+}
 
 hipError_t launch_attn_weights(const AttnWeightsArgs& a, bool fp8, hipStream_t stream);
 

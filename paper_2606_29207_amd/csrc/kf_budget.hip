@@ -1,8 +1,11 @@
 // gfx950 kernels of the operators that keep a cache within a budget:
 //   attn_weights_kernel -- the attention weight that every token receives
+//   attn_weights_join_kernel -- its sums where several workgroups shared the columns
 //   evict_select_kernel -- which tokens of a sequence and KV head stay, by one workgroup
 //   evict_count_kernel, evict_list_kernel -- the same by several, a launch for each pass
 //   evict_move_kernel   -- those tokens into the pages of another route
+#include <type_traits>
+
 #include "kf_budget.h"
 #include "kf_device.h"
 
@@ -25,14 +28,6 @@ __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// 16 bytes a lane from memory straight into LDS, 1 KiB a wave.
-__device__ __forceinline__ void to_lds16(const uint16_t* g, char* l) {
-  __builtin_amdgcn_global_load_lds(
-      (const __attribute__((address_space(1))) uint32_t*)g,
-      (__attribute__((address_space(3))) uint32_t*)(__attribute__((address_space(3))) void*)l, 16,
-      0, 0);
-}
-
 // One route and KV head as a workgroup sees it.  The (row, query head) pairs of the
 // sequence are its columns: column c is row c / G, head g G + c % G.
 struct Seen {
@@ -50,15 +45,63 @@ __device__ __forceinline__ int reach(const Seen& s, int64_t i) {
 // Whether a row has a softmax: it saw a token, and its lse is a number.
 __device__ __forceinline__ bool has_softmax(float lse) { return lse > neg_inf(); }
 
+// 16 bytes a lane from memory straight into LDS, 1 KiB a wave.
+__device__ __forceinline__ void to_lds16(const char* g, char* l) {
+  __builtin_amdgcn_global_load_lds(
+      (const __attribute__((address_space(1))) uint32_t*)g,
+      (__attribute__((address_space(3))) uint32_t*)(__attribute__((address_space(3))) void*)l, 16,
+      0, 2);  // once: the non-temporal hint (32K-token decode 204 us without it, 189 with)
+}
+
 // Few columns (a decode step, a small tree): they stay in registers, 16 a matrix
-// product, and the keys stream past, a page of 16 per product of depth 32.
+// product, and the keys stream past, a page of 16 per product of depth 32.  Pages go
+// through LDS, where each wave has two buffers of 8 KiB of its own: loads of 1 KiB in a
+// row, where the operands' own places are 64 bytes of each key's 256.
 template <bool FP8, int NC>
-__device__ __forceinline__ void few_columns(const AttnWeightsArgs& a, const Seen& s, int& flag) {
-  constexpr int kBatch = NC == 1 ? 4 : 2;  // pages on their way at a time
-  constexpr int kLoads = FP8 ? 2 : 4;
+__device__ __forceinline__ void few_columns(const AttnWeightsArgs& a, const Seen& s,
+                                            char* __restrict__ buf_x, char* __restrict__ buf_y,
+                                            int& flag) {
+  constexpr int kBatch = FP8 ? 4 : 2;                 // pages of a buffer
+  constexpr int kPageBytes = kPage * kDim * (FP8 ? 1 : 2), kLoads = kPageBytes / 1024;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int n16 = lane & 15, grp = lane >> 4, H = a.num_kv_heads, G = a.group;
   const uint32_t C = (uint32_t)s.rows * G;
+  constexpr int kStep = 4 * kBatch;  // the four waves take batches in turn
+  int p = s.p0 + kBatch * wave;
+  if (p >= s.p1) return;
+  buf_x += 8192 * wave;
+  buf_y += 8192 * wave;
+  // Chunk c (16 bytes) of row r lies at chunk c ^ r (fp8: of its row of two, c ^ r / 2):
+  // the sixteen rows that an operand reads at once cover all banks.
+  uint32_t from[kLoads];  // in a page, of the lane's chunk of each load
+#pragma unroll
+  for (int k = 0; k < kLoads; ++k) {
+    const int x = 64 * k + lane;  // chunk of the page
+    from[k] = 16 * (FP8 ? (x & ~7) | ((x ^ (x >> 4)) & 7) : (x & ~15) | ((x ^ (x >> 4)) & 15));
+  }
+  const char* pool = static_cast<const char*>(a.k_pool);
+
+  struct Batch {
+    float scale[kBatch], old[kBatch];
+    int pid[kBatch];
+  };
+  auto load = [&](Batch& b, int p, char* __restrict__ buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (p + i >= s.p1) break;
+      int pid = fixed(a.page_ids)[s.base + p + i];
+      b.pid[i] = pid;
+      if ((uint32_t)pid >= (uint32_t)a.num_pages) pid = 0;
+      const char* page = pool + slice_of(pid, s.g, H, a.num_pages, a.head_major) * kPageBytes;
+#pragma unroll
+      for (int k = 0; k < kLoads; ++k) to_lds16(page + from[k], buf + kPageBytes * i + 1024 * k);
+      b.scale[i] = FP8 ? fixed(a.k_scale)[(size_t)pid * H + s.g] : 1.0f;
+      b.old[i] = 0.0f;
+      if (a.decay != 0.0f) b.old[i] = a.weights[((size_t)pid * H + s.g) * kPage + n16];
+    }
+  };
+  Batch x, y;
+  load(x, p, buf_x);
   u32x4 q[NC][4];
   float lse[NC][4];
   int sees[NC][4];
@@ -73,47 +116,28 @@ __device__ __forceinline__ void few_columns(const AttnWeightsArgs& a, const Seen
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t m = 16 * t + 4 * grp + i, mm = m < C ? m : C - 1;
-      const float x = a.lse[(s.row0 + (int64_t)(mm / G)) * a.num_q_heads + s.g * G + mm % G];
-      lse[t][i] = x * kLog2e;
-      sees[t][i] = m < C && has_softmax(x) ? reach(s, mm / G) : -1;
+      const float z = a.lse[(s.row0 + (int64_t)(mm / G)) * a.num_q_heads + s.g * G + mm % G];
+      lse[t][i] = z * kLog2e;
+      sees[t][i] = m < C && has_softmax(z) ? reach(s, mm / G) : -1;
     }
   }
-  const size_t head_bytes = kPage * kDim * (FP8 ? 1 : 2);
-  const char* pool = static_cast<const char*>(a.k_pool);
-  const uint32_t at = FP8 ? n16 * kDim + 16 * grp : 2 * (n16 * kDim + 8 * grp);
-
-  struct Batch {
-    u32x4 k[kBatch][kLoads];
-    float scale[kBatch], old[kBatch];
-    int pid[kBatch];
-  };
-  auto load = [&](Batch& b, int p) __attribute__((always_inline)) {
+  auto work = [&](const Batch& b, int p, const char* __restrict__ buf)
+      __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       if (p + i >= s.p1) break;
-      int pid = fixed(a.page_ids)[s.base + p + i];
-      b.pid[i] = pid;
-      if ((uint32_t)pid >= (uint32_t)a.num_pages) pid = 0;
-      const char* from = pool + slice_of(pid, s.g, H, a.num_pages, a.head_major) * head_bytes + at;
-#pragma unroll
-      for (int k = 0; k < kLoads; ++k)
-        b.k[i][k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from + 64 * k));
-      b.scale[i] = FP8 ? a.k_scale[(size_t)pid * H + s.g] : 1.0f;
-      b.old[i] = 0.0f;
-      if (a.decay != 0.0f) b.old[i] = a.weights[((size_t)pid * H + s.g) * kPage + n16];
-    }
-  };
-  auto work = [&](const Batch& b, int p) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      if (p + i >= s.p1) break;
+      const char* page = buf + kPageBytes * i;
       u32x4 k[4];
       if constexpr (FP8) {
-        widen(b.k[i][0], k[0], k[1]);
-        widen(b.k[i][1], k[2], k[3]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          widen(*reinterpret_cast<const u32x4*>(page + 128 * n16 +
+                                                16 * ((4 * u + grp) ^ (n16 >> 1))),
+                k[2 * u], k[2 * u + 1]);
       } else {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) k[u] = b.k[i][u];
+        for (int u = 0; u < 4; ++u)
+          k[u] = *reinterpret_cast<const u32x4*>(page + 256 * n16 + 16 * ((4 * u + grp) ^ n16));
       }
       const float c = a.scale_log2 * b.scale[i];
       const int j = (p + i) * kPage + n16;
@@ -139,241 +163,490 @@ __device__ __forceinline__ void few_columns(const AttnWeightsArgs& a, const Seen
             j < s.first && a.decay != 0.0f ? __builtin_fmaf(a.decay, b.old[i], sum) : sum;
     }
   };
-  constexpr int kStep = 4 * kBatch;  // the four waves take batches in turn
-  int p = s.p0 + kBatch * wave;
-  if (p >= s.p1) return;
-  Batch x, y;
-  load(x, p);
-  for (;;) {
-    if (p + kStep < s.p1) load(y, p + kStep);
-    work(x, p);
-    if ((p += kStep) >= s.p1) break;
-    if (p + kStep < s.p1) load(x, p + kStep);
-    work(y, p);
-    if ((p += kStep) >= s.p1) break;
+  // Waits for a batch: the loads of the next one, if it is whole, may still be out (8 of
+  // its pages, and what its tokens' weights were; ids and scales are scalar loads).
+  auto wait = [&](int next) __attribute__((always_inline)) {
+    static_assert(kBatch * kLoads == 8, "");
+    asm volatile("" ::: "memory");
+    if (next + kBatch > s.p1)
+      __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+    else if (a.decay != 0.0f)
+      __builtin_amdgcn_s_waitcnt(0x0F70 | (8 + kBatch));
+    else
+      __builtin_amdgcn_s_waitcnt(0x0F70 | 8);
+    asm volatile("" ::: "memory");
+  };
+  auto read = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };  // what the wave reads
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // the columns: or every step would wait for them
+  // (One function with both buffers, so that the reads of one are known not to wait for
+  // loads into the other.)
+  auto step = [&](const Batch& now, const char* __restrict__ buf_now, Batch& next,
+                  char* __restrict__ buf_next) __attribute__((always_inline)) {
+    if (p + kStep < s.p1) load(next, p + kStep, buf_next);
+    wait(p + kStep);
+    work(now, p, buf_now);
+    read();
+    p += kStep;
+    return p < s.p1;
+  };
+  while (step(x, buf_x, y, buf_y) && step(y, buf_y, x, buf_x)) {
   }
 }
 
-// Many columns (prompts): 64 keys a wave stay in registers, the columns that see them
-// stream past through LDS, 32 a matrix product.  KW waves lie along the keys, 4 / KW
-// along the columns of a step.
-template <bool FP8, int KW>
-__device__ __forceinline__ void many_columns(const AttnWeightsArgs& a, const Seen& s, char* lds,
-                                             float* red, int& flag) {
-  constexpr int RW = 4 / KW, kCols = 32 * RW, kPieces = 2 * RW;
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const int half = lane >> 5, l32 = lane & 31;
-  const int kw = wave % KW, rw = wave / KW;
-  const int H = a.num_kv_heads, G = a.group;
-  const size_t head_bytes = kPage * kDim * (FP8 ? 1 : 2);
-  const uint16_t* q = a.q + s.row0 * a.q_stride + (size_t)s.g * G * kDim;
-  const float* lse = a.lse + (int64_t)s.row0 * a.num_q_heads + s.g * G;
-  const int last = (s.n - 1) / kPage;
-  const int turn = kCols / G, rest = kCols % G;  // rows and heads that a step moves on by
-  for (int p = s.p0; p < s.p1; p += 4 * KW) {
-    // keys 32 kt + l32 of the wave's 64
-    const int pk = p + 4 * kw;
-    u32x4 k[2][8];
-    float c[2][2];
-    int pid[2];
+__device__ __forceinline__ void lds_barrier() {  // for LDS that the waves wrote themselves
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Many columns (prompts, the last rows of one): 64 keys a wave and 256 a workgroup stay
+// in registers, the columns that see them stream past through LDS, 32 a matrix product
+// and a step.
+//
+// A product of 32 keys and 32 columns takes the matrix unit 256 cycles, and its 1024
+// exponentials take the vector unit as many.  So a product is issued between the
+// exponentials of the one before it, two a step in turn, with its own columns in
+// registers, those behind them in LDS and others on their way.  2000 rows behind 30K
+// tokens, 32 / 8 heads: 540 us, 0.94 PFLOP/s (the largest plain product reaches 1.19).
+// With 64 and 128 keys a workgroup (its waves then also beside each other along the
+// columns) 690 and 585, with eight waves 550 .. 680.
+template <bool FP8>
+struct Columns {
+  static constexpr int kCols = 32, kStep = kCols * 256;  // bytes of a step in LDS
+  const AttnWeightsArgs& a;
+  const Seen& s;
+  int tid, lane, wave, half, l32;
+  uint32_t magic, single;  // 2^32 / G, rounded up; G = 1: 0 and all bits
+  const uint16_t* q;
+  const float* lse;
+  int all;         // columns of the sequence
+  int front;       // the first row's position less tok_begin, in 32 bits
+  // the wave's keys: 32 t + l32 of 64
+  u32x4 k[2][8];
+  float c[2][2], key_scale[2];
+  int pid[2];
+  f32x16 acc[2];
+  int j0;          // index of its first key
+  // columns on their way to LDS
+  u32x4 piece[2];
+  float piece_lse;
+  bool even;                     // a step is a whole number of rows
+  uint32_t piece_at[2], lse_at;  // the lane's places in a step, in elements
+
+  __device__ __forceinline__ void begin() {
+    tid = threadIdx.x;
+    lane = tid & 63;
+    wave = uniform(tid >> 6);
+    half = lane >> 5;
+    l32 = lane & 31;
+    const int G = a.group;
+    magic = G == 1 ? 0 : 0xFFFFFFFFu / (uint32_t)G + 1;
+    single = G == 1 ? ~0u : 0;
+    q = a.q + s.row0 * a.q_stride + (size_t)s.g * G * kDim;
+    lse = a.lse + (int64_t)s.row0 * a.num_q_heads + s.g * G;
+    all = s.rows * G;
+    front = (int)max((int64_t)INT32_MIN, min((int64_t)INT32_MAX, s.first));
+    even = kCols % G == 0 && a.q_stride <= 1 << 24;
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      pid[kt] = a.page_ids[s.base + min(pk + 2 * kt + (l32 >> 4), last)];
-      const int id = (uint32_t)pid[kt] < (uint32_t)a.num_pages ? pid[kt] : 0;
-      const char* from = static_cast<const char*>(a.k_pool) +
-                         slice_of(id, s.g, H, a.num_pages, a.head_major) * head_bytes;
-      if constexpr (FP8) {
-        from += (l32 & 15) * kDim + 16 * half;
-        u32x4 x[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) x[u] = ld16(from + 32 * u);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) widen(x[u], k[kt][2 * u], k[kt][2 * u + 1]);
-        const float sc = a.scale_log2 * a.k_scale[(size_t)id * H + s.g];
-        c[kt][0] = __shfl(sc, 0);
-        c[kt][1] = __shfl(sc, 16);
-      } else {
-        from += 2 * ((l32 & 15) * kDim + 8 * half);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) k[kt][u] = ld16(from + 32 * u);
-        c[kt][0] = c[kt][1] = a.scale_log2;
-      }
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t col = 8 * wave + 4 * u + (lane >> 4);
+      piece_at[u] = col / (uint32_t)G * (uint32_t)a.q_stride + col % (uint32_t)G * kDim +
+                    8 * (lane & 15);
     }
-    // the first row that sees the first of the workgroup's keys, and its columns
-    const int64_t before = (int64_t)p * kPage - s.first;
-    const int i0 = (int)max((int64_t)0, min((int64_t)s.rows, before));
-    const int C = (s.rows - i0) * G, steps = (C + kCols - 1) / kCols;
-    // staged pieces: column 4 piece + lane / 16 of the step
-    int64_t off[kPieces];
-    int hh[kPieces];
+    lse_at = l32 / G * a.num_q_heads + l32 % G;
+  }
+
+  __device__ __forceinline__ int row_of(int col) const {  // col < 2^28
+    return (int)(__umulhi((uint32_t)col, magic) + ((uint32_t)col & single));
+  }
+  // The columns of step st: all of a sequence's workgroups begin at its last one, so
+  // that those of a KV head read the same ones at a time.
+  __device__ __forceinline__ int step_begin(int st) const { return all - (st + 1) * kCols; }
+  // Sends for them (the first one in place of those before it).  FAST: a step is a whole
+  // number of rows and this one is all there: a lane's places in it are the same as in
+  // all others, and a scalar address moves, where the others divide for every column.
+  // (No branch in any of these: the compiler would move exponentials past it.)
+  template <bool FAST>
+  __device__ __forceinline__ void send(int st) {
+    const int first = step_begin(st);
+    if constexpr (FAST) {
+      const int64_t row = row_of(first);
+      const uint16_t* from = q + row * a.q_stride;
 #pragma unroll
-    for (int u = 0; u < kPieces; ++u) {
-      const uint32_t col = 4 * (kPieces * wave + u) + (lane >> 4);
-      hh[u] = col % (uint32_t)G;
-      off[u] = (i0 + (int64_t)(col / (uint32_t)G)) * a.q_stride + hh[u] * kDim;
+      for (int u = 0; u < 2; ++u) piece[u] = ld16(from + piece_at[u]);
+      piece_lse = lse[row * a.num_q_heads + lse_at];
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int x = max(first + 8 * wave + 4 * u + (lane >> 4), 0), i = row_of(x);
+        piece[u] = ld16(q + i * a.q_stride + (x - i * a.group) * kDim + 8 * (lane & 15));
+        __builtin_amdgcn_sched_barrier(0);  // one address at a time: registers
+      }
+      const int x = max(first + l32, 0), i = row_of(x);
+      piece_lse = lse[(int64_t)i * a.num_q_heads + (x - i * a.group)];
     }
-    const int64_t off_last = (s.rows - 1) * a.q_stride + (G - 1) * kDim;
-    const int64_t off_turn = turn * a.q_stride + rest * kDim, off_wrap = a.q_stride - G * kDim;
-    int left = C;  // columns not staged yet
-    auto stage = [&](char* to) __attribute__((always_inline)) {
+  }
+  // A column's 16-byte chunks lie in the order of chunk ^ column % 16: the columns that
+  // an operand reads at once then cover all banks.  (Every wave writes all the lse: the
+  // same values.)
+  __device__ __forceinline__ void put(char* to, float* to_lse) {
 #pragma unroll
-      for (int u = 0; u < kPieces; ++u) {
-        const int col = 4 * (kPieces * wave + u) + (lane >> 4);
-        const int64_t o = col < left ? off[u] : off_last;
-        to_lds16(q + o + 8 * ((lane & 15) ^ (col & 15)), to + 1024 * (kPieces * wave + u));
-        off[u] += off_turn;
-        hh[u] += rest;
-        if (hh[u] >= G) {
-          hh[u] -= G;
-          off[u] += off_wrap;
-        }
-      }
-      left -= kCols;
-    };
-    // the lane's column of a product: 32 rw + l32 of the step
-    int col_left = C - (32 * rw + l32), ch = (32 * rw + l32) % G, ci = i0 + (32 * rw + l32) / G;
-    float next_lse = 0.0f;
-    int next_sees = -1;
-    auto column = [&]() __attribute__((always_inline)) {
-      next_sees = col_left > 0 ? reach(s, ci) : -1;
-      next_lse = col_left > 0 ? lse[(int64_t)ci * a.num_q_heads + ch] : neg_inf();
-      col_left -= kCols;
-      ci += turn;
-      ch += rest;
-      if (ch >= G) {
-        ch -= G;
-        ++ci;
-      }
-    };
-    f32x16 acc[2];
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[kt][i] = 0.0f;
-    const int j0 = pk * kPage;
-    if (steps > 0) {
-      stage(lds);
-      column();
+    for (int u = 0; u < 2; ++u) {
+      const int col = 8 * wave + 4 * u + (lane >> 4);
+      *reinterpret_cast<u32x4*>(to + col * 256 + (((lane & 15) ^ (col & 15)) << 4)) = piece[u];
     }
-    for (int st = 0; st < steps; ++st) {
-      char* now = lds + (st & 1) * (kCols * 256);
-      __syncthreads();  // this step's columns are there, and the other buffer is free
-      const float z = next_lse * kLog2e;
-      const int sees = has_softmax(next_lse) ? next_sees : -1;
-      if (st + 1 < steps) {
-        stage(lds + (~st & 1) * (kCols * 256));
-        column();
-      }
-      if (__ballot(sees >= j0) == 0) continue;
-      u32x4 b[8];
+    to_lse[l32] = piece_lse;
+  }
+  __device__ __forceinline__ u32x4 get(const char* from, int u) const {
+    const int chunk = FP8 ? 4 * (u >> 1) + 2 * half + (u & 1) : 2 * u + half;
+    return *reinterpret_cast<const u32x4*>(from + l32 * 256 + ((chunk ^ (l32 & 15)) << 4));
+  }
+  // The lse of the lane's column, in units of log2, and the last token that its row sees
+  // (-1: none).
+  __device__ __forceinline__ float column(const float* from_lse) const {
+    return from_lse[l32] * kLog2e;
+  }
+  __device__ __forceinline__ int last_seen(int st, float z) const {
+    const int x = step_begin(st) + l32;
+    return x >= 0 && has_softmax(z) ? max(-1, __builtin_elementwise_add_sat(front, row_of(x))) : -1;
+  }
+  // Whether every column of the steps up to st sees all of the wave's keys.
+  __device__ __forceinline__ bool sees_all(int st) const {
+    const int at = step_begin(st);
+    return at >= 0 && reach(s, row_of(at)) - 63 >= j0;
+  }
+
+  // Keys t of the wave's from `page` on: bf16 straight into their operand, fp8 codes into
+  // half of it, to be widened when they are there.
+  template <int t>
+  __device__ __forceinline__ void load_keys(int page) {
+    const int H = a.num_kv_heads, last = (s.n - 1) / kPage;
+    const size_t head_bytes = kPage * kDim * (FP8 ? 1 : 2);
+    pid[t] = a.page_ids[s.base + min(page + 2 * t + (l32 >> 4), last)];
+    const int id = (uint32_t)pid[t] < (uint32_t)a.num_pages ? pid[t] : 0;
+    const char* from = static_cast<const char*>(a.k_pool) +
+                       slice_of(id, s.g, H, a.num_pages, a.head_major) * head_bytes +
+                       (FP8 ? (l32 & 15) * kDim + 16 * half : 2 * ((l32 & 15) * kDim + 8 * half));
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int chunk = FP8 ? 4 * (u >> 1) + 2 * half + (u & 1) : 2 * u + half;
-        b[u] = *reinterpret_cast<const u32x4*>(now + (32 * rw + l32) * 256 +
-                                               ((chunk ^ (l32 & 15)) << 4));
-      }
-      f32x16 d[2];
+    for (int u = 0; u < (FP8 ? 4 : 8); ++u) k[t][u] = ld16(from + 32 * u);
+    key_scale[t] = FP8 ? a.k_scale[(size_t)id * H + s.g] : 1.0f;
+  }
+  template <int t>
+  __device__ __forceinline__ void take_keys() {
+    if constexpr (FP8) {
+      u32x4 x[4];
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
+      for (int u = 0; u < 4; ++u) x[u] = k[t][u];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) d[kt][i] = 0.0f;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) d[kt] = mfma32(k[kt][u], b[u], d[kt]);
-      }
-      if (__ballot(sees - 63 < j0) == 0) {
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            acc[kt][i] += exp2_fast(__builtin_fmaf(d[kt][i], c[kt][i >> 3], -z));
-      } else {
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int j = j0 + 32 * kt + 8 * (i >> 2) + 4 * half + (i & 3);
-            const float e = exp2_fast(__builtin_fmaf(d[kt][i], c[kt][i >> 3], -z));
-            acc[kt][i] += j <= sees ? e : 0.0f;
-          }
-      }
+      for (int u = 0; u < 4; ++u) widen(x[u], k[t][2 * u], k[t][2 * u + 1]);
+      const float sc = a.scale_log2 * key_scale[t];
+      c[t][0] = __shfl(sc, 0);
+      c[t][1] = __shfl(sc, 16);
+    } else {
+      c[t][0] = c[t][1] = a.scale_log2;
     }
-    // The sums over the 32 columns of a half wave: lane l32 ends with that of value
-    // 16 kt + i = l32.  In every turn a lane gives half of its values away.
+  }
+
+  // The product of keys kk and the columns b, between the exponentials of `was`, that of
+  // keys T and the columns of step st, which see some of them (MASK) or all.  READ: each
+  // operand makes room for the next step's, in `from`.
+  template <int T, bool READ, bool MASK>
+  __device__ __forceinline__ void turn(const u32x4 (&kk)[8], u32x4 (&b)[8], f32x16& d,
+                                       const f32x16& was, float z, int st, const char* from) {
+    const int up_to = MASK ? last_seen(st, z) - (j0 + 32 * T + 4 * half) : 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) d[i] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      d = mfma32(kk[u], b[u], d);
+      if constexpr (READ) b[u] = get(from, u);
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        const int i = 2 * u + v;
+        float e = exp2_fast(__builtin_fmaf(was[i], c[T][i >> 3], -z));
+        if (MASK) e = 8 * (i >> 2) + (i & 3) <= up_to ? e : 0.0f;
+        acc[T][i] += e;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // The exponentials of the last product, of keys 1.
+  __device__ __forceinline__ void last_turn(const f32x16& was, float z, int st) {
+    const int up_to = last_seen(st, z) - (j0 + 32 + 4 * half);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float e = exp2_fast(__builtin_fmaf(was[i], c[1][i >> 3], -z));
+      acc[1][i] += 8 * (i >> 2) + (i & 3) <= up_to ? e : 0.0f;
+    }
+  }
+  __device__ __forceinline__ void first_product(const char* from, u32x4 (&b)[8], f32x16& d) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) b[u] = get(from, u);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[t][i] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) d[i] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) d = mfma32(k[0][u], b[u], d);
+  }
+
+  // The sums over the 32 columns of a half wave: lane l32 ends with that of value
+  // 16 t + i = l32.  In every turn a lane gives half of its values away.
+  template <int M>
+  __device__ __forceinline__ void halve(float (&v)[32]) const {
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      const float give = l32 & M ? v[i] : v[i + M], keep = l32 & M ? v[i + M] : v[i];
+      v[i] = keep + __shfl_xor(give, M);
+    }
+    if constexpr (M > 1) halve<M / 2>(v);
+  }
+  __device__ __forceinline__ float reduce() const {
     float v[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = acc[i >> 4][i & 15];
-#pragma unroll
-    for (int m = 16; m >= 1; m >>= 1)
-#pragma unroll
-      for (int i = 0; i < m; ++i) {
-        const float give = lane & m ? v[i] : v[i + m], keep = lane & m ? v[i + m] : v[i];
-        v[i] = keep + __shfl_xor(give, m);
-      }
-    float sum = v[0];
-    const int kt = l32 >> 4, i = l32 & 15;
-    const int m = 32 * kt + 8 * (i >> 2) + 4 * half + (i & 3);  // of the wave's 64 keys
-    const int id0 = __shfl(pid[0], m & 16), id1 = __shfl(pid[1], m & 16);
-    const int id = kt ? id1 : id0, j = j0 + m;
-    float* at = a.weights + ((size_t)id * H + s.g) * kPage + (m & 15);
-    const bool mine = rw == 0 && j < s.n && pk + (m >> 4) < s.p1;
-    const float old = mine && a.decay != 0.0f && (uint32_t)id < (uint32_t)a.num_pages ? *at : 0.0f;
-    if constexpr (RW > 1) {
-      red[64 * wave + m] = sum;
-      __syncthreads();
-      sum = 0.0f;
-#pragma unroll
-      for (int w = 0; w < RW; ++w) sum += red[64 * (kw + KW * w) + m];
-    }
-    if (mine) {
-      if ((uint32_t)id >= (uint32_t)a.num_pages)
-        flag |= KF_EFLAG_BAD_PAGE;
-      else
-        *at = j < s.first && a.decay != 0.0f ? __builtin_fmaf(a.decay, old, sum) : sum;
-    }
-    __syncthreads();  // (the next keys' first columns go where this step's may still be read)
+    halve<16>(v);
+    return v[0];
   }
-}
+  // Which of the wave's 64 keys that is.
+  __device__ __forceinline__ int key_of_lane() const {
+    return 32 * (l32 >> 4) + 8 * ((l32 >> 2) & 3) + 4 * half + (l32 & 3);
+  }
 
-template <bool FP8, int KW>
-__global__ __launch_bounds__(256, 2) void attn_weights_kernel(AttnWeightsArgs a) {
-  constexpr int kCols = 32 * (4 / KW);
-  __shared__ __align__(16) char lds[2 * kCols * 256];
-  __shared__ float red[256];
+  // The sums of the wave's keys, whose page ids id0 and id1 hold as pid does, into their
+  // tokens' weights.
+  __device__ __forceinline__ void write(float sum, int id0, int id1, int& flag) {
+    const int m = key_of_lane(), j = j0 + m;
+    const int x = __shfl(id0, m & 16), y = __shfl(id1, m & 16), id = m & 32 ? y : x;
+    if (j0 / kPage + (m >> 4) >= s.p1 || j >= s.n) return;
+    if ((uint32_t)id >= (uint32_t)a.num_pages) {
+      flag |= KF_EFLAG_BAD_PAGE;
+      return;
+    }
+    float* at = a.weights + ((size_t)id * a.num_kv_heads + s.g) * kPage + (m & 15);
+    *at = j < s.first && a.decay != 0.0f ? __builtin_fmaf(a.decay, *at, sum) : sum;
+  }
+
+  // Columns that all fit in LDS (the last rows of a prompt): they are put there once, and
+  // each wave takes its share of the pages, four at a time, without a barrier.  The last
+  // 32 rows of 8 prompts of 2K .. 32K tokens, 64 / 8 heads, fp8: 74 us, 84 with the
+  // columns put there anew for every 256 keys.
+  __device__ __forceinline__ void run_resident(char* lds_x, char* lds_y, float* lds_lse,
+                                               int& flag) {
+    begin();
+    const int steps = (all + kCols - 1) / kCols;
+    constexpr int kInX = kHeldColumns / 2 / kCols;  // steps in lds_x
+    auto place = [&](int st) {
+      return st < kInX ? lds_x + st * kStep : lds_y + (st - kInX) * kStep;
+    };
+    int p = s.p0 + 4 * wave;
+    if (p < s.p1) {
+      load_keys<0>(p);
+      load_keys<1>(p);
+    }
+    for (int st = 0; st < steps; ++st) {
+      send<false>(st);
+      put(place(st), lds_lse + st * kCols);
+    }
+    lds_barrier();
+    u32x4 b[8];
+    f32x16 d0, d1;
+    for (; p < s.p1; p += 16) {
+      j0 = p * kPage;
+      take_keys<0>();
+      take_keys<1>();
+      const int id0 = pid[0], id1 = pid[1];
+      first_product(lds_x, b, d0);
+      int st = 0;
+      auto body = [&](auto mask) __attribute__((always_inline)) {
+        constexpr bool MASK = decltype(mask)::value;
+        const float z = column(lds_lse + st * kCols);
+        turn<0, true, MASK>(k[1], b, d1, d0, z, st, place(st + 1));
+        turn<1, false, MASK>(k[0], b, d0, d1, z, st, nullptr);
+        ++st;
+      };
+      auto whole = [&]() {
+        return sees_all(st) && __ballot(!has_softmax(column(lds_lse + st * kCols))) == 0;
+      };
+      while (st + 1 < steps) {  // (two loops: see run)
+        while (st + 1 < steps && whole()) body(std::false_type{});
+        while (st + 1 < steps && !whole()) body(std::true_type{});
+      }
+      // the last step: no product of other columns follows, and the next keys are sent for
+      // where these have been used
+      const float z = column(lds_lse + st * kCols);
+      turn<0, false, true>(k[1], b, d1, d0, z, st, nullptr);
+      if (p + 16 < s.p1) {
+        load_keys<0>(p + 16);
+        load_keys<1>(p + 16);
+      }
+      last_turn(d1, z, st);
+      write(reduce(), id0, id1, flag);
+    }
+  }
+
+  // Columns beyond that.  segment: which part of the steps, where several workgroups
+  // share the columns; their sums then go to `sums` (256 of a workgroup).
+  __device__ __forceinline__ void run(char* lds, float* lds_lse, int segment, float* sums,
+                                      int& flag) {
+    begin();
+    char* buf[2] = {lds, lds + kStep};
+    float* buf_lse[2] = {lds_lse, lds_lse + kCols};
+    const int most = (all + kCols - 1) / kCols;
+    const int per = a.segments == 1 ? most : 2 * ((most + 2 * a.segments - 1) / (2 * a.segments));
+    for (int p = s.p0; p < s.p1; p += 16) {
+      // the first row that sees the first of the workgroup's keys, and its columns
+      const int64_t before = (int64_t)p * kPage - s.first;
+      const int first = (int)max((int64_t)0, min((int64_t)s.rows, before)) * a.group;
+      const int steps = min((all - first + kCols - 1) / kCols, (segment + 1) * per);
+      const int from = segment * per;
+      j0 = (p + 4 * wave) * kPage;
+      float sum = 0.0f;
+      if (from < steps) {
+        send<false>(from);
+        load_keys<0>(p + 4 * wave);
+        load_keys<1>(p + 4 * wave);
+        take_keys<0>();
+        take_keys<1>();
+        // Step st works on columns in b, which it replaces by those of step st + 1 from
+        // LDS; those of st + 2 are put there, and those of st + 3 sent for.
+        u32x4 b[8];
+        f32x16 d0, d1;
+        put(buf[0], buf_lse[0]);
+        send<false>(from + 1);
+        lds_barrier();
+        first_product(buf[0], b, d0);
+        float z = column(buf_lse[0]), next_z = 0.0f;
+        put(buf[1], buf_lse[1]);
+        send<false>(from + 2);
+        // (the products behind the last step's are not used)
+        auto step = [&](auto mode, auto odd, int st) __attribute__((always_inline)) {
+          constexpr bool MASK = decltype(mode)::value == 0, FAST = decltype(mode)::value == 2;
+          constexpr int S = decltype(odd)::value, R = S ^ 1;
+          const float z2 = column(buf_lse[R]);
+          put(buf[S], buf_lse[S]);
+          send<FAST>(st + 3);
+          turn<0, true, MASK>(k[1], b, d1, d0, z, st, buf[R]);
+          turn<1, false, MASK>(k[0], b, d0, d1, z, st, nullptr);
+          z = z2;
+          lds_barrier();  // the columns that the next step reads are there, these are free
+        };
+        // Two steps at a time, and loops of their own for steps that some column does not
+        // see whole (or none of: it lies before the first one, or its row has no softmax)
+        // and for all others: a branch in the loop has the sums copied back and forth.
+        lds_barrier();
+        auto whole = [&](int st) {
+          if (!sees_all(st + 1)) return false;
+          next_z = column(buf_lse[1]);
+          return __ballot(!has_softmax(z) || !has_softmax(next_z)) == 0;
+        };
+        auto fast = [&](int st) { return even && step_begin(st + 4) >= 0; };
+        auto body = [&](auto mode, int& st) __attribute__((always_inline)) {
+          step(mode, std::integral_constant<int, 0>{}, st);
+          step(mode, std::integral_constant<int, 1>{}, st + 1);
+          st += 2;
+        };
+        for (int st = from; st < steps;) {
+          while (st < steps && fast(st) && whole(st)) body(std::integral_constant<int, 2>{}, st);
+          while (st < steps && !fast(st) && whole(st)) body(std::integral_constant<int, 1>{}, st);
+          while (st < steps && !whole(st)) body(std::integral_constant<int, 0>{}, st);
+        }
+        sum = reduce();
+      } else if (!sums) {  // (nothing sees these keys; their pages count all the same)
+        load_keys<0>(p + 4 * wave);
+        load_keys<1>(p + 4 * wave);
+      }
+      if (sums)
+        sums[64 * wave + key_of_lane()] = sum;
+      else
+        write(sum, pid[0], pid[1], flag);
+      lds_barrier();  // the next keys' columns go where these may still be read
+    }
+  }
+};
+
+// The route of a workgroup and the pages that are its own; whether there are any.
+__device__ __forceinline__ bool find_keys(const AttnWeightsArgs& a, Seen& s) {
   const int H = a.num_kv_heads, r = blockIdx.y;
-  const int g = blockIdx.x % H, chunk = blockIdx.x / H;
+  const int chunk = (int)(blockIdx.x / H);
   const auto* rp = fixed(reinterpret_cast<const int32_t*>(a.routes)) + 6 * (int64_t)r;
-  const int seq = rp[0], tb = rp[2], te = rp[3], base = rp[4], cap = rp[5];
-  Seen s;
+  const int seq = rp[0], tb = rp[2], te = rp[3], cap = rp[5];
+  s.g = blockIdx.x % H;
+  s.base = rp[4];
   bool bad = seq < 0 || seq >= a.num_seqs;
   if (!bad) {
     s.row0 = fixed(a.seq_row_begin)[seq];
     const int end = fixed(a.seq_row_begin)[seq + 1];
+    s.first = (int64_t)fixed(a.first_pos)[seq] - tb;
     s.rows = end - s.row0;
     bad = s.row0 < 0 || end < s.row0 || end > a.num_rows;
-    if (!bad && s.rows == 0) return;  // not looked at
-    bad = bad || !route_row_ok(tb, te, base, cap, a.max_pages_per_route, a.num_page_ids);
+    if (!bad && s.rows == 0) return false;  // not looked at
+    bad = bad || !route_row_ok(tb, te, s.base, cap, a.max_pages_per_route, a.num_page_ids);
   }
   if (bad) {
-    if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
-    return;
+    if (blockIdx.x == 0 && blockIdx.z == 0 && threadIdx.x == 0)
+      atomicOr(a.err_flags, KF_EFLAG_BAD_ROUTE);
+    return false;
   }
-  s.g = g;
   s.n = te - tb;
-  s.base = base;
-  s.first = (int64_t)fixed(a.first_pos)[seq] - tb;
   const int pages = (int)(((int64_t)s.n + kPage - 1) / kPage);
-  if ((int64_t)chunk * a.chunk_pages >= pages) return;
+  if ((int64_t)chunk * a.chunk_pages >= pages) return false;
   s.p0 = chunk * a.chunk_pages;
   s.p1 = (int)min((int64_t)pages, (int64_t)s.p0 + a.chunk_pages);
-  int flag = 0;
+  return true;
+}
+// The sums of a workgroup's keys over segment `segment` of the columns.
+__device__ __forceinline__ float* sums_of(const AttnWeightsArgs& a, int segment) {
+  return a.sums + 256 * (((size_t)segment * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x);
+}
+
+template <bool FP8>
+__global__ __launch_bounds__(256, 2) void attn_weights_kernel(AttnWeightsArgs a) {
+  constexpr int kHalf = kHeldColumns * 128;
+  __shared__ __align__(16) char lds_x[kHalf], lds_y[kHalf];
+  __shared__ float lds_lse[kHeldColumns];
+  Seen s;
+  if (!find_keys(a, s)) return;
+  const int segment = blockIdx.z;
   const int64_t C = (int64_t)s.rows * a.group;
-  if (C <= 16)
-    few_columns<FP8, 1>(a, s, flag);
-  else if (C <= kFewColumns)
-    few_columns<FP8, kFewColumns / 16>(a, s, flag);
-  else
-    many_columns<FP8, KW>(a, s, lds, red, flag);
+  if (segment > 0 && C <= kHeldColumns) return;
+  int flag = 0;
+  if (C <= 16) {
+    few_columns<FP8, 1>(a, s, lds_x, lds_y, flag);
+  } else if (C <= kFewColumns) {
+    few_columns<FP8, kFewColumns / 16>(a, s, lds_x, lds_y, flag);
+  } else {
+    Columns<FP8> x{a, s};
+    if (C <= kHeldColumns)
+      x.run_resident(lds_x, lds_y, lds_lse, flag);
+    else
+      x.run(lds_x, lds_lse, segment, a.segments > 1 ? sums_of(a, segment) : nullptr, flag);
+  }
   if (__ballot(flag != 0) && (threadIdx.x & 63) == 0) atomicOr(a.err_flags, KF_EFLAG_BAD_PAGE);
+}
+
+// The segments' sums, in order, into the tokens' weights: a thread a token.
+__global__ __launch_bounds__(256) void attn_weights_join_kernel(AttnWeightsArgs a) {
+  Seen s;
+  if (!find_keys(a, s)) return;
+  const int j = s.p0 * kPage + threadIdx.x;
+  if ((int64_t)s.rows * a.group <= kHeldColumns || j >= s.n) return;
+  const int id = a.page_ids[s.base + j / kPage];
+  float x[kMaxSegments];
+#pragma unroll
+  for (int i = 0; i < kMaxSegments; ++i)
+    x[i] = i < a.segments ? sums_of(a, i)[threadIdx.x] : 0.0f;
+  if ((uint32_t)id >= (uint32_t)a.num_pages) {
+    atomicOr(a.err_flags, KF_EFLAG_BAD_PAGE);
+    return;
+  }
+  float sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kMaxSegments; ++i) sum += x[i];
+  float* at = a.weights + ((size_t)id * a.num_kv_heads + s.g) * kPage + j % kPage;
+  *at = j < s.first && a.decay != 0.0f ? __builtin_fmaf(a.decay, *at, sum) : sum;
 }
 
 // -------------------------------------------------------------------- evict
@@ -1005,19 +1278,14 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
 }  // namespace
 
 hipError_t launch_attn_weights(const AttnWeightsArgs& a, bool fp8, hipStream_t stream) {
-  const dim3 grid((uint32_t)a.chunks * a.num_kv_heads, a.num_routes);
-  if (fp8 && a.key_waves == 1)
-    attn_weights_kernel<true, 1><<<grid, 256, 0, stream>>>(a);
-  else if (fp8 && a.key_waves == 2)
-    attn_weights_kernel<true, 2><<<grid, 256, 0, stream>>>(a);
-  else if (fp8)
-    attn_weights_kernel<true, 4><<<grid, 256, 0, stream>>>(a);
-  else if (a.key_waves == 1)
-    attn_weights_kernel<false, 1><<<grid, 256, 0, stream>>>(a);
-  else if (a.key_waves == 2)
-    attn_weights_kernel<false, 2><<<grid, 256, 0, stream>>>(a);
+  const dim3 grid((uint32_t)a.chunks * a.num_kv_heads, a.num_routes, a.segments);
+  if (fp8)
+    attn_weights_kernel<true><<<grid, 256, 0, stream>>>(a);
   else
-    attn_weights_kernel<false, 4><<<grid, 256, 0, stream>>>(a);
+    attn_weights_kernel<false><<<grid, 256, 0, stream>>>(a);
+  const hipError_t st = hipGetLastError();
+  if (st != hipSuccess || a.segments == 1) return st;
+  attn_weights_join_kernel<<<dim3(grid.x, grid.y), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 

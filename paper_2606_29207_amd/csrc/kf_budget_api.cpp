@@ -22,15 +22,39 @@ int64_t div_up(int64_t x, int64_t y) { return (x + y - 1) / y; }
 // A page and a slot of it share 31 bits of the list of what stays.
 bool pages_fit(const kf_shape* s) { return s->num_pages <= INT32_MAX / KF_PAGE_SIZE; }
 
+// The columns of a launch, and a workgroup per route and KV head.
+bool weights_fit(const kf_shape* s, int32_t num_rows, int32_t num_routes) {
+  return num_routes <= kf::kMaxLaunchRoutes &&
+         (int64_t)num_rows * (s->num_q_heads / s->num_kv_heads) <= (1 << 28) - 256 &&
+         (int64_t)num_routes * s->num_kv_heads <= kf::kMaxBudgetWgs;
+}
+
 }  // namespace
 
 extern "C" {
+
+size_t kf_attn_weights_workspace_bytes(const kf_shape* shape, int32_t num_rows, int32_t num_routes,
+                                       int32_t max_pages_per_route) {
+  if (kf::check_shape(shape) != KF_OK || num_rows < 0 || num_routes < 0 ||
+      max_pages_per_route < 0 || !weights_fit(shape, num_rows, num_routes))
+    return 0;
+  kf::AttnWeightsArgs a{};
+  a.num_rows = num_rows;
+  a.num_seqs = shape->num_seqs;
+  a.num_kv_heads = shape->num_kv_heads;
+  a.group = shape->num_q_heads / shape->num_kv_heads;
+  a.num_routes = std::max(1, num_routes);
+  a.max_pages_per_route = max_pages_per_route;
+  kf::plan_attn_weights(a, 2 * (int64_t)kf::cu_count());
+  return std::max<size_t>(256, kf::attn_weights_bytes(a));
+}
 
 int kf_attn_weights(const kf_shape* shape, const void* q, int32_t num_rows, int64_t q_stride,
                     const float* lse, const int32_t* seq_row_begin, const int32_t* first_pos,
                     const void* k_pool, const float* k_scale, const kf_route* routes,
                     int32_t num_routes, int32_t max_pages_per_route, const int32_t* page_ids,
-                    float decay, float* weights, int32_t* err_flags, void* stream) {
+                    float decay, float* weights, void* workspace, size_t workspace_bytes,
+                    int32_t* err_flags, void* stream) {
   const int st = kf::check_shape(shape);
   if (st != KF_OK) return st;
   if (num_rows < 0 || num_routes < 0 || max_pages_per_route < 0 || !isfinite(decay))
@@ -46,9 +70,7 @@ int kf_attn_weights(const kf_shape* shape, const void* q, int32_t num_rows, int6
   for (const void* p : p4)
     if (p && !aligned(p, 4)) return KF_ERR_INVALID_ARG;
   const int32_t H = shape->num_kv_heads, group = shape->num_q_heads / H;
-  if (num_routes > kf::kMaxLaunchRoutes || (int64_t)num_rows * group > INT32_MAX - 256 ||
-      (int64_t)num_routes * H > kf::kMaxBudgetWgs)
-    return KF_ERR_UNSUPPORTED;
+  if (!weights_fit(shape, num_rows, num_routes)) return KF_ERR_UNSUPPORTED;
 
   kf::AttnWeightsArgs a{};
   a.q = static_cast<const uint16_t*>(q);
@@ -75,6 +97,10 @@ int kf_attn_weights(const kf_shape* shape, const void* q, int32_t num_rows, int6
   a.num_page_ids = shape->num_page_ids;
   a.head_major = shape->kv_layout == KF_KV_HEAD_MAJOR;
   kf::plan_attn_weights(a, 2 * (int64_t)kf::cu_count());
+  const size_t need = kf::attn_weights_bytes(a);
+  if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
+    return KF_ERR_WORKSPACE;
+  a.sums = static_cast<float*>(workspace);
   return kf::launch_attn_weights(a, fp8_pool(shape), as_stream(stream)) == hipSuccess ? KF_OK
                                                                                      : KF_ERR_HIP;
 }
@@ -165,23 +191,26 @@ EvictLayout evict_layout(const kf_shape& s, int32_t max_keep) {
   return l;
 }
 
-// How a launch's keys are dealt out, by what the host knows: the pages that the table
-// reserves, and the (row, head) pairs of a sequence on the mean.
+// By the (row, head) pairs of a sequence on the mean, and the workgroups of 256 keys
+// that the table has room for.
 void plan_attn_weights(AttnWeightsArgs& a, int64_t slots) {
   const int64_t most = std::max(1, a.max_pages_per_route);
-  const int64_t pages = std::max<int64_t>(1, std::min((int64_t)a.num_page_ids, a.num_routes * most)) *
-                        a.num_kv_heads;
-  int64_t chunk;
-  if ((int64_t)a.num_rows * a.group <= (int64_t)kFewColumns * a.num_seqs) {
-    a.key_waves = 4;
-    chunk = std::min<int64_t>(128, std::max<int64_t>(16, pages / (4 * slots) / 16 * 16));
-  } else {
-    a.key_waves = pages >= 32 * slots ? 4 : pages >= 16 * slots ? 2 : 1;
-    chunk = 4 * a.key_waves;
-  }
+  const int64_t columns = (int64_t)a.num_rows * a.group / std::max(1, a.num_seqs);
+  // A workgroup's pages: 16 (one decode row over 32K tokens, 16 sequences, 190 us; 8 and
+  // 32 212 and 195, 64 204, 128 222, 256 195), where the columns stay in LDS twice as many
+  // (74 us, 80 with 16, 77 with 64).
+  int64_t chunk = columns > kFewColumns && columns <= kHeldColumns ? 32 : 16;
   while (div_up(most, chunk) * a.num_kv_heads * a.num_routes > kMaxBudgetWgs) chunk *= 2;
   a.chunk_pages = (int32_t)std::min<int64_t>(chunk, INT32_MAX / 2);
   a.chunks = (int32_t)div_up(most, a.chunk_pages);
+  // A prompt's first keys are seen by all of its rows, its last ones by a few: in one
+  // workgroup each, the first ones would end last.
+  const int64_t wgs = (int64_t)a.chunks * a.num_kv_heads * a.num_routes;
+  const int64_t steps = (int64_t)a.num_rows * a.group / 32;
+  a.segments = 1;
+  if (columns > kHeldColumns && chunk == 16 && wgs < kSegmentWgs * slots)
+    a.segments = (int32_t)std::max<int64_t>(
+        1, std::min<int64_t>({kMaxSegments, kSegmentWgs * slots / wgs, steps / kSegmentSteps}));
 }
 
 }  // namespace kf

@@ -43,8 +43,8 @@ EXPORTS = ("kf_kv_append", "kf_partial_attn_workspace_bytes", "kf_partial_attn_p
            "kf_merge_partials", "kf_decode_step", "kf_decode_step_no_alloc",
            "kf_kv_append_rows_workspace_bytes", "kf_kv_append_rows",
            "kf_rows_attn_workspace_bytes", "kf_prompt_attn", "kf_window_attn", "kf_tree_attn",
-           "kf_attn_weights", "kf_kv_evict_workspace_bytes", "kf_kv_evict", "kf_debug_gather",
-           "kf_status_str", "kf_version")
+           "kf_attn_weights_workspace_bytes", "kf_attn_weights", "kf_kv_evict_workspace_bytes",
+           "kf_kv_evict", "kf_debug_gather", "kf_status_str", "kf_version")
 
 
 class KFError(RuntimeError):
@@ -116,8 +116,10 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.kf_tree_attn.argtypes = [sp, vp, i32, i64, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, i32, i32,
                                  vp, vp, vp, vp, vp, sz, vp, vp]
     lib.kf_tree_attn.restype = ctypes.c_int
+    lib.kf_attn_weights_workspace_bytes.argtypes = [sp, i32, i32, i32]
+    lib.kf_attn_weights_workspace_bytes.restype = sz
     lib.kf_attn_weights.argtypes = [sp, vp, i32, i64, vp, vp, vp, vp, vp, vp, i32, i32, vp,
-                                    ctypes.c_float, vp, vp, vp]
+                                    ctypes.c_float, vp, vp, sz, vp, vp]
     lib.kf_attn_weights.restype = ctypes.c_int
     lib.kf_kv_evict_workspace_bytes.argtypes = [sp, i32]
     lib.kf_kv_evict_workspace_bytes.restype = sz
@@ -712,12 +714,19 @@ def alloc_weights(shape: Shape, device="cuda") -> torch.Tensor:
     return torch.zeros((shape.num_pages, shape.num_kv_heads, PAGE_SIZE), device=device)
 
 
+def attn_weights_workspace_bytes(shape: Shape, num_rows: int, num_routes: int,
+                                 max_pages_per_route: int) -> int:
+    return int(load().kf_attn_weights_workspace_bytes(ctypes.byref(shape), int(num_rows),
+                                                      int(num_routes), int(max_pages_per_route)))
+
+
 def bind_attn_weights(shape: Shape, q, lse, first_pos, k_pool, routes, max_pages_per_route,
                       page_ids, seq_row_begin, decay, weights, err_flags,
-                      k_scale=None) -> BoundCall:
+                      k_scale=None, workspace=None) -> BoundCall:
     """kf_attn_weights bound to its buffers; call it as (stream).  q bf16 [N, Hq, 128],
     lse float32 [N, Hq]: packed rows and what their attention returned; first_pos
-    int32 [B], seq_row_begin int32 [B + 1]; weights float32 [P, Hkv, 16] (updated)."""
+    int32 [B], seq_row_begin int32 [B + 1]; weights float32 [P, Hkv, 16] (updated).
+    workspace=None allocates what the call needs (4 MB at most)."""
     H = shape.num_kv_heads
     stride = _rows(q, "q", shape.num_q_heads)
     N = q.shape[0]
@@ -734,23 +743,34 @@ def bind_attn_weights(shape: Shape, q, lse, first_pos, k_pool, routes, max_pages
     _check_tables(shape, k_pool, k_pool, routes, page_ids)
     if shape.kv_dtype == KV_FP8_E4M3:
         _check_scales(shape, k_scale, k_scale)
+    if workspace is None:
+        n = attn_weights_workspace_bytes(shape, N, routes.shape[0], max_pages_per_route)
+        if n == 0:
+            raise KFError("invalid workspace request")
+        workspace = torch.empty(n, dtype=torch.uint8, device=k_pool.device)
+    _dev(workspace, "workspace")
     _same_device(k_pool, ((q, "q"), (lse, "lse"), (first_pos, "first_pos"), (routes, "routes"),
                           (page_ids, "page_ids"), (seq_row_begin, "seq_row_begin"),
-                          (weights, "weights"), (err_flags, "err_flags"), (k_scale, "k_scale")))
+                          (weights, "weights"), (err_flags, "err_flags"), (k_scale, "k_scale"),
+                          (workspace, "workspace")))
     sh = _copy_shape(shape)
     args = (ctypes.byref(sh), _ptr(q), N, stride, _ptr(lse), _ptr(seq_row_begin), _ptr(first_pos),
             _ptr(k_pool), _ptr(k_scale), _ptr(routes), routes.shape[0], int(max_pages_per_route),
-            _ptr(page_ids), float(decay), _ptr(weights), _ptr(err_flags))
+            _ptr(page_ids), float(decay), _ptr(weights), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _ptr(err_flags))
     keep = (sh, q, lse, seq_row_begin, first_pos, k_pool, k_scale, routes, page_ids, weights,
-            err_flags)
+            workspace, err_flags)
     return BoundCall(load().kf_attn_weights, "kf_attn_weights", args, keep, k_pool.device.index)
 
 
 def attn_weights(shape: Shape, q, lse, first_pos, k_pool, routes, max_pages_per_route, page_ids,
-                 seq_row_begin, decay, weights, err_flags, k_scale=None, stream=None):
-    """kf_attn_weights: the attention weight of every token, accumulated."""
+                 seq_row_begin, decay, weights, err_flags, k_scale=None, workspace=None,
+                 stream=None):
+    """kf_attn_weights: the attention weight of every token, accumulated.  On another
+    stream than the current one give a workspace of your own."""
+    _need(workspace is not None or stream is None, "a workspace is needed with a stream")
     bind_attn_weights(shape, q, lse, first_pos, k_pool, routes, max_pages_per_route, page_ids,
-                      seq_row_begin, decay, weights, err_flags, k_scale)(stream)
+                      seq_row_begin, decay, weights, err_flags, k_scale, workspace)(stream)
 
 
 def kv_evict_workspace_bytes(shape: Shape, max_keep: int) -> int:
