@@ -852,8 +852,9 @@ struct Walk {
   int base, n;    // its first page id's index, its tokens that the row tile sees (with a
                   // window: those before the tile's last row, in its window or not)
   int tb;         // its first token
-  int j, tiles;   // next tile of the route, its tiles
-  int from, to;   // with a window: the tile behind the sinks, where the window begins
+  int j, tiles;   // next tile of the route, its tiles (with a window and no JUMP: those up to
+                  // the end of its sinks, then all of them)
+  int from, to;   // JUMP: the tile behind the sinks, where the window begins
   int pid[2];     // page ids of that tile (sent for a step ahead, awaited at its barrier)
 };
 
@@ -921,24 +922,47 @@ __device__ __forceinline__ int sight_tiles(const Sight& s, int begin, int end) {
   return tiles - to + from;
 }
 
+// With a window, the walk gets from a route's sinks to its window either by a look at
+// every tile (JUMP) or as it gets to another route, from the route's row.  bf16's kernel
+// has the scalar registers for the former, fp8's has not: 16K-token prompts, window 2048,
+// 609 us and 625; fp8 chunks, window 8000, 819 and 740.
 // Enters the route begin .. end - 1 at the k-th of its visible tiles.
-template <bool WINDOW>
+template <bool WINDOW, bool JUMP>
 __device__ __forceinline__ void walk_route(Walk& w, const Sight& s, int begin, int end, int base,
                                            int k) {
-  route_sight<WINDOW>(s, begin, end, w.n, w.from, w.to, w.tiles);
+  int from, to;
+  route_sight<WINDOW>(s, begin, end, w.n, from, to, w.tiles);
   w.tb = begin;
   w.base = base;
-  w.j = WINDOW && k >= w.from ? k - w.from + w.to : k;
+  w.j = k;
+  if (WINDOW && k >= from)
+    w.j = k - from + to;
+  else if (WINDOW && !JUMP && from < to)
+    w.tiles = from;
+  if (JUMP) {
+    w.from = from;
+    w.to = to;
+  }
 }
 
 // Behind a route's last tile: the next route that has any.
-template <bool WINDOW>
+template <bool WINDOW, bool JUMP>
 __device__ __forceinline__ void walk_on(const RowsArgs& a, Walk& w, const Sight& s) {
   while (w.j >= w.tiles && w.r < w.r_end) {
+    if (WINDOW && !JUMP) {  // from the sinks to the window of the same route
+      const auto* rp = fixed(reinterpret_cast<const int32_t*>(a.routes)) + 6 * (int64_t)w.r;
+      int n, from, to, tiles;
+      route_sight<WINDOW>(s, rp[2], rp[3], n, from, to, tiles);
+      if (w.tiles == from && from < to) {
+        w.j = to;
+        w.tiles = tiles;
+        break;
+      }
+    }
     if (++w.r < w.r_end) {
       const auto* rp = fixed(reinterpret_cast<const int32_t*>(a.routes)) + 6 * (int64_t)w.r;
       if (WINDOW) {
-        walk_route<WINDOW>(w, s, rp[2], rp[3], rp[4], 0);
+        walk_route<WINDOW, JUMP>(w, s, rp[2], rp[3], rp[4], 0);
       } else {
         w.n = visible(rp[2], rp[3], s.last_pos);
         w.tb = rp[2];
@@ -979,7 +1003,7 @@ __device__ __forceinline__ int count_tiles(const RowsArgs& a, int b, int r0, int
 
 // Positions the walk at key tile k of the sequence; tiles of a route: its
 // visible tokens / 32, rounded up.  Sixty-four routes at a time.
-template <bool WINDOW>
+template <bool WINDOW, bool JUMP>
 __device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int r1, const Sight& s,
                                         int64_t k, int lane) {
   w.r = w.r_end = r1;
@@ -1008,9 +1032,9 @@ __device__ __forceinline__ void walk_to(const RowsArgs& a, Walk& w, int r0, int 
       w.r = r + at;
       if (WINDOW) {
         const int j = uniform((int)(k - __shfl((long long)(x - tiles), at)));
-        walk_route<WINDOW>(w, s, __builtin_amdgcn_readlane(tb, at),
-                           __builtin_amdgcn_readlane(te, at), __builtin_amdgcn_readlane(base, at),
-                           j);
+        walk_route<WINDOW, JUMP>(w, s, __builtin_amdgcn_readlane(tb, at),
+                                 __builtin_amdgcn_readlane(te, at),
+                                 __builtin_amdgcn_readlane(base, at), j);
       } else {
         w.n = __builtin_amdgcn_readlane(n, at);
         w.tb = __builtin_amdgcn_readlane(tb, at);
@@ -1239,6 +1263,7 @@ __device__ __forceinline__ void fill_nan(const RowsArgs& a, int row0, int64_t m0
 // 64K tokens, 4.1 GB, 678 us, 6.0 TB/s.
 template <bool FP8, bool TREE, bool WINDOW>
 struct Work {
+  static constexpr bool kJump = WINDOW && !FP8;
   const RowsArgs& a;
   int tid, lane, wave, g;
   int row0, n_rows;
@@ -1247,9 +1272,8 @@ struct Work {
   u32x4 q[8];
   // positions: the lane's row, the wave's and the workgroup's first, the workgroup's last
   int pos, pos_min, tile_min, last_pos;
-  // with a window, where it begins: of the lane's row, of the wave's and workgroup's
-  // last, of the workgroup's first
-  int low, low_max, tile_low, first_low;
+  // with a window, where it begins: of the lane's row, of the workgroup's last and first
+  int low, tile_low, first_low;
   uint64_t draft;            // drafted rows that the lane's row sees
   Walk walk;
   int left;                  // tiles of this part still to come
@@ -1285,11 +1309,11 @@ struct Work {
         pg.pid[i] = pid;
       }
       ++walk.j;
-      if (WINDOW && walk.j == walk.from) walk.j = walk.to;
+      if (kJump && walk.j == walk.from) walk.j = walk.to;
       if (__builtin_expect(walk.j < walk.tiles, 1))
         walk_ids(a, walk);
       else
-        walk_on<WINDOW>(a, walk, Sight{last_pos, first_low, a.sinks});
+        walk_on<WINDOW, kJump>(a, walk, Sight{last_pos, first_low, a.sinks});
     } else if (TREE && drafts > 0) {
       t.pos0 = n_rows - drafts;
       t.left = drafts;
@@ -1299,10 +1323,9 @@ struct Work {
     return t;
   }
 
-  // Whether some token of the tile lies before a window that begins at `begin`, and is
-  // no sink.
-  __device__ __forceinline__ bool cut_before(const Tile& t, int begin) const {
-    return t.pos0 < begin && __builtin_elementwise_sub_sat(a.sinks, t.pos0) < kKeyTile;
+  // Whether some token of the tile is no sink (0 or 1: joined without a branch).
+  __device__ __forceinline__ int not_sinks(const Tile& t) const {
+    return __builtin_elementwise_sub_sat(a.sinks, t.pos0) < kKeyTile;
   }
 
   __device__ __forceinline__ static bool paged(const Tile& t) {
@@ -1376,7 +1399,7 @@ struct Work {
     // (what a window adds stands in statements of its own: as terms of these two
     // conditions, false at compile time, it cost the tree kernels 217 scalar registers)
     bool partly = t.kind || __builtin_elementwise_sub_sat(tile_min, t.pos0) < kKeyTile - 1;
-    if constexpr (WINDOW) partly |= cut_before(t, tile_low);
+    if constexpr (WINDOW) partly |= (int)(t.pos0 < tile_low) & not_sinks(t);
     if (__builtin_expect(partly, 0)) {
       // some row of the workgroup does not see all of it
       if (cut_tile(t.left, tid, lv)) *odd_step = steps;
@@ -1408,7 +1431,7 @@ struct Work {
     const int half = lane >> 5;
     uint32_t sees = ~0u;
     bool mask = t.kind || __builtin_elementwise_sub_sat(pos_min, t.pos0) < kKeyTile - 1;
-    if constexpr (WINDOW) mask |= cut_before(t, low_max);
+    if constexpr (WINDOW) mask |= (int)(__ballot(t.pos0 < low) != 0) & not_sinks(t);
     if (__builtin_expect(mask, 0)) {
       const int e = min(__builtin_elementwise_sub_sat(pos, t.pos0), t.left - 1);
       sees = e < 0 ? 0 : e >= 31 ? ~0u : (2u << e) - 1;
@@ -1667,7 +1690,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   }
   w.pos = w.pos_min = w.tile_min = INT32_MAX;
   w.last_pos = sight.last_pos;
-  w.low = w.low_max = w.tile_low = w.first_low = sight.low;
+  w.low = w.tile_low = w.first_low = sight.low;
   w.draft = 0;
   if constexpr (TREE) {
     w.draft = mine ? a.tree_mask[row0 + row] : 0;
@@ -1681,7 +1704,6 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
         return window_begin(a, p0, (int)((uint32_t)min(pair, m1 - 1) / (uint32_t)G));
       };
       w.low = begins(m);
-      w.low_max = uniform(begins(m0 + 32 * wave + 31));
       w.tile_low = uniform(begins(m1 - 1));
     }
   }
@@ -1718,7 +1740,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     w.walk.r = route0;
     w.walk.r_end = route1;
     if (WINDOW) {
-      walk_route<WINDOW>(w.walk, sight, it.tok_begin, it.tok_end, it.page_base, it.key0);
+      walk_route<WINDOW, WINDOW && !FP8>(w.walk, sight, it.tok_begin, it.tok_end, it.page_base, it.key0);
     } else {
       w.walk.n = see;
       w.walk.tb = it.tok_begin;
@@ -1728,7 +1750,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     }
     walk_ids(a, w.walk);
   } else {
-    walk_to<WINDOW>(a, w.walk, route0, route1, sight, it.key0, lane);
+    walk_to<WINDOW, WINDOW && !FP8>(a, w.walk, route0, route1, sight, it.key0, lane);
   }
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) {
