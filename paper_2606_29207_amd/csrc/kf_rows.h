@@ -16,6 +16,7 @@ constexpr int kMinPart = 4;       // key tiles of a part at least: 8 drafted tok
                                   // 64 rows over 1000 26.1 instead of 21.3
 constexpr int kMeanSteps = 24;    // steps of a workgroup up to which a launch needs no plan:
 constexpr int kMostSteps = 96;    // mean, and at most
+constexpr int kWindowSteps = 512; // (with a window that the mean sequence fills)
 constexpr int kSplitSlots = 4;    // (row tile, KV head) pairs per resident workgroup from which on
                                   // a launch splits none (2, 4 and 8: prompts of 6K .. 16K tokens
                                   // the same within 1 %; 8 packed ones 145, 144 and 148 us)

@@ -1063,7 +1063,8 @@ __device__ __forceinline__ int v_at(int page, int d, int hh) {
 // will read them soon (the non-temporal hint): a tree's cache is read by one
 // workgroup, or by two beside each other, a prompt's by many one after another.
 // Agentic trees 888 -> 824 us, 32-row trees over 32K 433 -> 425 with the hint; a
-// 16K-token prompt would go 2307 -> 2456.
+// 16K-token prompt would go 2307 -> 2456.  Decode steps of 48 sequences, window 4096,
+// 153 -> 130, prompts with a window of 2048 611 -> 680.
 template <bool ONCE>
 __device__ __forceinline__ void to_lds(const char* g, char* l) {
   __builtin_amdgcn_global_load_lds(
@@ -1261,7 +1262,7 @@ __device__ __forceinline__ void fill_nan(const RowsArgs& a, int row0, int64_t m0
 // the softmax.  fp8 trees have scalar registers spilled in the loop as well (some 140;
 // 120 scalar instructions a step).  bf16 trees of few rows wait for memory: 48 over 2K ..
 // 64K tokens, 4.1 GB, 678 us, 6.0 TB/s.
-template <bool FP8, bool TREE, bool WINDOW>
+template <bool FP8, bool TREE, bool WINDOW, bool ONCE>
 struct Work {
   static constexpr bool kJump = WINDOW && !FP8;
   const RowsArgs& a;
@@ -1344,11 +1345,11 @@ struct Work {
     if constexpr (!FP8) asm volatile("" : "+s"(own));
     l += own;
     if constexpr (!FP8) {
-      to_lds<TREE>(from + pg.at[0] + off, l);
-      to_lds<TREE>(from + pg.at[1] + off, l + 4096);
+      to_lds<ONCE>(from + pg.at[0] + off, l);
+      to_lds<ONCE>(from + pg.at[1] + off, l + 4096);
     } else {  // two waves a page
       const uint64_t x = pg.at[0], y = pg.at[1];
-      to_lds<TREE>(from + (wave >> 1 ? y : x) + off, l);
+      to_lds<ONCE>(from + (wave >> 1 ? y : x) + off, l);
     }
   }
   // fp8: the scales of tile t, every wave a copy: K of both pages, then V.
@@ -1583,7 +1584,7 @@ struct Work {
   }
 };
 
-template <bool FP8, bool TREE, bool WINDOW>
+template <bool FP8, bool TREE, bool WINDOW, bool ONCE>
 __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   // K and V: four tiles each (bf16), or two tiles and a ring of four (fp8)
   constexpr int kTile = kKeyTile * kDim * 2, kRing = FP8 ? kKeyTile * kDim : 16;
@@ -1675,7 +1676,7 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
   const uint32_t mc = mine ? m : m1 - 1;
   const int row = mc / (uint32_t)G, h = g * G + mc % (uint32_t)G;
   const float c0 = a.scale_log2;
-  Work<FP8, TREE, WINDOW> w{a};
+  Work<FP8, TREE, WINDOW, ONCE> w{a};
   w.tid = tid;
   w.lane = lane;
   w.wave = wave;
@@ -1969,7 +1970,7 @@ hipError_t launch_append_rows(const AppendRowsArgs& a, bool fp8, hipStream_t str
   return hipGetLastError();
 }
 
-template <bool TREE, bool WINDOW>
+template <bool TREE, bool WINDOW, bool ONCE>
 hipError_t launch_rows(const RowsArgs& a, bool fp8, hipStream_t stream) {
   hipError_t st;
   if (a.parts == 0) {
@@ -1980,9 +1981,9 @@ hipError_t launch_rows(const RowsArgs& a, bool fp8, hipStream_t stream) {
   const int items = a.parts > 0 ? a.max_tiles * a.parts : a.max_tiles + (a.may_split ? a.max_recs : 0);
   const uint32_t grid = (uint32_t)items * a.num_kv_heads;
   if (fp8)
-    rows_kernel<true, TREE, WINDOW><<<grid, 256, 0, stream>>>(a);
+    rows_kernel<true, TREE, WINDOW, ONCE><<<grid, 256, 0, stream>>>(a);
   else
-    rows_kernel<false, TREE, WINDOW><<<grid, 256, 0, stream>>>(a);
+    rows_kernel<false, TREE, WINDOW, ONCE><<<grid, 256, 0, stream>>>(a);
   st = hipGetLastError();
   if (st != hipSuccess || a.parts == 1 || (a.parts == 0 && !a.may_split)) return st;
   // a wave per (row, head) and turn; most splits at most
@@ -1994,9 +1995,12 @@ hipError_t launch_rows(const RowsArgs& a, bool fp8, hipStream_t stream) {
 }
 
 hipError_t launch_rows_attn(const RowsArgs& a, bool fp8, bool tree, hipStream_t stream) {
-  if (tree) return launch_rows<true, false>(a, fp8, stream);
-  return a.window < 0 ? launch_rows<false, false>(a, fp8, stream)
-                      : launch_rows<false, true>(a, fp8, stream);
+  if (tree) return launch_rows<true, false, true>(a, fp8, stream);
+  if (a.window < 0) return launch_rows<false, false, false>(a, fp8, stream);
+  // rows of one row tile a sequence (decode steps): no other workgroup reads their tokens
+  return (int64_t)a.num_rows * a.group <= (int64_t)kRowTile * a.num_seqs
+             ? launch_rows<false, true, true>(a, fp8, stream)
+             : launch_rows<false, true, false>(a, fp8, stream);
 }
 
 }  // namespace kf
