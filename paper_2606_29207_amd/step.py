@@ -5,14 +5,15 @@ routes and page ids) and the output buffers as torch device tensors, and runs
 one decode step as the paper orders it (Section 3.2, steps 3-4; Section 5.1):
 the tail routes append the step's K/V token, every route computes its partial,
 and the partials of each sequence are merged.  Prompts, drafted trees and
-accepted rows go over the same buffers (append_rows, prompt_attn, tree_attn).
+accepted rows go over the same buffers (append_rows, prompt_attn, tree_attn), and so do
+the calls that keep the cache within a budget (window_attn, attn_weights, evict).
 Marshalling only: the calls are the library's HIP kernels, enqueued on the current
 stream.  The arguments of a decode step are checked and marshalled once, when the
 state is built.  Those of the calls on whole rows, whose tensors differ from call to
 call, are checked in every call, which also allocates its outputs and workspace (24 to
 35 us of host time, more than the kernels of a small tree); a loop that keeps its
-buffers binds them with kf.bind_prompt_attn, kf.bind_tree_attn and
-kf.bind_kv_append_rows (8 us a call).
+buffers binds them with kf.bind_prompt_attn, kf.bind_tree_attn, kf.bind_window_attn,
+kf.bind_kv_append_rows, kf.bind_attn_weights and kf.bind_kv_evict (8 us a call).
 """
 from __future__ import annotations
 
@@ -92,6 +93,7 @@ class DecodeState:
                                              self.err_flags)
         self._fused = self._bind_fused(self.workspace)
         self._no_alloc = None
+        self._weights = None
         self._frozen = True
 
     def __setattr__(self, name, value):
@@ -239,6 +241,48 @@ class DecodeState:
                          self.seq_route_begin, seq_row_begin, out, lse, ws, self.err_flags,
                          self.k_scale, self.v_scale)
         return out, lse
+
+    # ------------------------------------------------- operators of a budget
+    @property
+    def weights(self) -> torch.Tensor:
+        """Token weights float32 [P, Hkv, 16] of this state's pools (attn_weights, evict),
+        zero until they are first used."""
+        if self._weights is None:
+            self._weights = kf.alloc_weights(self.shape, self.device)
+        return self._weights
+
+    def window_attn(self, q: torch.Tensor, first_pos: torch.Tensor, seq_row_begin: torch.Tensor,
+                    sinks: int, window: int, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+        """prompt_attn with a sliding window and attention sinks (kf_window_attn): the row
+        at position p sees the tokens t <= p with t < sinks or t > p - window."""
+        with torch.cuda.stream(stream):
+            out, lse, ws = self._rows_buffers(q)
+            kf.window_attn(self.shape, q, first_pos, sinks, window, self.k_pool, self.v_pool,
+                           self.routes, self.max_pages_per_route, self.page_ids,
+                           self.seq_route_begin, seq_row_begin, out, lse, ws, self.err_flags,
+                           self.k_scale, self.v_scale)
+        return out, lse
+
+    def attn_weights(self, q: torch.Tensor, lse: torch.Tensor, first_pos: torch.Tensor,
+                     seq_row_begin: torch.Tensor, decay: float = 1.0, stream=None):
+        """Adds to `weights` what the rows q, whose attention over this state's cache
+        returned lse, gave to each token (kf_attn_weights).  After a decode step: q and
+        lse of this state, first_pos the position of each sequence's newest token."""
+        with torch.cuda.stream(stream):
+            kf.attn_weights(self.shape, q, lse, first_pos, self.k_pool, self.routes,
+                            self.max_pages_per_route, self.page_ids, seq_row_begin, decay,
+                            self.weights, self.err_flags, self.k_scale)
+
+    def evict(self, into: torch.Tensor, keep: torch.Tensor, max_keep: int, keep_first: int,
+              keep_last: int, stream=None):
+        """Moves what stays of each sequence, by `weights`, into the pages of its empty
+        route into[b] (kf_kv_evict); the other routes of the sequence are empty then.
+        Appends go on in into[b]: write it into tail_route, whose decode steps read it."""
+        with torch.cuda.stream(stream):
+            kf.kv_evict(self.shape, self.k_pool, self.v_pool, self.weights, self.routes,
+                        self.max_pages_per_route, self.page_ids, self.seq_route_begin, into, keep,
+                        max_keep, keep_first, keep_last, self.err_flags, self.k_scale,
+                        self.v_scale)
 
     def flags(self) -> int:
         return int(self.err_flags.item())
