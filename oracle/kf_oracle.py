@@ -473,8 +473,8 @@ def attn_weights(q, lse, row_begin, first_pos, k_pool, routes, page_ids, weights
         i0, i1 = int(row_begin[b]), int(row_begin[b + 1])
         if i0 == i1 and 0 <= i0 <= N:
             continue
-        if not 0 <= i0 <= i1 <= N or not _route_ok(routes[r], B, len(page_ids),
-                                                   max_pages_per_route):
+        if (not 0 <= i0 <= i1 <= N or not _route_ok(routes[r], B, len(page_ids), max_pages_per_route)
+                or int(routes[r][3]) - int(routes[r][2]) > 2 ** 31 - 1025):
             flags |= EFLAG_BAD_ROUTE
             continue
         tok = np.arange(routes[r][2], routes[r][3], dtype=np.int64)

@@ -12,11 +12,15 @@
 namespace kf {
 namespace {
 
+// The tokens of a route, and of a sequence that is evicted: places a workgroup's tile
+// behind the last one still fit in 32 bits.
+constexpr int kMostTokens = INT32_MAX - 1024;
+
 // A route's row (seq, part, tok_begin, tok_end, page_base, page_cap) is sound.
 __device__ __forceinline__ bool route_row_ok(int tok_begin, int tok_end, int base, int cap,
                                              int max_pages, int num_page_ids) {
   const int64_t n = (int64_t)tok_end - tok_begin, pages = n > 0 ? (n + kPage - 1) / kPage : 0;
-  return n >= 0 && n <= INT32_MAX && base >= 0 && pages <= cap && pages <= max_pages &&
+  return n >= 0 && n <= kMostTokens && base >= 0 && pages <= cap && pages <= max_pages &&
          base + pages <= num_page_ids;
 }
 
@@ -753,7 +757,7 @@ __device__ __forceinline__ EvictSeq evict_sequence(const EvictArgs& a, int b, Ev
     if (__syncthreads_or(bad)) return s;
     before = waves_before(sh.sum, w, all);
   }
-  if (all > INT32_MAX - 1024) return s;
+  if (all > kMostTokens) return s;
   if (own < s.routes && (!few || w == 0)) sh.pre[own] = (int)(before + x) - n;
   if (tid == 0) sh.pre[s.routes] = (int)all;
   s.L = (int)all;
@@ -1021,7 +1025,7 @@ struct EvictPart {
 };
 __device__ __forceinline__ EvictPart evict_part(const EvictArgs& a, const EvictSeq& s, int p) {
   EvictPart x;
-  x.parts = max(1, min(a.parts, (s.L + kPartTokens - 1) / kPartTokens));
+  x.parts = min(a.parts, (s.L - 1) / kPartTokens + 1);
   const int per = ((s.L + x.parts - 1) / x.parts + 1023) / 1024 * 1024;
   x.lo = (int)min((int64_t)s.L, (int64_t)p * per);
   x.hi = (int)min((int64_t)s.L, (int64_t)x.lo + per);

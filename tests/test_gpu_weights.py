@@ -145,6 +145,24 @@ def test_a_bad_row_of_the_row_table(gpu):
     assert got[1] == 2
 
 
+def test_a_route_of_nearly_all_of_32_bits_is_refused(gpu):
+    """Longer than any place behind its last token can be counted: left as it was."""
+    import torch
+    from paper_2606_29207_amd import kf
+    pages = 2 ** 27
+    ids = torch.zeros(pages, dtype=torch.int32, device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    shape = kf.make_shape(1, 4, 1, kf.KV_BF16, 2, pages, 0.1)
+    k = torch.zeros((2, 1, 16, 128), dtype=torch.bfloat16, device="cuda")
+    q = torch.zeros((1, 4, 128), dtype=torch.bfloat16, device="cuda")
+    for end in (2 ** 31 - 1024, 2 ** 31 - 1):
+        w, err = torch.full((2, 1, 16), 0.25, device="cuda"), torch.zeros(1, **i32)
+        kf.attn_weights(shape, q, torch.zeros((1, 4), device="cuda"), torch.tensor([end - 1], **i32),
+                        k, torch.tensor([[0, 0, 0, end, 0, pages]], **i32), pages, ids,
+                        torch.tensor([0, 1], **i32), 1.0, w, err)
+        assert (w == 0.25).all() and int(err.item()) == kf.EFLAG_BAD_ROUTE
+
+
 def test_sequences_without_rows_are_not_looked_at(gpu):
     c = Cache([90, 100, 110], H=2, part=64, seed=13)
     r = Rows(c, [0, 30, 0], 2, seed=13)
