@@ -45,6 +45,7 @@ size_t kf_attn_weights_workspace_bytes(const kf_shape* shape, int32_t num_rows, 
   a.group = shape->num_q_heads / shape->num_kv_heads;
   a.num_routes = std::max(1, num_routes);
   a.max_pages_per_route = max_pages_per_route;
+  a.num_page_ids = shape->num_page_ids;
   kf::plan_attn_weights(a, 2 * (int64_t)kf::cu_count());
   return std::max<size_t>(256, kf::attn_weights_bytes(a));
 }
@@ -195,7 +196,7 @@ EvictLayout evict_layout(const kf_shape& s, int32_t max_keep) {
 // By the (row, head) pairs of a sequence on the mean, and the workgroups of 256 keys
 // that the table has room for.
 void plan_attn_weights(AttnWeightsArgs& a, int64_t slots) {
-  const int64_t most = std::max(1, a.max_pages_per_route);
+  const int64_t most = std::max(1, std::min(a.max_pages_per_route, a.num_page_ids));
   const int64_t columns = (int64_t)a.num_rows * a.group / std::max(1, a.num_seqs);
   // A workgroup's pages: 16 (one decode row over 32K tokens, 16 sequences, 190 us; 8 and
   // 32 212 and 195, 64 204, 128 222, 256 195), where the columns stay in LDS twice as many

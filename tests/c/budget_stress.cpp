@@ -6,6 +6,7 @@
 #include <stdio.h>
 #include <stdlib.h>
 
+#include <algorithm>
 #include <random>
 
 #include "kf.h"
@@ -47,7 +48,7 @@ hipError_t launch_attn_weights(const AttnWeightsArgs& a, bool fp8, hipStream_t) 
   CHECK(!fp8 || a.k_scale);
   CHECK(a.chunk_pages >= 16 && a.chunks >= 1);
   // every page of a route has a workgroup, and a join's thread per token
-  CHECK((int64_t)a.chunks * a.chunk_pages >= a.max_pages_per_route);
+  CHECK((int64_t)a.chunks * a.chunk_pages >= std::min(a.max_pages_per_route, a.num_page_ids));
   CHECK(a.segments >= 1 && a.segments <= kMaxSegments);
   CHECK(a.segments == 1 || a.chunk_pages == 16);
   const int64_t wgs = (int64_t)a.chunks * a.num_kv_heads * a.num_routes;
