@@ -246,9 +246,13 @@ class DecodeState:
     @property
     def weights(self) -> torch.Tensor:
         """Token weights float32 [P, Hkv, 16] of this state's pools (attn_weights, evict),
-        zero until they are first used."""
+        zero until they are first used.  That is not in a graph's capture, whose replays
+        would clear them."""
         if self._weights is None:
+            if torch.cuda.is_current_stream_capturing():
+                raise kf.KFError("use DecodeState.weights once before a capture")
             self._weights = kf.alloc_weights(self.shape, self.device)
+            torch.cuda.current_stream(self.device).synchronize()  # zero for all streams
         return self._weights
 
     def window_attn(self, q: torch.Tensor, first_pos: torch.Tensor, seq_row_begin: torch.Tensor,

@@ -179,6 +179,24 @@ def test_a_graph_of_weights_and_eviction_after_decode_steps(gpu):
             assert torch.equal(t.view(torch.uint8), w.view(torch.uint8)), i
 
 
+def test_weights_are_not_first_used_in_a_capture(gpu):
+    import torch
+    from paper_2606_29207_amd import kf
+    from paper_2606_29207_amd.step import DecodeState
+    c = Cache([40], H=1, seed=1)
+    st = DecodeState(q=bits(np.zeros((1, 4, 128))), k_pool=c.k_pool, v_pool=c.v_pool,
+                     routes=c.routes, page_ids=c.page_ids, seq_route_begin=c.seq_route_begin,
+                     tail_route=np.zeros(1, np.int32), scale=SCALE, max_pages_per_route=c.max_pages)
+    x = torch.zeros(4, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        with pytest.raises(kf.KFError, match="before a capture"):
+            st.weights
+        x += 1                           # (a graph of something)
+    g.replay()
+    assert (st.weights == 0).all() and st.weights is st.weights
+
+
 def test_calls_on_streams_at_once(gpu):
     """A window, weights and an eviction over caches of their own, in flight together."""
     import torch
