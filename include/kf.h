@@ -486,19 +486,26 @@ int kf_tree_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64_t
  *     kf_prompt_attn) and the query heads h of g's group of
  *     exp(scale * (q[i][h] . k_t) - lse[i][h]),
  *   old = decay * weights[t][g] for t < first_pos[b], else 0,
- * where lse [num_rows][num_q_heads] is what the rows' attention returned.  A token
+ * where lse [num_rows][num_q_heads] is what the rows' attention returned: that of
+ * kf_prompt_attn or a decode step (kf_window_attn's and kf_tree_attn's count other
+ * tokens than those that are summed here).  A token
  * whose own row is in the call is new and starts from 0, so that a decode step's
  * call (one row per sequence, first_pos its position), a prompt's and a chunk's
- * need no clearing; with decay = 0 weights are not read.  A row whose lse is -inf
+ * need no clearing (a token that was new in no call has what its slot held before);
+ * with decay = 0 weights are not read.  A row whose lse is -inf
  * or NaN gives nothing.  Sums are float32; the same arguments give the same bits.
  * q and lse as for kf_prompt_attn (q_stride elements between rows of q).
  * Routes are taken one by one, as kf_partial_attn takes them, and weights of
  * sequences without rows, and of slots that hold no token, are left as they were.
+ * A page in several routes of sequences with rows (a prefix that they share) ends
+ * with the weights that one of them gives, any one, which is not detected: give
+ * such sequences their rows in calls of their own, the later ones with decay = 1.
  * max_pages_per_route as for kf_prompt_attn.
  * Device checks: a route whose sequence is outside [0, num_seqs), or whose
  * sequence's row of seq_row_begin decreases or leaves [0, num_rows], or that fails
- * kf_partial_attn's checks sets KF_EFLAG_BAD_ROUTE and is left as it was; tokens of
- * a page whose id lies outside the pool set KF_EFLAG_BAD_PAGE and have no weight.
+ * kf_partial_attn's checks, or has 2^31 - 1024 tokens or more, sets
+ * KF_EFLAG_BAD_ROUTE and is left as it was; tokens of a page whose id lies outside
+ * the pool set KF_EFLAG_BAD_PAGE and have no weight.
  * At most 65535 routes, and 2^28 - 256 (row, query head of a group) pairs, in a call.
  * workspace: kf_attn_weights_workspace_bytes of the same arguments (launches of many
  * rows over few pages split the rows' sum and use it: 4 MB at most), 16-byte aligned;
@@ -524,7 +531,9 @@ int kf_attn_weights(const kf_shape* shape, const void* q, int32_t num_rows, int6
  * pages reserved -- with their weights, and the routes' rows follow:
  * routes[into[b]].tok_end = tok_begin + K, and every other route of the sequence is
  * empty, its pages the caller's again.  Nothing else of the pools changes: not the
- * pages that the tokens came from, not the slots behind the last one.  into[b] = -1
+ * pages that the tokens came from (which other sequences may share), not the slots
+ * behind the last one.  The pages that tokens move into belong to no other route of
+ * the call, which is not detected.  into[b] = -1
  * leaves sequence b alone.  max_keep bounds keep[b].
  * The table, the CSR rows and a later kf_decode_step agree without the host: give
  * into as the tail_route that follows, and the emptied route as the next call's.
