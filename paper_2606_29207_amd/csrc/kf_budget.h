@@ -53,7 +53,9 @@ hipError_t launch_attn_weights(const AttnWeightsArgs& a, bool fp8, hipStream_t s
 constexpr int kPartTokens = 8192;  // of a part of a sequence whose tokens are told apart by several
                                    // workgroups, and the most parts
 constexpr int kMaxParts = 32;
-constexpr int64_t kOneWorkgroup = 23 * 1024;  // tokens of a sequence up to which one does
+constexpr int64_t kOneWorkgroup = 40 * 1024;  // tokens of a sequence up to which one does, and
+constexpr int64_t kHeldTokens = 64 * 1024;    // where the parts would be more than kFewParts
+constexpr int64_t kFewParts = 256;
 constexpr size_t kMostParts = 4096;  // of a launch: 100 MB of bins
 
 struct EvictArgs {

@@ -654,7 +654,6 @@ __global__ __launch_bounds__(256) void attn_weights_join_kernel(AttnWeightsArgs 
 }
 
 // -------------------------------------------------------------------- evict
-constexpr int kKeysInLds = 34 * 1024;  // tokens of a sequence whose keys stay in LDS
 constexpr int kEvictRoutes = 1024;     // routes of a sequence at most
 constexpr int kBins = 2048;            // of a pass of 11 bits
 
@@ -896,69 +895,129 @@ struct EvictRule {
   }
 };
 
-// Which tokens of a sequence and KV head stay, by one workgroup: a threshold by radix
-// over their keys, which stay in LDS, up to 34K of them.  Each wave has a stretch of the
-// places of its own, so that a place's rank is its wave's first rank and a count of
-// ballots.
-__global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
-  __shared__ uint32_t keys[kKeysInLds];
-  __shared__ uint32_t hist[kBins];
-  __shared__ EvictShared sh;
-  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
-  const int g = blockIdx.x, b = blockIdx.y;
-  int32_t* plan = a.plan + 2 * b;
-  EvictSeq s = evict_sequence(a, b, sh);
-  const int per = (s.L + 1023) / 1024 * 64;
-  const int lo = min(s.L, w * per), hi = min(s.L, lo + per);
-  // The keys stay in registers, if a wave's share is a batch, or in LDS, or are read anew.
-  const bool in_regs = per <= 512, in_lds = !in_regs && s.L <= kKeysInLds;
-  EvictBatch own;
-  if (s.status == 0) {
-    bool bad = evict_bad_target(a, s);
-    if (in_regs) {
-      if (lo < hi) {
-        EvictWalk walk = evict_enter(s, sh, lo);
-        evict_load(a, sh, g, walk, lo, hi, true, own);
+// The keys of a wave's places lo .. hi - 1 in registers, at most N batches of 512, with
+// AT also where they are in the pool (every index is known at compile time).  All page
+// ids are sent for before the first weight.  N = 0: none, they are read anew.
+template <int N, bool AT>
+struct EvictHeld {
+  const EvictArgs& a;
+  const EvictSeq& s;
+  const EvictShared& sh;
+  int g, lo, hi;
+  uint32_t x[8 * N + 1];
+  int at[AT ? 8 * N : 1];
+
+  template <class F>
+  __device__ __forceinline__ void batches(F f) const {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) bad |= lo + 64 * i + lane < hi && own.at[i] < 0;
+    for (int b = 0; b < N; ++b)
+      if (lo + 512 * b < hi) f(b, lo + 512 * b + (int)(threadIdx.x & 63));
+  }
+  // Whether a place lies in a page outside the pool.
+  __device__ __forceinline__ bool load() {
+    bool bad = false;
+    if constexpr (N == 0) {
+      evict_walk(a, s, sh, g, lo, hi, false,
+                 [&](int e, int at, float wt) { bad |= e < hi && at < 0; });
+      return bad;
+    }
+    if (lo >= hi) return false;
+    uint32_t slots[N + 1];
+    EvictWalk w = evict_enter(s, sh, lo);
+    batches([&](int b, int e0) __attribute__((always_inline)) {
+      slots[b] = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int e = min(e0 + 64 * i, hi - 1);
+        if (e >= w.end) {
+          do ++w.r;
+          while (e >= sh.pre[w.r + 1]);
+          w.begin = sh.pre[w.r];
+          w.end = sh.pre[w.r + 1];
+          w.base = sh.base[w.r];
+        }
+        x[8 * b + i] = a.page_ids[w.base + (e - w.begin) / kPage];
+        slots[b] |= (uint32_t)((e - w.begin) & (kPage - 1)) << (4 * i);
       }
-    } else {
-      evict_walk(a, s, sh, g, lo, hi, in_lds, [&](int e, int at, float wt) {
-        if (e >= hi) return;
-        bad |= at < 0;
-        if (in_lds) keys[e] = order_key(wt);
+    });
+    batches([&](int b, int) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint32_t id = x[8 * b + i];
+        const uint32_t slot = slots[b] >> (4 * i) & (kPage - 1);
+        bad |= id >= (uint32_t)a.num_pages;
+        id = id < (uint32_t)a.num_pages ? id : 0;
+        if constexpr (AT) at[8 * b + i] = (int)(id * kPage + slot);
+        x[8 * b + i] = __builtin_bit_cast(
+            uint32_t, a.weights[((size_t)id * a.num_kv_heads + g) * kPage + slot]);
+      }
+    });
+    batches([&](int b, int) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        x[8 * b + i] = order_key(__builtin_bit_cast(float, x[8 * b + i]));
+    });
+    return bad;
+  }
+  // f(place, key), places beyond hi too.
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+    if constexpr (N == 0)
+      evict_walk(a, s, sh, g, lo, hi, true, [&](int e, int at, float wt) { f(e, order_key(wt)); });
+    batches([&](int b, int e0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f(e0 + 64 * i, x[8 * b + i]);
+    });
+  }
+  // f(place, where it is, key)
+  template <class F>
+  __device__ __forceinline__ void each_at(F f) const {
+    if constexpr (N == 0) {
+      evict_walk(a, s, sh, g, lo, hi, true,
+                 [&](int e, int at, float wt) { f(e, at, order_key(wt)); });
+    } else if constexpr (AT) {
+      batches([&](int b, int e0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f(e0 + 64 * i, at[8 * b + i], x[8 * b + i]);
+      });
+    } else if (lo < hi) {
+      EvictWalk w = evict_enter(s, sh, lo);
+      batches([&](int b, int e0) __attribute__((always_inline)) {
+        EvictBatch there;
+        evict_load(a, sh, g, w, lo + 512 * b, hi, false, there);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f(e0 + 64 * i, there.at[i], x[8 * b + i]);
       });
     }
+  }
+};
+
+// Which tokens of a sequence and KV head stay, by one workgroup: a threshold by radix
+// over their keys.  Each wave has a stretch of the places of its own, so that a place's
+// rank is its wave's first rank and a count of ballots.
+// The keys of up to 64K tokens stay in registers: 48 sequences of 2K .. 64K tokens 110 us,
+// 191 with those of up to 34K in LDS and a wait for ids and weights every 512 places; 16 of
+// 16K 30 and 41.  Code for each size: 700 tokens 13.9 us, 19 in the largest one's.
+template <int N, bool AT>
+__device__ __forceinline__ void evict_select(const EvictArgs& a, EvictSeq& s, EvictShared& sh,
+                                             uint32_t* hist, int per) {
+  const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
+  const int g = blockIdx.x, b = blockIdx.y;
+  const int lo = min(s.L, w * per), hi = min(s.L, lo + per);
+  EvictHeld<N, AT> own{a, s, sh, g, lo, hi};
+  if (s.status == 0) {
+    bool bad = evict_bad_target(a, s);
+    bad |= own.load();
     if (__syncthreads_or(bad)) s.status = KF_EFLAG_BAD_PAGE;
   }
   if (g == 0 && tid == 0) {
+    int32_t* plan = a.plan + 2 * b;
     plan[0] = s.status ? -1 : s.K;
     plan[1] = s.base;
     if (s.status > 0) atomicOr(a.err_flags, s.status);
   }
   if (s.status) return;
 
-  // the keys of this wave's places, eight at a time a lane
-  auto each = [&](auto f) __attribute__((always_inline)) {
-    if (in_regs) {
-      if (lo < hi) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f(lo + 64 * i + lane, order_key(own.weight[i]));
-      }
-      return;
-    }
-    if (!in_lds) {
-      evict_walk(a, s, sh, g, lo, hi, true, [&](int e, int at, float wt) { f(e, order_key(wt)); });
-      return;
-    }
-    for (int e0 = lo; e0 < hi; e0 += 512) {
-      uint32_t k[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) k[i] = keys[min(e0 + 64 * i + lane, s.L - 1)];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f(e0 + 64 * i + lane, k[i]);
-    }
-  };
   int want = s.K - s.c0 - (s.L - s.c1);  // of those that compete
   EvictRule rule{s.c0, s.c1, want == 0, want == s.c1 - s.c0, 0};
   if (!rule.none && !rule.every) {
@@ -967,7 +1026,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
       const int bins = pass_bins(pass);
       hist[tid] = hist[tid + 1024] = 0;
       __syncthreads();
-      each([&](int e, uint32_t key) {
+      own.each([&](int e, uint32_t key) {
         evict_count(hist, e >= from && e < till && pass_takes(pass, key, rule.top),
                     key >> pass_shift(pass) & (bins - 1));
       });
@@ -981,7 +1040,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
     want = 0;
   }
   int sure = 0, equals = 0;
-  each([&](int e, uint32_t key) {
+  own.each([&](int e, uint32_t key) {
     sure += __builtin_popcountll(__ballot(e < hi && rule.sure(e, key)));
     equals += __builtin_popcountll(__ballot(e < hi && rule.equal(e, key)));
   });
@@ -996,7 +1055,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
   equals = waves_before(sh.scan[1], w, all);
   int32_t* list = a.list + ((size_t)b * a.num_kv_heads + g) * a.max_keep;
   const uint64_t lower = ((uint64_t)1 << lane) - 1;
-  auto enlist = [&](int e, int at, uint32_t key) __attribute__((always_inline)) {
+  own.each_at([&](int e, int at, uint32_t key) __attribute__((always_inline)) {
     const bool yes = e < hi && rule.sure(e, key), eq = e < hi && rule.equal(e, key);
     const uint64_t ys = __ballot(yes), es = __ballot(eq);
     const int eq_rank = equals + __builtin_popcountll(es & lower);
@@ -1004,17 +1063,22 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
       list[sure + __builtin_popcountll(ys & lower) + min(eq_rank, want)] = at;
     sure += __builtin_popcountll(ys);
     equals += __builtin_popcountll(es);
-  };
-  if (in_regs) {
-    if (lo < hi) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) enlist(lo + 64 * i + lane, own.at[i], order_key(own.weight[i]));
-    }
-  } else {
-    evict_walk(a, s, sh, g, lo, hi, !in_lds, [&](int e, int at, float wt) {
-      enlist(e, at, in_lds ? keys[min(e, s.L - 1)] : order_key(wt));
-    });
-  }
+  });
+}
+
+__global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
+  __shared__ uint32_t hist[kBins];
+  __shared__ EvictShared sh;
+  EvictSeq s = evict_sequence(a, blockIdx.y, sh);
+  const int per = (s.L + 1023) / 1024 * 64;  // places of a wave
+  if (per <= 512)
+    evict_select<1, true>(a, s, sh, hist, per);
+  else if (per <= 512 * 4)
+    evict_select<4, true>(a, s, sh, hist, per);
+  else if (per <= 512 * 8)
+    evict_select<8, false>(a, s, sh, hist, per);
+  else
+    evict_select<0, false>(a, s, sh, hist, per);
 }
 
 // The same by several workgroups of a sequence and KV head, a launch for each pass:

@@ -176,14 +176,17 @@ int kf_kv_evict(const kf_shape* shape, void* k_pool, void* v_pool, float* k_scal
 namespace kf {
 
 // Sequences of many tokens, on the mean of what the table reserves, are told apart by
-// several workgroups each: 128K tokens 325 us by one and 54 by sixteen (8 KV heads), 48 of
-// 2K .. 64K 187 and 176 by three; but 16 of 16K 40 and 47 by two.
+// several workgroups each; by one, which reads their weights once, up to kHeldTokens, but
+// where the parts are few.  By one and by several, 8 KV heads, selection and a small move,
+// us: one of 30K tokens 52 and 61, of 64K 92 and 64; 8 of 64K 96 and 107, 16 of them 98 and
+// 190; 48 of 2K .. 64K 121 and 202; 4 of 128K 358 and 87, 16 of them 368 and 286.
 EvictLayout evict_layout(const kf_shape& s, int32_t max_keep) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   EvictLayout l{};
   const int64_t tokens = (int64_t)s.num_page_ids * KF_PAGE_SIZE / std::max(1, s.num_seqs);
-  l.parts = tokens < kOneWorkgroup ? 1 : (int32_t)std::min<int64_t>(kMaxParts, tokens / kPartTokens);
   const size_t units = (size_t)s.num_seqs * s.num_kv_heads;
+  l.parts = (int32_t)std::min<int64_t>(kMaxParts, tokens / kPartTokens);
+  if (tokens < kOneWorkgroup || (tokens <= kHeldTokens && units * l.parts > kFewParts)) l.parts = 1;
   while (l.parts > 1 && units * l.parts > kMostParts) --l.parts;
   l.list_off = up((size_t)s.num_seqs * 2 * sizeof(int32_t)) + 256;
   l.state_off = l.list_off + up(units * max_keep * sizeof(int32_t));

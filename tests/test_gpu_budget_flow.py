@@ -201,7 +201,7 @@ def test_calls_on_streams_at_once(gpu):
     """A window, weights and an eviction over caches of their own, in flight together."""
     import torch
     c1, c2 = Cache([3000, 900], H=2, part=1024, seed=1), Cache([2500, 400, 70], H=2, fp8=True, seed=2)
-    c3 = Evictable([30000, 2000], [3000, 500], H=2, part=9000, seed=3)
+    c3 = Evictable([90000, 2000], [3000, 500], H=2, part=9000, seed=3)
     r1, r2 = Rows(c1, [300, 20], 4, seed=3), Rows(c2, [30, 400, 3], 4, seed=4)
     lse = r2.oracle()[1].astype(np.float32)
     w0 = np.zeros((c2.k_pool.shape[0], 2, 16), np.float32)

@@ -214,10 +214,18 @@ def test_graph_replays_and_streams(gpu):
 
 @pytest.mark.parametrize("fp8", [False, True])
 def test_one_long_sequence_among_short_ones(gpu, fp8):
-    # more tokens than a workgroup keeps in LDS, where the launch has one per sequence
+    # a long one, where the launch has a workgroup per sequence
     lens = [40000] + [20] * 9
     c = Evictable(lens, [7000] + [15] * 9, H=1, fp8=fp8, part=9000, seed=12)
     check(c, 4, 500)
+
+
+@pytest.mark.parametrize("L", [8191, 8192, 8193, 16385, 32767, 32768, 32769, 65535, 65536, 65537])
+@pytest.mark.parametrize("part", [70000, 1000])
+def test_lengths_around_what_one_workgroup_holds(gpu, L, part):
+    c = Evictable([L] + [20] * 9, [L // 4] + [15] * 9, H=1, part=part, seed=L)
+    c.weights[np.random.default_rng(3).random(c.weights.shape) < 0.3] = 0.5
+    check(c, 4, L // 8)
 
 
 @pytest.mark.parametrize("keep,first,last", [(1, 0, 0), (9000, 0, 9000), (20000, 20000, 0),
@@ -225,6 +233,15 @@ def test_one_long_sequence_among_short_ones(gpu, fp8):
                                              (0, 0, 0)])
 def test_parts_of_a_long_sequence(gpu, keep, first, last):
     c = Evictable([30000, 9000], [keep, keep], H=2, part=7000, seed=13)
+    c.weights[np.random.default_rng(3).random(c.weights.shape) < 0.4] = 0.5
+    check(c, first, last)
+
+
+@pytest.mark.parametrize("keep,first,last", [(1, 0, 0), (9000, 0, 9000), (20000, 20000, 0),
+                                             (60000, 10, 10), (100000, 5, 5), (0, 0, 0)])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_parts_of_longer_sequences(gpu, keep, first, last, fp8):
+    c = Evictable([80000, 30000], [keep, keep], H=1, fp8=fp8, part=17000, seed=13)
     c.weights[np.random.default_rng(3).random(c.weights.shape) < 0.4] = 0.5
     check(c, first, last)
 
@@ -250,3 +267,26 @@ def test_refusals_of_a_long_sequence(gpu, what):
     lo, hi = c.seq_route_begin[bad], c.seq_route_begin[bad + 1]
     assert np.array_equal(got[3][lo:hi], c.routes[lo:hi])
     assert got[3][c.into[1 - bad], 3] == (900, 1000)[1 - bad]
+
+
+@pytest.mark.parametrize("what", ["page", "first_page", "dst_page", "cap", "row"])
+def test_refusals_of_longer_sequences(gpu, what):
+    """The same where several workgroups tell a sequence's tokens apart."""
+    c = Evictable([70000, 40000], [900, 1000], H=2, part=17500, seed=14)
+    row, into = int(c.seq_route_begin[1]), [int(x) for x in c.into]
+    bad = 0 if what == "first_page" else 1
+    if what == "page":
+        c.page_ids[c.routes[row + 1, 4] + 1000] = -1
+    elif what == "first_page":           # the first one that sequence 0's tokens go to
+        c.page_ids[c.routes[into[0], 4]] = -1
+    elif what == "dst_page":
+        c.page_ids[c.routes[into[1], 4] + 60] = c.k_pool.shape[0]
+    elif what == "cap":
+        c.routes[into[1], 5] = 3
+    else:
+        c.routes[row, 0] = 0
+    got = check(c, 4, 10)
+    assert got[6] == {"page": 4, "first_page": 4, "dst_page": 4, "cap": 1, "row": 2}[what]
+    lo, hi = c.seq_route_begin[bad], c.seq_route_begin[bad + 1]
+    assert np.array_equal(got[3][lo:hi], c.routes[lo:hi])
+    assert got[3][into[1 - bad], 3] == (900, 1000)[1 - bad]
