@@ -1350,9 +1350,10 @@ __device__ __forceinline__ void evict_page(const EvictArgs& a, int g, int page, 
       for (int i = 0; i < kVecs; ++i) y[i] = ld16(out + 1024 * i + 16 * lane);
     }
     // Tokens come in the order of their pages.  bf16: a page is read once for all of its
-    // own, two tokens at a time (48 agentic requests 719 us, 728 with four, 738 with one,
-    // 830 anew for every token); fp8, whose pages are half as large, anew for every token,
-    // four at a time (16 sequences 16K -> 3000 tokens 128 us, 142 .. 163 the other way).
+    // own, two tokens at a time (48 agentic requests moved in 528 us, 537 with four, 547
+    // with one, 640 anew for every token); fp8, whose pages are half as large, anew for
+    // every token, four at a time (16 sequences 16K -> 3000 tokens 87 us, 101 .. 122 the
+    // other way).
     constexpr int kTogether = FP8 ? 4 : 2;
     auto fresh = [&](int s) {
       return FP8 || s == 0 || (__builtin_amdgcn_readlane(mine, s) ^

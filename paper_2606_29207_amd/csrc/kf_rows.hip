@@ -591,8 +591,9 @@ __global__ __launch_bounds__(1024) void rows_plan_kernel(RowsArgs a) {
     b = lo;
     wrong = info[4 * b + 2] != 0;
     if (wrong) return 1;
-    const int k = key_tiles<TREE, WINDOW>(a, TREE ? 0 : pos[b], t - tiles_of[b], begin[b + 1] - begin[b],
-                                  info[4 * b], info[4 * b + 1], info[4 * b + 3]);
+    const int k = key_tiles<TREE, WINDOW>(a, TREE ? 0 : pos[b], t - tiles_of[b],
+                                          begin[b + 1] - begin[b], info[4 * b], info[4 * b + 1],
+                                          info[4 * b + 3]);
     return k > 0 ? k : 1;
   };
   int own_b = 0, own_k = 0;  // this thread's first tile
@@ -1741,7 +1742,8 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(RowsArgs a) {
     w.walk.r = route0;
     w.walk.r_end = route1;
     if (WINDOW) {
-      walk_route<WINDOW, WINDOW && !FP8>(w.walk, sight, it.tok_begin, it.tok_end, it.page_base, it.key0);
+      walk_route<WINDOW, WINDOW && !FP8>(w.walk, sight, it.tok_begin, it.tok_end, it.page_base,
+                                         it.key0);
     } else {
       w.walk.n = see;
       w.walk.tb = it.tok_begin;

@@ -150,7 +150,7 @@ def test_binding_refuses_host_tensors_and_odd_sizes():
 @pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
 def test_host_layer_under_asan_and_ubsan(tmp_path):
     """kf_budget_api.cpp built with g++ under both sanitizers against a host-only HIP test
-    double, its launchers replaced by checkers (tests/c/budget_stress.cpp)."""
+    double, its launchers replaced by checking ones (tests/c/budget_stress.cpp)."""
     san = ["-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-fno-omit-frame-pointer"]
     src = os.path.join(ROOT, "paper_2606_29207_amd", "csrc")
     inc = ["-I", os.path.join(ROOT, "tests", "c", "hipstub"), "-I", os.path.join(ROOT, "include"),
