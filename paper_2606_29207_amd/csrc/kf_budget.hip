@@ -763,8 +763,13 @@ __device__ __forceinline__ EvictSeq evict_sequence(const EvictArgs& a, int b, Ev
   s.K = min(s.L, keep);
   s.base = to.page_base;
   const int64_t pages = ((int64_t)s.K + kPage - 1) / kPage;
+  // (first of these: a full target is full wherever its reservation lies in the table)
+  if (pages > to.page_cap) {
+    s.status = KF_EFLAG_TAIL_FULL;
+    return s;
+  }
   if ((int64_t)to.tok_begin + s.K > INT32_MAX || to.page_base + pages > a.num_page_ids) return s;
-  s.status = pages > to.page_cap ? KF_EFLAG_TAIL_FULL : 0;
+  s.status = 0;
   const int first = min(s.K, a.keep_first), last = min(s.K - first, a.keep_last);
   s.c0 = first;
   s.c1 = s.L - last;

@@ -161,6 +161,20 @@ def evict_oracle(c, first, last, max_keep=None):
                            k_scale=c.k_scale, v_scale=c.v_scale)
 
 
+def evict_parts(c, max_keep=None, G=2):
+    """Into how many parts an eviction's launch divides a sequence and KV head, from the
+    workspace that it asks for: a list of max_keep places each, and for each of several
+    parts 4 words and 3 x 2048 bins."""
+    from paper_2606_29207_amd import kf
+    max_keep = int(c.keep.max()) if max_keep is None else max_keep
+    units, up = len(c.lens) * c.H, lambda x: -(-x // 256) * 256
+    more = (kf.kv_evict_workspace_bytes(c.shape(c.H * G), max_keep) - up(len(c.lens) * 8) - 256
+            - up(units * max_keep * 4))
+    parts = more // (units * 4 * (4 + 3 * 2048))
+    assert more == parts * units * 3 * 2048 * 4 + up(parts * units * 16)
+    return max(1, parts)
+
+
 def evict_gpu(c, first, last, max_keep=None, head_major=False, G=2, stream=None, run=True, d=None):
     """k_pool, v_pool, weights, routes, k_scale, v_scale (numpy, as the oracle lays them
     out) and flags of kf_kv_evict."""

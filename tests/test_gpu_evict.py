@@ -2,7 +2,8 @@
 import numpy as np
 import pytest
 
-from budget_testlib import (Evictable, assert_evicted, evict_gpu, evict_oracle, evict_result)
+from budget_testlib import (Evictable, assert_evicted, evict_gpu, evict_oracle, evict_parts,
+                            evict_result)
 
 pytestmark = pytest.mark.gpu
 
@@ -290,3 +291,23 @@ def test_refusals_of_longer_sequences(gpu, what):
     lo, hi = c.seq_route_begin[bad], c.seq_route_begin[bad + 1]
     assert np.array_equal(got[3][lo:hi], c.routes[lo:hi])
     assert got[3][into[1 - bad], 3] == (900, 1000)[1 - bad]
+
+
+@pytest.mark.parametrize("how", ["short", "end"])
+@pytest.mark.parametrize("long", [False, True])
+def test_a_full_target_at_the_end_of_the_page_table_is_full(gpu, how, long):
+    """Too few pages reserved is a full tail wherever the route lies: also where the pages
+    that it lacks (or the tokens' places) would be beyond the table."""
+    c = (Evictable([70000, 40000], [900, 1000], H=2, part=17500, seed=14) if long else
+         Evictable([100, 150], [40, 50], H=2, part=64, seed=9))
+    to = int(c.into[1])
+    assert (evict_parts(c) > 1) == long
+    c.routes[to, 5] -= 1
+    if how == "short":                   # the last reservation ends with the table
+        c.page_ids = c.page_ids[:c.routes[to, 4] + c.routes[to, 5]]
+    else:
+        c.routes[to, 2:4] = 2 ** 31 - 20
+    lo = int(c.seq_route_begin[1])
+    got = check(c, 4, 10)
+    assert got[6] == 1 and np.array_equal(got[3][lo:], c.routes[lo:])
+    assert got[3][c.into[0], 3] == c.keep[0]
