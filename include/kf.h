@@ -546,9 +546,11 @@ int kf_attn_weights(const kf_shape* shape, const void* q, int32_t num_rows, int6
  * stays): kf_kv_append goes on from either.
  * A sequence is evicted whole or not at all.  Device checks (flag, that sequence
  * unchanged): its CSR row, at most 1024 routes, each sound (kf_partial_attn's checks)
- * and its own, into[b] among them and empty, 0 <= keep[b] <= max_keep, L below 2^31 -
- * 1024 (KF_EFLAG_BAD_ROUTE); pages reserved for K tokens (KF_EFLAG_TAIL_FULL); page
- * ids of the tokens and of the pages that they go to (KF_EFLAG_BAD_PAGE).
+ * and its own, into[b] among them and empty, and sound with K tokens too (so that
+ * max_pages_per_route bounds the pages of what stays as well), 0 <= keep[b] <= max_keep,
+ * L below 2^31 - 1024 (KF_EFLAG_BAD_ROUTE); pages reserved for K tokens
+ * (KF_EFLAG_TAIL_FULL); page ids of the tokens and of the pages that they go to
+ * (KF_EFLAG_BAD_PAGE).
  * workspace: kf_kv_evict_workspace_bytes(shape, max_keep), 16-byte aligned; dead
  * between calls, and calls that may overlap need their own.  0 for invalid
  * arguments and for more than 65535 sequences or KV heads, which no launch takes.

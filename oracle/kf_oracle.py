@@ -533,7 +533,8 @@ def kv_evict(k_pool, v_pool, weights, routes, page_ids, seq_route_begin, into, k
         if pages > routes[to][5]:
             flags |= EFLAG_TAIL_FULL
             continue
-        if int(routes[to][2]) + K > 2 ** 31 - 1 or int(routes[to][4]) + pages > len(page_ids):
+        if (int(routes[to][2]) + K > 2 ** 31 - 1 or int(routes[to][4]) + pages > len(page_ids)
+                or pages > max_pages_per_route):
             flags |= EFLAG_BAD_ROUTE
             continue
         spid = np.array([page_ids[p] for p, _ in src], np.int64).reshape(-1)

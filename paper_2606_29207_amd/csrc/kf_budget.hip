@@ -768,7 +768,10 @@ __device__ __forceinline__ EvictSeq evict_sequence(const EvictArgs& a, int b, Ev
     s.status = KF_EFLAG_TAIL_FULL;
     return s;
   }
-  if ((int64_t)to.tok_begin + s.K > INT32_MAX || to.page_base + pages > a.num_page_ids) return s;
+  // the row that it leaves: as sound as those it came from
+  if ((int64_t)to.tok_begin + s.K > INT32_MAX || pages > a.max_pages_per_route ||
+      to.page_base + pages > a.num_page_ids)
+    return s;
   s.status = 0;
   const int first = min(s.K, a.keep_first), last = min(s.K - first, a.keep_last);
   s.c0 = first;

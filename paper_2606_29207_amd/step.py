@@ -281,6 +281,7 @@ class DecodeState:
               keep_last: int, stream=None):
         """Moves what stays of each sequence, by `weights`, into the pages of its empty
         route into[b] (kf_kv_evict); the other routes of the sequence are empty then.
+        Its pages of what stays are within max_pages_per_route, as every route's.
         Appends go on in into[b]: write it into tail_route, whose decode steps read it."""
         with torch.cuda.stream(stream):
             kf.kv_evict(self.shape, self.k_pool, self.v_pool, self.weights, self.routes,

@@ -311,3 +311,17 @@ def test_a_full_target_at_the_end_of_the_page_table_is_full(gpu, how, long):
     got = check(c, 4, 10)
     assert got[6] == 1 and np.array_equal(got[3][lo:], c.routes[lo:])
     assert got[3][c.into[0], 3] == c.keep[0]
+
+
+@pytest.mark.parametrize("long", [False, True])
+def test_what_stays_is_a_route_that_the_bounds_of_the_call_hold(gpu, long):
+    """More pages of tokens than max_pages_per_route would be a bad route to every call
+    behind the eviction: refused, and the sequence as it was."""
+    c = (Evictable([70000, 40000], [900, 17000], H=2, part=16384, seed=14) if long else
+         Evictable([100, 150, 80], [40, 50, 30], H=2, part=32, seed=9))
+    c.max_pages = 1024 if long else 3
+    assert (evict_parts(c) > 1) == long
+    lo, hi = c.seq_route_begin[1:3]
+    got = check(c, 4, 10)
+    assert got[6] == 2 and np.array_equal(got[3][lo:hi], c.routes[lo:hi])
+    assert all(got[3][c.into[b], 3] == c.keep[b] for b in range(len(c.lens)) if b != 1)
