@@ -325,3 +325,58 @@ def test_what_stays_is_a_route_that_the_bounds_of_the_call_hold(gpu, long):
     got = check(c, 4, 10)
     assert got[6] == 2 and np.array_equal(got[3][lo:hi], c.routes[lo:hi])
     assert all(got[3][c.into[b], 3] == c.keep[b] for b in range(len(c.lens)) if b != 1)
+
+
+@pytest.mark.parametrize("how", ["equal", "zero", "two", "negative", "odd", "close"])
+def test_weights_that_are_alike_or_odd_in_several_parts(gpu, how):
+    """Told apart by several workgroups, beside a sequence left alone, short ones and an
+    empty one."""
+    c = Evictable([120000, 120000, 9000, 700, 0], [9000, 9, 3000, 300, 5], H=1, part=17000, seed=3)
+    c.into[1] = -1
+    assert evict_parts(c) > 1
+    rng = np.random.default_rng(5)
+    w = c.weights
+    if how == "equal":
+        w[:] = 0.25
+    elif how == "zero":
+        w[:] = 0.0
+        w[rng.random(w.shape) < 0.5] = -0.0
+    elif how == "two":
+        w[:] = np.where(rng.random(w.shape) < 0.05, 1.5, 0.125)
+    elif how == "negative":
+        w[:] = rng.standard_normal(w.shape)
+    elif how == "odd":
+        w[:] = rng.choice(np.array([np.nan, np.inf, -np.inf, 0.0, -0.0, 1e-45, -1e-45, 3.0],
+                                   np.float32), w.shape)
+    else:                                # differ in their last bits alone
+        w[:] = (np.float32(1.0).view(np.uint32) + rng.integers(0, 40, w.shape, np.uint32)
+                ).view(np.float32)
+    got = check(c, 1, 5, how)
+    assert got[6] == 0
+
+
+@pytest.mark.parametrize("L", [8191, 8192, 8193, 40000, 65536, 65537])
+def test_lengths_in_several_parts(gpu, L):
+    """Around the parts' own edges, beside a sequence that makes the mean a long one."""
+    c = Evictable([L, 200000], [L // 3, 100], H=1, part=1000, seed=L)
+    c.weights[np.random.default_rng(3).random(c.weights.shape) < 0.3] = 0.5
+    assert evict_parts(c) > 1
+    check(c, 4, L // 8)
+
+
+@pytest.mark.parametrize("what", ["equal", "nan", "all", "none", "edges"])
+def test_where_the_threshold_lies_in_several_parts(gpu, what):
+    """None or all of what competes stays; ties over every part; wanted ones that end at a
+    part's edge."""
+    L = 131072
+    keep = {"all": L, "none": 1200, "edges": 4 + 1000 + 16384}.get(what, 20000)
+    c = Evictable([L], [keep], H=2, part=30000, seed=5)
+    assert evict_parts(c) > 1
+    if what == "nan":
+        c.weights[:] = np.nan
+    elif what != "all":
+        c.weights[:] = 0.5
+    if what == "none":
+        check(c, 200, 1000)
+    else:
+        check(c, 4, 1000)
