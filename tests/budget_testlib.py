@@ -103,6 +103,17 @@ def weights_gpu(r, lse, weights, decay, scale=SCALE, head_major=False, pad=0, st
     return w.cpu().numpy(), int(d["err"].item())
 
 
+def weights_segments(r, chunk_pages=16):
+    """How many workgroups share the columns of the same keys, from the workspace that the
+    launch asks for: 256 sums of each, for stretches of chunk_pages pages."""
+    from paper_2606_29207_amd import kf
+    c = r.cache
+    n, R = kf.attn_weights_workspace_bytes(c.shape(r.q.shape[1]), r.q.shape[0], len(c.routes),
+                                           c.max_pages), len(c.routes)
+    chunks = -(-min(c.max_pages, len(c.page_ids)) // chunk_pages)
+    return max(1, n // (R * chunks * c.H * 1024))
+
+
 def assert_weights(got, ref, before, what=""):
     """Weights against the oracle's.  A term exp(s - lse) is off by what its exponent is:
     the 128 products of a score, added in 32 bits, by at most 128 x 2^-24 of the sum of

@@ -3,7 +3,8 @@
 import numpy as np
 import pytest
 
-from budget_testlib import assert_weights, rows_lse, start_weights, weights_gpu, weights_oracle
+from budget_testlib import (assert_weights, rows_lse, start_weights, weights_gpu, weights_oracle,
+                            weights_segments)
 from rows_testlib import Cache, Rows
 
 pytestmark = pytest.mark.gpu
@@ -217,3 +218,48 @@ def test_same_bits_graph_replays_and_streams(gpu):
         torch.cuda.synchronize()
         assert np.array_equal(w.cpu().numpy(), twice), i
     assert err.item() == 0
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_many_columns_over_stretches_of_32_pages(gpu, fp8):
+    # a mean of 133 columns: workgroups of 32 pages, which the one sequence of more than
+    # 256 columns takes 16 at a time
+    c = Cache([2000, 900, 300, 40], H=2, fp8=fp8, seed=3)
+    r = Rows(c, [130, 1, 1, 1], 4, seed=5)
+    assert weights_segments(r, chunk_pages=32) == 1
+    check(r)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("rows,segments", [(70, 2), (96, 3), (128, 4), (160, 5), (192, 6), (224, 7),
+                                           (256, 8), (400, 8)])
+def test_every_number_of_segments(gpu, rows, segments, fp8):
+    c = Cache([700], H=2, fp8=fp8, part=300, seed=rows)
+    r = Rows(c, [rows], 4, seed=rows)
+    assert weights_segments(r) == segments
+    check(r)
+
+
+@pytest.mark.parametrize("spare,segments", [(550, 1), (1300, 1), (260, 4)])
+def test_long_prompts_of_many_routes(gpu, spare, segments):
+    # so many workgroups that each takes all columns of its keys, or four share them
+    c = Cache([300, 310, 290], H=2, part=32, spare=spare, seed=spare)
+    r = Rows(c, [300, 280, 100], 4, seed=3)
+    assert weights_segments(r) == segments
+    check(r)
+
+
+@pytest.mark.parametrize("rows", [1, 100, 600])
+def test_stretches_that_a_launch_s_limit_makes_longer(gpu, rows):
+    # 18 stretches of 16 pages, 16 KV heads and 60002 routes would be more than 2^24
+    # workgroups: twice as many pages each
+    c = Cache([600, 0], H=16, part=320, seed=4)
+    n, k = 60000, len(c.page_ids)
+    c.routes = np.concatenate([c.routes, np.tile(np.array([[1, 9, 0, 0, k, 0]], np.int32), (n, 1))])
+    c.page_ids = np.concatenate([c.page_ids, np.full(288 - k, -1, np.int32)])
+    c.max_pages = 288
+    r = Rows(c, [rows, 0], 1, first_pos=[600 - rows, 0], seed=rows)
+    w = start_weights(c)
+    lse = (4.0 + np.random.default_rng(1).random((rows, 16))).astype(np.float32)
+    got = weights_gpu(r, lse, w, 0.7)
+    assert_weights(got, weights_oracle(r, lse, w, 0.7), w)
