@@ -493,12 +493,15 @@ int kf_tree_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64_t
  * call (one row per sequence, first_pos its position), a prompt's and a chunk's
  * need no clearing (a token that was new in no call has what its slot held before);
  * with decay = 0 weights are not read.  A row whose lse is -inf
- * or NaN gives nothing.  Sums are float32; the same arguments give the same bits.
+ * or NaN gives nothing.  Sums are float32; the same arguments give the same bits, but
+ * for pages that routes share (below).
  * q and lse as for kf_prompt_attn (q_stride elements between rows of q).
  * Routes are taken one by one, as kf_partial_attn takes them, and weights of
  * sequences without rows, and of slots that hold no token, are left as they were.
- * A page in several routes of sequences with rows (a prefix that they share) ends
- * with the weights that one of them gives, any one, which is not detected: give
+ * The weights of a page in several routes of sequences with rows (a prefix that they
+ * share) are unspecified: each of its routes reads and writes them, in no order, so
+ * that one of them may be lost, or decay and add to what another has just written, and
+ * another call of the same arguments may give others.  This is not detected: give
  * such sequences their rows in calls of their own, the later ones with decay = 1.
  * max_pages_per_route as for kf_prompt_attn.
  * Device checks: a route whose sequence is outside [0, num_seqs), or whose

@@ -263,3 +263,23 @@ def test_stretches_that_a_launch_s_limit_makes_longer(gpu, rows):
     lse = (4.0 + np.random.default_rng(1).random((rows, 16))).astype(np.float32)
     got = weights_gpu(r, lse, w, 0.7)
     assert_weights(got, weights_oracle(r, lse, w, 0.7), w)
+
+
+@pytest.mark.parametrize("rows", [1, 40, 100])
+def test_sequences_that_share_pages_in_calls_of_their_own(gpu, rows):
+    """A prefix of 96 tokens in the routes of two sequences: each has its rows in a call
+    of its own, the second one's with decay = 1."""
+    c = Cache([250, 250], H=2, part=96, seed=4)
+    a, b = c.seq_route_begin[:2]
+    c.routes[b, 4] = c.routes[a, 4]
+    w, ref = start_weights(c), start_weights(c).astype(np.float64)
+    before = np.abs(w)
+    flags = terms = 0
+    for k, decay in ((0, 0.5), (1, 1.0)):
+        r = Rows(c, [rows * (k == 0), rows * (k == 1)], 4, first_pos=[250 - rows] * 2, seed=k)
+        lse = rows_lse(r)
+        ref, flags, n = weights_oracle(r, lse, ref, decay)
+        terms += n
+        w, got = weights_gpu(r, lse, w, decay)
+        assert got == flags == 0
+    assert_weights((w, 0), (ref, 0, terms), before)
