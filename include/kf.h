@@ -439,7 +439,9 @@ int kf_prompt_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64
  * row sees are not read, but every route of the sequence is checked and t, p are
  * logical positions, so that a launch costs what its rows see, whatever the cache
  * holds.  sinks, window >= 0.  Arguments, outputs, checks, alignment and workspace
- * (kf_rows_attn_workspace_bytes) otherwise as for kf_prompt_attn.
+ * (kf_rows_attn_workspace_bytes) otherwise as for kf_prompt_attn, and so is the
+ * precision, of decode steps too: bfloat16 weights and outputs, about 2e-3 (L2), where
+ * kf_decode_step's float32 outputs are within 5e-6.
  */
 int kf_window_attn(const kf_shape* shape, const void* q, int32_t num_rows, int64_t q_stride,
                    const int32_t* seq_row_begin, const int32_t* first_pos, int32_t sinks,
@@ -554,7 +556,9 @@ int kf_attn_weights(const kf_shape* shape, const void* q, int32_t num_rows, int6
  * L below 2^31 - 1024 (KF_EFLAG_BAD_ROUTE); pages reserved for K tokens
  * (KF_EFLAG_TAIL_FULL); page ids of the tokens and of the pages that they go to
  * (KF_EFLAG_BAD_PAGE).
- * workspace: kf_kv_evict_workspace_bytes(shape, max_keep), 16-byte aligned; dead
+ * workspace: kf_kv_evict_workspace_bytes(shape, max_keep), 16-byte aligned (4 bytes a
+ * kept token and KV head, and where several workgroups tell a sequence's tokens apart
+ * 24 KB for each of them, 100 MB at most); dead
  * between calls, and calls that may overlap need their own.  0 for invalid
  * arguments and for more than 65535 sequences or KV heads, which no launch takes.
  * Alignment: pools 16 bytes, the rest 4.

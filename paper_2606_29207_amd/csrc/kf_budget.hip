@@ -70,7 +70,9 @@ __device__ __forceinline__ void few_columns(const AttnWeightsArgs& a, const Seen
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int n16 = lane & 15, grp = lane >> 4, H = a.num_kv_heads, G = a.group;
   const uint32_t C = (uint32_t)s.rows * G;
-  constexpr int kStep = 4 * kBatch;  // the four waves take batches in turn
+  // The four waves take batches in turn (of a workgroup's 16 pages: bf16 two a wave, fp8
+  // one, whose second buffer is not used then).
+  constexpr int kStep = 4 * kBatch;
   int p = s.p0 + kBatch * wave;
   if (p >= s.p1) return;
   buf_x += 8192 * wave;
@@ -212,8 +214,10 @@ __device__ __forceinline__ void lds_barrier() {  // for LDS that the waves wrote
 // exponentials of the one before it, two a step in turn, with its own columns in
 // registers, those behind them in LDS and others on their way.  2000 rows behind 30K
 // tokens, 32 / 8 heads: 540 us, 0.94 PFLOP/s (the largest plain product reaches 1.19).
-// With 64 and 128 keys a workgroup (its waves then also beside each other along the
-// columns) 690 and 585, with eight waves 550 .. 680.
+// 40 vector registers are spilled (fp8 43), most of them outside the loops; the loop of
+// columns that some keys are hidden from reloads three.  With 64 and 128 keys a workgroup
+// (its waves then also beside each other along the columns) 690 and 585, with eight waves
+// 550 .. 680.
 template <bool FP8>
 struct Columns {
   static constexpr int kCols = 32, kStep = kCols * 256;  // bytes of a step in LDS
@@ -746,7 +750,7 @@ __device__ __forceinline__ EvictSeq evict_sequence(const EvictArgs& a, int b, Ev
     bad = bad || (r0 + own == into && n != 0);
     if (!few || w == 0) sh.base[own] = row.page_base;
   }
-  // (64 bits: a route has up to 2^31 - 1 tokens)
+  // (64 bits: a route has up to kMostTokens, a sequence many of them)
   const int64_t x = wave_scan((int64_t)n, lane);
   int64_t all = __shfl((long long)x, 63), before = 0;
   if (few) {

@@ -175,11 +175,17 @@ int kf_kv_evict(const kf_shape* shape, void* k_pool, void* v_pool, float* k_scal
 
 namespace kf {
 
-// Sequences of many tokens, on the mean of what the table reserves, are told apart by
-// several workgroups each; by one, which reads their weights once, up to kHeldTokens, but
-// where the parts are few.  By one and by several, 8 KV heads, selection and a small move,
-// us: one of 30K tokens 52 and 61, of 64K 92 and 64; 8 of 64K 96 and 107, 16 of them 98 and
-// 190; 48 of 2K .. 64K 121 and 202; 4 of 128K 358 and 87, 16 of them 368 and 286.
+// Sequences of many tokens, on the mean of what the table reserves (the pages that what
+// stays goes to among it), are told apart by several workgroups each; by one, which reads
+// their weights once, up to kHeldTokens, but where the parts are few.  By one and by
+// several, 8 KV heads, 64 tokens kept, the whole call, us: one of 30K tokens 52 and 61, of
+// 40K 67 and 60, of 64K 92 and 52; 8 of 40K 70 and 70, of 64K 96 and 84, 16 of 64K 98 and
+// 151; 48 of 2K .. 64K 116 and 196; 4 of 128K 347 and 86, 16 of them 361 and 284.  With
+// 4096 kept, one of 30K 62 and 58, of 40K 80 and 61, 8 of 64K 258 and 242, 16 of them 420
+// and 472: those of 64K count as 68K and go by several, 16 of them to their loss.  The mean
+// less max_keep would send these by one, but 8 of 64K and one of 40K too.  (The sequences'
+// own tokens are not known here: where they differ much, or two routes of full length take
+// turns, the mean is not theirs.)
 EvictLayout evict_layout(const kf_shape& s, int32_t max_keep) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   EvictLayout l{};
@@ -201,8 +207,8 @@ EvictLayout evict_layout(const kf_shape& s, int32_t max_keep) {
 void plan_attn_weights(AttnWeightsArgs& a, int64_t slots) {
   const int64_t most = std::max(1, std::min(a.max_pages_per_route, a.num_page_ids));
   const int64_t columns = (int64_t)a.num_rows * a.group / std::max(1, a.num_seqs);
-  // A workgroup's pages: 16 (one decode row over 32K tokens, 16 sequences, 190 us; 8 and
-  // 32 212 and 195, 64 204, 128 222, 256 195), where the columns stay in LDS twice as many
+  // A workgroup's pages: 16 (one decode row over 32K tokens of bf16, 16 sequences, 190 us; 8
+  // and 32 212 and 195, 64 204, 128 222, 256 195), where the columns stay in LDS twice as many
   // (74 us, 80 with 16, 77 with 64).
   int64_t chunk = columns > kFewColumns && columns <= kHeldColumns ? 32 : 16;
   while (div_up(most, chunk) * a.num_kv_heads * a.num_routes > kMaxBudgetWgs) chunk *= 2;

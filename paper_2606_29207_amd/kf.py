@@ -652,7 +652,7 @@ def bind_window_attn(shape: Shape, q, first_pos, sinks, window, k_pool, v_pool, 
                      workspace, err_flags, k_scale=None, v_scale=None) -> BoundCall:
     """kf_window_attn bound to its buffers; call it as (stream).  A row at position p
     sees the tokens t <= p with t < sinks or t > p - window; the rest as for
-    bind_prompt_attn (a decode step: one row per sequence)."""
+    bind_prompt_attn, its precision too (a decode step: one row per sequence)."""
     _dev(first_pos, "first_pos", torch.int32)
     _need(first_pos.numel() >= shape.num_seqs, "first_pos must be int32 [num_seqs]")
     sinks, window = int(sinks), int(window)
@@ -784,7 +784,9 @@ def bind_kv_evict(shape: Shape, k_pool, v_pool, weights, routes, max_pages_per_r
     sequence's empty route that takes what stays (-1: leave it alone); keep int32 [B],
     at most max_keep: tokens that stay, the first keep_first and the last keep_last
     among them; pools, scales, weights float32 [P, Hkv, 16] and routes are updated.
-    workspace=None allocates what the call needs (4 bytes a kept token and KV head)."""
+    workspace=None allocates what the call needs (kv_evict_workspace_bytes: 4 bytes a kept
+    token and KV head, and where several workgroups tell a sequence's tokens apart 24 KB
+    for each of them, 100 MB at most)."""
     B = shape.num_seqs
     for t, n in ((k_pool, "k_pool"), (v_pool, "v_pool"), (routes, "routes"),
                  (page_ids, "page_ids"), (err_flags, "err_flags")):
